@@ -488,7 +488,9 @@ def _exact_route(s):
             value, place = left.max(dim=2, keepdim=True)
             total += value[:, :, 0]
             left.scatter_(2, place, -1e30)
-        better = (total[:, None, :] > total[:, :, None]).sum(dim=2)
+        group = torch.arange(case["groups"], device="cuda")
+        first = group[None, :] < group[:, None]   # of two equal groups the first
+        better = ((total[:, None, :] > total[:, :, None]) | ((total[:, None, :] == total[:, :, None]) & first)).sum(dim=2)
         c = c.view(T, case["groups"], -1).masked_fill((better >= case["top_groups"])[:, :, None], -1e30).view(T, E)
     place = torch.arange(E, device="cuda")
     ids = []
