@@ -431,6 +431,108 @@ hm_status hm_swap_select(int32_t d, const int32_t *U /* host */, int32_t G, int3
  */
 hm_status hm_swap_apply(int32_t *expert_to_rank, int32_t E, const int32_t *best_pair, void *hip_stream);
 
+/*
+ * ---- The router in front of the dispatch -------------------------------------------------------
+ *
+ * hm_route -- routing to experts: logits [T,E] -> topk_ids, topk_weights [T,K] as hm_plan takes them.
+ *     score    s = softmax(x) over the row, or 1 / (1 + exp(-x))
+ *     choice   c = s + bias; without a bias the order of the logits themselves decides
+ *     groups   the E experts are cut into `groups` contiguous equal groups; a group's score is the sum of its
+ *              group_best (1 or 2) largest choices (of scores without a bias, up to softmax's common factor),
+ *              and only experts of the top_groups best groups are chosen.  1, 1: no limit
+ *     ids      the K largest choices, descending; of equal ones (groups too) the lowest index first
+ *     weights  w = scale * s, divided by the sum of the K chosen scores if `renormalise`
+ * An expert whose logit is -infinity or NaN is never chosen and no part of a softmax; +infinity counts as the largest
+ * finite number.  Slots that no expert is left for get the id -1, a slot the router dropped, and weight 0; with
+ * no score above 0 to divide by all weights are 0.  Scores are fp32; a logistic score below 2^-126 may be 0.
+ *   logits: dtype HM_F32 or HM_BF16, row t from element t*ld on (ld >= E).  bias [E] fp32 or NULL.
+ * Limits: E <= 4096, K <= 64, K <= the experts of top_groups groups (else HM_ERR_SHAPE, as for top_groups > groups,
+ * groups not dividing E, group_best other than 1 or 2 or above the experts of a group).
+ */
+typedef enum { HM_BF16 = 0, HM_F32 = 1 } hm_dtype;
+typedef enum { HM_SCORE_SOFTMAX = 0, HM_SCORE_SIGMOID = 1 } hm_score;
+typedef struct {
+  int32_t E, K;
+  int32_t score;                  /* hm_score */
+  int32_t groups, top_groups, group_best;
+  int32_t renormalise;
+  float scale;
+} hm_router;
+hm_status hm_route(const void *logits, hm_dtype dtype, int64_t ld, const float *bias, int32_t T,
+                   const hm_router *router /* host */, int32_t *topk_ids, float *topk_weights, void *hip_stream);
+
+/*
+ * hm_route_backward -- gradient of the logits from that of the weights, g = grad_weights [T,K] fp32.  The choice is
+ * a constant of the pass: with S the ids of a token that lie in [0,E) and s as in hm_route,
+ *     logistic             dx_k = scale g_k s_k (1 - s_k)                                        k in S
+ *     logistic, normalised dx_k = scale / sum_S s * (g_k - sum_S g s / sum_S s) s_k (1 - s_k)    k in S
+ *     softmax              dx_i = scale s_i (g_i [i in S] - sum_S g s)                           every i
+ *     softmax, normalised  dx_k = scale u_k (g_k - sum_S g u),  u = s / sum_S s                  k in S
+ * and 0 for the others and for experts hm_route never chooses.  The ids of a token are distinct, as hm_route writes
+ * them.  groups, top_groups and group_best do not matter.  grad_logits has the dtype of the logits, row t from element
+ * t*grad_ld on; fp32 arithmetic.  Together with hm_combine_weight_grad this is the router's way back.
+ */
+hm_status hm_route_backward(const void *logits, hm_dtype dtype, int64_t ld, const int32_t *topk_ids,
+                            const float *grad_weights, int32_t T, const hm_router *router /* host */,
+                            void *grad_logits, int64_t grad_ld, void *hip_stream);
+
+/*
+ * hm_combine_weight_grad -- gradient of hm_combine's output for the router weights:
+ *     grad_weights[t,k] = sum_h gout[t,h] * y[slot_row[t,k], h],   fp32 accumulation,
+ * 0 for dropped slots and for rows outside [0,y_rows) (the latter flagged HM_ERR_CAPACITY).  gout [T,H] and y [y_rows,H]
+ * are both bf16 or both fp32 (dtype).  Uses plan->slot_row, status.  The slots of a token that share a row get the same
+ * gradient.  Any H and any alignment of the elements.
+ */
+hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype, int64_t y_rows, int32_t T, int32_t K,
+                                 int32_t H, const hm_plan_out *plan, float *grad_weights, void *hip_stream);
+
+/*
+ * ---- The experts behind it: products in 8 bits -------------------------------------------------
+ * Values are e4m3 (no infinities, largest 448) with one power of two for each block of 128 values, a byte whose code
+ * - 127 is the exponent (code 255: NaN).  hm_quantize_*: the least exponent with which no value of the block exceeds
+ * 448, at least -127; values are divided by it, which is exact, and rounded to nearest even.  NaN and infinities become NaN and
+ * do not count for the exponent.  Powers of two lose at most one bit of the scale, cost the matrix unit nothing and make every
+ * byte reproducible.  Layouts, with up(n,m) the multiple of m from n on:
+ *   rows     [rows, up(C,128)], zeros behind the C values; a block is 128 columns of a row; scales [rows, up(C,512)/128],
+ *            zeros behind the ceil(C/128) codes (so both travel through hm_dispatch_pack as rows of 2-byte units)
+ *   weights  [experts, N, up(C,128)] likewise; a block is 128 x 128; scales [experts, ceil(N/128), up(C,512)/128]
+ *   columns  of rows ordered by expert (segment e: rows offsets[e] .. offsets[e+1] - 1, as in hm_plan_mapped's
+ *            dest_offset), transposed: [C, 128 B] with B = rows/128 (rounded down) + segments blocks; segment e owns the blocks from
+ *            offsets[e]/128 + e on, its rows in order, zeros behind them up to a whole block; a block is 128 rows of one
+ *            column; scales [B, C].  Blocks that no segment needs are not written
+ * 8-bit buffers are 16-byte aligned, scales 4-byte aligned (HM_ERR_SHAPE otherwise).  offsets that descend or lie outside [0,rows]
+ * are data errors: no access leaves the buffers, the results are unspecified.
+ *
+ * x: dtype HM_F32 or HM_BF16, row r from element r*ld on, any alignment of the elements; fastest with whole 16-byte
+ * vectors.  hm_quantize_weights takes dense [experts, N, C]; with qt and scale_t it also writes the transposed weights
+ * [experts, C, up(N,128)], [experts, ceil(C/128), up(N,512)/128]: the same values, for the gradient of the rows.
+ */
+hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld, int64_t rows, int32_t C, uint8_t *q, uint8_t *scale,
+                           void *hip_stream);
+hm_status hm_quantize_columns(const void *x, hm_dtype dtype, int64_t ld, const int32_t *offsets, int32_t segments,
+                              int64_t rows, int32_t C, uint8_t *q, uint8_t *scale, void *hip_stream);
+hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, int32_t N, int32_t C, uint8_t *q,
+                              uint8_t *scale, uint8_t *qt /* may be NULL, with scale_t */, uint8_t *scale_t,
+                              void *hip_stream);
+
+/*
+ * hm_expert_matmul -- every row times the weights of its expert:
+ *     out[r,n] = sum_h x[r,h] w[e,n,h],   offsets[e] <= r < offsets[e+1],   fp32 accumulation, rounded once.
+ * x, w with their scales in the layouts `rows` and `weights` above (C = H), offsets device int32[experts + 1], out
+ * [rows,N] of out_dtype; rows from offsets[experts] on are left alone.  With the rows of the output's gradient and the
+ * transposed weights (N and H exchanged) the same call is the gradient of x.
+ * hm_expert_matmul_dw -- the gradient of the weights:
+ *     dw[e,n,h] = sum over the rows r of segment e of gy[r,n] x[r,h],
+ * gy (C = N) and x (C = H) in the layout `columns`; dw [experts,N,H] of dw_dtype, zeros for an expert without rows.
+ * Limits: experts <= 1024, rows <= 2^31-1 - 128 * experts, N and H up to 2^20.
+ */
+hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, const uint8_t *w, const uint8_t *w_scale,
+                           const int32_t *offsets, int32_t experts, int64_t rows, int32_t N, int32_t H, void *out,
+                           hm_dtype out_dtype, void *hip_stream);
+hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_scale, const uint8_t *x, const uint8_t *x_scale,
+                              const int32_t *offsets, int32_t experts, int64_t rows, int32_t N, int32_t H, void *dw,
+                              hm_dtype dw_dtype, void *hip_stream);
+
 /* Static, human-readable name of a status code. */
 const char *hm_status_string(hm_status s);
 

@@ -39,6 +39,8 @@ except ImportError as e:
 
 HM_DEDUP_NONE, HM_DEDUP_GPU, HM_DEDUP_NODE = 0, 1, 2
 HM_RECV_INTRA_NODE, HM_RECV_LOCAL_EXPERTS = 0, 1
+HM_BF16, HM_F32 = 0, 1
+HM_SCORE_SOFTMAX, HM_SCORE_SIGMOID = 0, 1
 HM_OK = 0
 HM_ERR_NULL, HM_ERR_SHAPE, HM_ERR_TOPOLOGY, HM_ERR_LEVEL = -1, -2, -3, -4
 HM_ERR_WORKSPACE, HM_ERR_CAPACITY, HM_ERR_BAD_ID, HM_ERR_HIP = -5, -6, -7, -8
@@ -51,7 +53,9 @@ EXPORTS = ("hm_plan_workspace_bytes", "hm_plan", "hm_plan_status", "hm_dispatch_
            "hm_alltoall_times", "hm_swap_workspace_bytes", "hm_swap_counts", "hm_swap_select_workspace_bytes",
            "hm_swap_select", "hm_level_dest_map", "hm_combine_f32", "hm_swap_apply",
            "hm_swap_counts_multi", "hm_swap_multi_workspace_bytes", "hm_combine_transpose_bf16", "hm_plan_one_launch_limit", "hm_plan_one_launch_capacity",
-           "hm_plan_static", "hm_plan_static_max_bytes", "hm_combine_launch_shape")
+           "hm_plan_static", "hm_plan_static_max_bytes", "hm_combine_launch_shape", "hm_route", "hm_route_backward",
+           "hm_combine_weight_grad", "hm_quantize_rows", "hm_quantize_columns", "hm_quantize_weights", "hm_expert_matmul",
+           "hm_expert_matmul_dw")
 
 # The entry points _hmcall is handed, in the order of its Library struct.
 _NATIVE = ("hm_plan", "hm_plan_mapped", "hm_dispatch_pack", "hm_combine", "hm_combine_f32", "hm_combine_mix", "hm_combine_transpose",
@@ -72,6 +76,12 @@ class hm_plan_out(ctypes.Structure):
                 ("status", ctypes.c_void_p), ("load_expert", ctypes.c_void_p),
                 ("load_rank", ctypes.c_void_p), ("load_node", ctypes.c_void_p),
                 ("max_rows_per_token", ctypes.c_int32), ("expected_rows", ctypes.c_int64)]
+
+
+class hm_router(ctypes.Structure):
+    _fields_ = [("E", ctypes.c_int32), ("K", ctypes.c_int32), ("score", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("group_best", ctypes.c_int32), ("renormalise", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 class HierMoEError(RuntimeError):
@@ -159,6 +169,16 @@ def lib():
                                      ctypes.c_double, ctypes.c_double, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.hm_level_dest_map.restype = ctypes.c_int
         L.hm_level_dest_map.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, vp]
+        router, out = ctypes.POINTER(hm_router), ctypes.POINTER(hm_plan_out)
+        for name, args in (("hm_route", [vp, ctypes.c_int, i64, vp, i32, router, vp, vp, vp]),
+                           ("hm_route_backward", [vp, ctypes.c_int, i64, vp, vp, i32, router, vp, i64, vp]),
+                           ("hm_combine_weight_grad", [vp, vp, ctypes.c_int, i64, i32, i32, i32, out, vp, vp]),
+                           ("hm_quantize_rows", [vp, ctypes.c_int, i64, i64, i32, vp, vp, vp]),
+                           ("hm_quantize_columns", [vp, ctypes.c_int, i64, vp, i32, i64, i32, vp, vp, vp]),
+                           ("hm_quantize_weights", [vp, ctypes.c_int, i32, i32, i32, vp, vp, vp, vp, vp]),
+                           ("hm_expert_matmul", [vp, vp, vp, vp, vp, i32, i64, i32, i32, vp, ctypes.c_int, vp]),
+                           ("hm_expert_matmul_dw", [vp, vp, vp, vp, vp, i32, i64, i32, i32, vp, ctypes.c_int, vp])):
+            getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_int, args
         L.hm_status_string.restype = ctypes.c_char_p
         L.hm_status_string.argtypes = [ctypes.c_int]
         _native.bind(*[ctypes.cast(getattr(L, name), vp).value for name in _NATIVE])
@@ -586,3 +606,191 @@ def hm_level_dest_map(expert_to_rank: torch.Tensor, G: int, my_rank: int, parent
                                  _dev(num_dest, torch.int32, "num_dest"), _stream(stream))
     _check("hm_level_dest_map", rc)
     return dest_map, num_dest
+
+
+# ---- the router in front of the dispatch, the experts behind it -----------------------------------------------------
+class Router:
+    """How a layer's router chooses (hm_router): `score` is "softmax" or "sigmoid"."""
+    def __init__(self, E: int, K: int, score: str = "softmax", groups: int = 1, top_groups: int = 1, group_best: int = 1,
+                 renormalise: bool = True, scale: float = 1.0):
+        if score not in ("softmax", "sigmoid"):
+            raise ValueError("score must be softmax or sigmoid, got %r" % (score,))
+        self.E, self.K = int(E), int(K)
+        self.c = hm_router(E, K, HM_SCORE_SIGMOID if score == "sigmoid" else HM_SCORE_SOFTMAX, groups, top_groups, group_best,
+                           int(bool(renormalise)), scale)
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def _floats(t: torch.Tensor, name: str) -> int:
+    if t.dtype == torch.bfloat16:
+        return HM_BF16
+    if t.dtype == torch.float32:
+        return HM_F32
+    raise TypeError("%s must be torch.bfloat16 or torch.float32, got %s" % (name, t.dtype))
+
+
+def _rows_of(t: torch.Tensor, name: str):
+    """(address, elements from row to row) of a matrix whose rows are dense but may lie apart."""
+    if not t.is_cuda:
+        raise TypeError("%s must be a GPU tensor (no CPU path exists)" % name)
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions, got %d" % (name, t.dim()))
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise TypeError("the rows of %s must be dense" % name)
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+
+
+def _shaped(t: torch.Tensor, shape, name: str) -> torch.Tensor:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t
+
+
+def _codes(t: torch.Tensor, shape, name: str) -> int:
+    """Address of a buffer of e4m3 values, which may also be given as bytes."""
+    return _dev(_shaped(t, shape, name), torch.uint8 if t.dtype == torch.uint8 else torch.float8_e4m3fn, name)
+
+
+def _scales(t: torch.Tensor, shape, name: str) -> int:
+    """Address of a buffer of scale codes, bytes or what they are: powers of two."""
+    return _dev(_shaped(t, shape, name), torch.float8_e8m0fnu if t.dtype == torch.float8_e8m0fnu else torch.uint8, name)
+
+
+def row8_bytes(C: int) -> int:
+    """Bytes of a row of C values in 8 bits."""
+    return (C + 127) // 128 * 128
+
+
+def scale8_bytes(C: int) -> int:
+    """Bytes of its scales."""
+    return (C + 511) // 512 * 4
+
+
+def alloc_rows8(rows: int, C: int, device="cuda"):
+    """(values, scales) for hm_quantize_rows."""
+    return (torch.empty((rows, row8_bytes(C)), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((rows, scale8_bytes(C)), dtype=torch.uint8, device=device))
+
+
+def alloc_columns8(rows: int, segments: int, C: int, device="cuda"):
+    """(values, scales) for hm_quantize_columns."""
+    blocks = rows // 128 + segments
+    return (torch.empty((C, 128 * blocks), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((blocks, C), dtype=torch.uint8, device=device))
+
+
+def alloc_weights8(experts: int, N: int, C: int, device="cuda"):
+    """(values, scales) for hm_quantize_weights; alloc_weights8(experts, C, N) are the transposed ones."""
+    return (torch.empty((experts, N, row8_bytes(C)), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((experts, (N + 127) // 128, scale8_bytes(C)), dtype=torch.uint8, device=device))
+
+
+def hm_route(logits: torch.Tensor, router: Router, topk_ids: torch.Tensor, topk_weights: torch.Tensor,
+             bias: Optional[torch.Tensor] = None, stream=None):
+    """Expert ids and weights of every token, as hm_plan takes them."""
+    at, ld = _rows_of(logits, "logits")
+    T, E = logits.shape
+    if E != router.E:
+        raise ValueError("logits have %d columns, the router %d experts" % (E, router.E))
+    if bias is not None:
+        _shaped(bias, (E,), "bias")
+    rc = lib().hm_route(at, _floats(logits, "logits"), ld, _dev(bias, torch.float32, "bias"), T, router.ref(),
+                        _dev(_shaped(topk_ids, (T, router.K), "topk_ids"), torch.int32, "topk_ids"),
+                        _dev(_shaped(topk_weights, (T, router.K), "topk_weights"), torch.float32, "topk_weights"), _stream(stream))
+    _check("hm_route", rc)
+    return topk_ids, topk_weights
+
+
+def hm_route_backward(logits: torch.Tensor, router: Router, topk_ids: torch.Tensor, grad_weights: torch.Tensor,
+                      grad_logits: torch.Tensor, stream=None) -> torch.Tensor:
+    at, ld = _rows_of(logits, "logits")
+    T, E = logits.shape
+    if E != router.E:
+        raise ValueError("logits have %d columns, the router %d experts" % (E, router.E))
+    to, grad_ld = _rows_of(_shaped(grad_logits, (T, E), "grad_logits"), "grad_logits")
+    if grad_logits.dtype != logits.dtype:
+        raise TypeError("grad_logits must be %s, got %s" % (logits.dtype, grad_logits.dtype))
+    rc = lib().hm_route_backward(at, _floats(logits, "logits"), ld,
+                                 _dev(_shaped(topk_ids, (T, router.K), "topk_ids"), torch.int32, "topk_ids"),
+                                 _dev(_shaped(grad_weights, (T, router.K), "grad_weights"), torch.float32, "grad_weights"),
+                                 T, router.ref(), to, grad_ld, _stream(stream))
+    _check("hm_route_backward", rc)
+    return grad_logits
+
+
+def hm_combine_weight_grad(gout: torch.Tensor, y: torch.Tensor, plan: Plan, grad_weights: torch.Tensor, stream=None) -> torch.Tensor:
+    T, H = gout.shape
+    _rows_call_shape(plan, T, grad_weights, "gout")
+    if y.shape[1] != H:
+        raise ValueError("y has %d columns, gout %d" % (y.shape[1], H))
+    rc = lib().hm_combine_weight_grad(_dev(gout, gout.dtype, "gout"), _dev(y, gout.dtype, "y"), _floats(gout, "gout"), y.shape[0],
+                                      T, plan.K, H, plan.ref(), _dev(grad_weights, torch.float32, "grad_weights"), _stream(stream))
+    _check("hm_combine_weight_grad", rc)
+    return grad_weights
+
+
+def hm_quantize_rows(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, stream=None):
+    at, ld = _rows_of(x, "x")
+    rows, C = x.shape
+    rc = lib().hm_quantize_rows(at, _floats(x, "x"), ld, rows, C, _codes(q, (rows, row8_bytes(C)), "q"),
+                                _scales(scale, (rows, scale8_bytes(C)), "scale"), _stream(stream))
+    _check("hm_quantize_rows", rc)
+    return q, scale
+
+
+def hm_quantize_columns(x: torch.Tensor, offsets: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, stream=None):
+    """offsets [segments + 1]: a plan's dest_offset."""
+    at, ld = _rows_of(x, "x")
+    rows, C = x.shape
+    segments = offsets.numel() - 1
+    blocks = rows // 128 + segments
+    rc = lib().hm_quantize_columns(at, _floats(x, "x"), ld, _dev(offsets, torch.int32, "offsets"), segments, rows, C,
+                                   _codes(q, (C, 128 * blocks), "q"), _scales(scale, (blocks, C), "scale"), _stream(stream))
+    _check("hm_quantize_columns", rc)
+    return q, scale
+
+
+def hm_quantize_weights(w: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, qt: Optional[torch.Tensor] = None,
+                        scale_t: Optional[torch.Tensor] = None, stream=None):
+    """With qt and scale_t the transposed weights too."""
+    E, N, C = w.shape
+    if qt is not None:
+        _shaped(qt, (E, C, row8_bytes(N)), "qt")
+    if scale_t is not None:
+        _shaped(scale_t, (E, (C + 127) // 128, scale8_bytes(N)), "scale_t")
+    rc = lib().hm_quantize_weights(_dev(w, w.dtype, "w"), _floats(w, "w"), E, N, C, _codes(q, (E, N, row8_bytes(C)), "q"),
+                                   _scales(scale, (E, (N + 127) // 128, scale8_bytes(C)), "scale"),
+                                   None if qt is None else _codes(qt, qt.shape, "qt"),
+                                   None if scale_t is None else _scales(scale_t, scale_t.shape, "scale_t"), _stream(stream))
+    _check("hm_quantize_weights", rc)
+    return (q, scale) if qt is None else (q, scale, qt, scale_t)
+
+
+def hm_expert_matmul(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, offsets: torch.Tensor,
+                     out: torch.Tensor, stream=None) -> torch.Tensor:
+    """out [rows, N]: every row times the weights of its expert.  x and w hold as many blocks of 128 columns, the columns
+    themselves are told from them: zeros fill the last block, so its end does not matter."""
+    E, N, width = w.shape
+    rows = x.shape[0]
+    rc = lib().hm_expert_matmul(_codes(x, (rows, width), "x"), _scales(x_scale, (rows, scale8_bytes(width)), "x_scale"),
+                                _codes(w, (E, N, width), "w"), _scales(w_scale, (E, (N + 127) // 128, scale8_bytes(width)), "w_scale"),
+                                _dev(_shaped(offsets, (E + 1,), "offsets"), torch.int32, "offsets"), E, rows, N, width,
+                                _dev(_shaped(out, (rows, N), "out"), out.dtype, "out"), _floats(out, "out"), _stream(stream))
+    _check("hm_expert_matmul", rc)
+    return out
+
+
+def hm_expert_matmul_dw(gy: torch.Tensor, gy_scale: torch.Tensor, x: torch.Tensor, x_scale: torch.Tensor, offsets: torch.Tensor,
+                        rows: int, dw: torch.Tensor, stream=None) -> torch.Tensor:
+    """dw [experts, N, H] from the columns of gy [N, ...] and x [H, ...] over `rows` rows ordered by expert."""
+    E, N, H = dw.shape
+    blocks = rows // 128 + E
+    rc = lib().hm_expert_matmul_dw(_codes(gy, (N, 128 * blocks), "gy"), _scales(gy_scale, (blocks, N), "gy_scale"),
+                                   _codes(x, (H, 128 * blocks), "x"), _scales(x_scale, (blocks, H), "x_scale"),
+                                   _dev(_shaped(offsets, (E + 1,), "offsets"), torch.int32, "offsets"), E, rows, N, H,
+                                   _dev(dw, dw.dtype, "dw"), _floats(dw, "dw"), _stream(stream))
+    _check("hm_expert_matmul_dw", rc)
+    return dw

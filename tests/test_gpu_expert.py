@@ -1,0 +1,347 @@
+"""hm_quantize_* and hm_expert_matmul / _dw against 64-bit references."""
+import numpy as np
+import pytest
+import torch
+
+import layer_reference as R
+from gpu_harness import dev
+from paper_2508_09591_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F8 = torch.float8_e4m3fn
+DTYPES = [torch.bfloat16, torch.float32]
+
+
+def values(rng, *shape):
+    """Values of many sizes: rows, blocks and single elements apart by powers of two, zeros among them."""
+    x = rng.standard_normal(shape).astype(np.float32)
+    x *= np.ldexp(1.0, rng.integers(-12, 12, shape[:-1] + (1,))).astype(np.float32)
+    x *= np.ldexp(1.0, rng.integers(-6, 7, shape)).astype(np.float32)
+    x[rng.random(shape) < 0.05] = 0.0
+    return x
+
+
+def strided(x, dtype, extra):
+    """The matrix with rows `extra` elements further apart, off a vector's alignment where that is odd."""
+    t = torch.full((x.shape[0] * (x.shape[1] + extra) + extra,), float("nan"), dtype=dtype, device="cuda")
+    m = t[extra:].view(x.shape[0], x.shape[1] + extra)[:, :x.shape[1]]
+    m.copy_(dev(x))
+    return m
+
+
+def poisoned(pair):
+    for t in pair:
+        t.view(torch.uint8).fill_(0xAB)
+    return pair
+
+
+def numbers(q):
+    return q.float().cpu().numpy().astype(np.float64)
+
+
+def codes(s):
+    return s.cpu().numpy().astype(np.int64)
+
+
+def offsets_of(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+
+
+# ---- 8 bits: every byte ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,C", [(1, 1), (1, 7168), (3, 127), (7, 128), (5, 129), (65, 511), (9, 512), (33, 513), (4, 1030), (130, 2056), (2, 4100)])
+def test_rows(rows, C, dtype):
+    rng = np.random.default_rng(rows + C)
+    x = torch.from_numpy(values(rng, rows, C)).to(dtype).float().numpy()
+    want, want_codes = R.rows8(x)
+    for extra in (0, 8, 3):
+        q, s = poisoned(B.alloc_rows8(rows, C))
+        B.hm_quantize_rows(strided(x, dtype, extra), q, s)
+        assert np.array_equal(numbers(q), want) and np.array_equal(codes(s), want_codes)
+        assert not q.view(torch.uint8)[:, C:].any()
+
+
+def edge_values():
+    """A block for each: zeros, the least and the largest numbers, the border between two exponents, NaN and infinities."""
+    x = np.zeros((12, 128), dtype=np.float32)
+    x[1, 3] = 1e-45
+    x[2] = 1.1754944e-38
+    x[3, :2] = np.finfo(np.float32).max, -1.0
+    x[4, :3] = 448.0, 1.0, -0.5
+    x[5, :3] = np.nextafter(np.float32(448.0), np.float32(1e9)), 1.0, -0.5
+    x[6] = np.linspace(-448, 448, 128)
+    x[7, :4] = np.nan, 2.0, -3.0, 5.0
+    x[8, :4] = np.inf, -np.inf, 1.0, 100.0
+    x[9] = np.nan
+    x[10, :6] = 1.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, 2.0 ** -12, -2.0 ** -11
+    x[11, :9] = 448.0, 17.0, 19.0, 21.0, 23.0, 1.0625, 1.1875, 9.5, 8.5   # ties
+    return x
+
+
+def test_edges_of_the_number_range():
+    x = edge_values()
+    want, want_codes = R.rows8(x)
+    q, s = poisoned(B.alloc_rows8(*x.shape))
+    B.hm_quantize_rows(dev(x), q, s)
+    assert np.array_equal(numbers(q), want, equal_nan=True) and np.array_equal(codes(s), want_codes)
+    off = np.array([0, 128], dtype=np.int32)
+    want, want_codes, there = R.columns8(x.T.copy(), off)
+    q, s = poisoned(B.alloc_columns8(128, 1, 12))
+    B.hm_quantize_columns(dev(x.T.copy()), dev(off), q, s)
+    assert there.tolist() == [True, False]
+    assert np.array_equal(numbers(q)[:, :128], want[:, :128], equal_nan=True) and np.array_equal(codes(s)[:1], want_codes[:1])
+    w = np.zeros((12, 64, 70), dtype=np.float32)
+    w[:, :8, 3:19] = x.reshape(12, 8, 16)
+    want = R.weights8(w)
+    got = poisoned(B.alloc_weights8(12, 64, 70)) + poisoned(B.alloc_weights8(12, 70, 64))
+    B.hm_quantize_weights(dev(w), *got)
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert np.array_equal(numbers(a) if i % 2 == 0 else codes(a), b, equal_nan=True), i
+
+
+COUNTS = [[1], [128], [129], [0, 5, 0], [300, 0, 1, 127, 128, 2], [0, 0, 0], [64] * 70, [1] * 130, [1000, 24], [0, 0, 256, 0]]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("C", [1, 64, 70, 200, 1030])
+@pytest.mark.parametrize("counts", COUNTS)
+def test_columns(counts, C, dtype):
+    rng = np.random.default_rng(C + len(counts))
+    off = offsets_of(counts)
+    rows, spare = int(off[-1]), 3   # rows behind the last segment belong to none
+    x = torch.from_numpy(values(rng, rows + spare, C)).to(dtype).float().numpy()
+    want, want_codes, there = R.columns8(x, off)
+    for extra in (0, 5):
+        q, s = poisoned(B.alloc_columns8(rows + spare, len(counts), C))
+        B.hm_quantize_columns(strided(x, dtype, extra), dev(off), q, s)
+        got, got_codes = numbers(q).reshape(C, -1, 128), codes(s)
+        assert np.array_equal(got[:, there], want.reshape(C, -1, 128)[:, there]) and np.array_equal(got_codes[there], want_codes[there])
+        assert (q.view(torch.uint8).view(C, -1, 128)[:, dev(~there)] == 0xAB).all() and np.all(got_codes[~there] == 0xAB)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("E,N,C", [(1, 1, 1), (2, 128, 128), (3, 130, 7), (1, 7, 600), (5, 256, 512), (2, 1000, 300), (1, 640, 129)])
+def test_weights(E, N, C, dtype):
+    w = torch.from_numpy(values(np.random.default_rng(N + C), E, N, C)).to(dtype)
+    want = R.weights8(w.float().numpy())
+    got = poisoned(B.alloc_weights8(E, N, C)) + poisoned(B.alloc_weights8(E, C, N))
+    B.hm_quantize_weights(w.cuda(), *got)
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert np.array_equal(numbers(a) if i % 2 == 0 else codes(a), b), i
+    alone = poisoned(B.alloc_weights8(E, N, C))
+    B.hm_quantize_weights(w.cuda(), *alone)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(alone, got[:2]))
+
+
+# ---- products -------------------------------------------------------------------------------------------------------
+def operand(rng, *shape):
+    """Random bytes that are numbers, with zeros, and random codes around 127."""
+    q = rng.integers(0, 256, shape, dtype=np.uint8)
+    q[(q & 0x7F) == 0x7F] = 0
+    return q
+
+
+def f8(bits):
+    return torch.from_numpy(bits).view(F8)
+
+
+def bound(want, size, largest, count, dtype):
+    """bf16: the result is rounded (2^-9), and of a step's 64 products each may lose 2^-13 of the largest; twice 64 a block.
+    fp32: each of the additions rounds by 2^-24 of what it adds to, here of the sum of magnitudes."""
+    if dtype == torch.bfloat16:
+        return 2.0 ** -8 * np.abs(want) + 128 * 2.0 ** -13 * largest + 1e-37
+    return (count + 8) * 2.0 ** -24 * size + 1e-37
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,H", [(1, 1), (16, 128), (33, 129), (130, 512), (64, 1030), (257, 300), (1000, 640), (4, 2056)])
+@pytest.mark.parametrize("counts", [[1], [0, 5, 0, 1], [130, 0, 1, 127, 128, 2], [3] * 70, [0, 0], [513], [16, 17, 31, 32, 33, 64, 65]])
+def test_products_of_rows(counts, N, H, dtype):
+    rng = np.random.default_rng(N * H + len(counts))
+    off, E, spare = offsets_of(counts), len(counts), 2
+    rows = int(off[-1]) + spare
+    W = R.up(H, 128)
+    x, w = operand(rng, rows, W), operand(rng, E, N, W)
+    x[:, H:], w[:, :, H:] = 0, 0
+    xs = rng.integers(120, 135, (rows, R.up(H, 512) // 128), dtype=np.uint8)
+    ws = rng.integers(115, 130, (E, R.up(N, 128) // 128, R.up(H, 512) // 128), dtype=np.uint8)
+    out = torch.full((rows, N), -77.0, dtype=dtype, device="cuda")
+    B.hm_expert_matmul(f8(x).cuda(), dev(xs), f8(w).cuda(), dev(ws), dev(off), out)
+    a = R.row_values(f8(x).float().numpy().astype(np.float64), xs.astype(np.int64))
+    b = R.weight_values(f8(w).float().numpy().astype(np.float64), ws.astype(np.int64))
+    got = out.float().cpu().numpy().astype(np.float64)
+    assert np.all(got[off[-1]:] == -77.0)
+    for e in range(E):
+        r = slice(off[e], off[e + 1])
+        if counts[e] == 0:
+            continue
+        want, size, largest = R.product(a[r], b[e], W // 128)
+        assert np.all(np.abs(got[r] - want) <= bound(want, size, largest, W, dtype)), (e, np.abs(got[r] - want).max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,H", [(1, 1), (16, 128), (33, 129), (130, 70), (257, 300)])
+@pytest.mark.parametrize("counts", [[1], [0, 5, 0, 1], [130, 0, 1, 127, 128, 2], [3] * 70, [0, 0], [700]])
+def test_products_of_columns(counts, N, H, dtype):
+    rng = np.random.default_rng(N * H + len(counts))
+    off, E = offsets_of(counts), len(counts)
+    rows = int(off[-1])
+    blocks = rows // 128 + E
+    gy, x = operand(rng, N, 128 * blocks), operand(rng, H, 128 * blocks)
+    there = np.zeros(128 * blocks, dtype=bool)
+    for e in range(E):
+        first = 128 * (off[e] // 128 + e)
+        there[first:first + counts[e]] = True
+        for q in (gy, x):   # zeros behind a segment up to a whole block; what is in no segment's block may be anything
+            q[:, first + counts[e]:first + R.up(counts[e], 128)] = 0
+    gs, xs = rng.integers(120, 135, (blocks, N), dtype=np.uint8), rng.integers(115, 130, (blocks, H), dtype=np.uint8)
+    dw = torch.full((E, N, H), -77.0, dtype=dtype, device="cuda")
+    B.hm_expert_matmul_dw(f8(gy).cuda(), dev(gs), f8(x).cuda(), dev(xs), dev(off), rows, dw)
+    a = R.column_values(f8(gy).float().numpy().astype(np.float64), gs.astype(np.int64))
+    b = R.column_values(f8(x).float().numpy().astype(np.float64), xs.astype(np.int64))
+    got = dw.float().cpu().numpy().astype(np.float64)
+    for e in range(E):
+        first, n = 128 * (off[e] // 128 + e), R.up(counts[e], 128)
+        want, size, largest = R.product(a[first:first + n].T, b[first:first + n].T, n // 128)
+        assert np.all(np.abs(got[e] - want) <= bound(want, size, largest, n, dtype)), (e, np.abs(got[e] - want).max())
+
+
+def test_a_nan_stays_in_its_row_and_column():
+    """NaN codes, in values and in scales, reach the results they are part of and no others."""
+    rows, N, H, E = 40, 48, 256, 2
+    rng = np.random.default_rng(1)
+    x, w = operand(rng, rows, H), operand(rng, E, N, H)
+    xs, ws = np.full((rows, 4), 127, dtype=np.uint8), np.full((E, 1, 4), 127, dtype=np.uint8)
+    x[3, 200], w[1, 5, 0], xs[7, 1] = 0x7F, 0xFF, 255
+    off = np.array([0, 20, 40], dtype=np.int32)
+    for dtype in DTYPES:
+        out = torch.zeros((rows, N), dtype=dtype, device="cuda")
+        B.hm_expert_matmul(f8(x).cuda(), dev(xs), f8(w).cuda(), dev(ws), dev(off), out)
+        bad = torch.isnan(out).cpu().numpy()
+        want = np.zeros((rows, N), dtype=bool)
+        want[3], want[20:, 5], want[7] = True, True, True
+        assert np.array_equal(bad, want)
+
+
+def test_offsets_that_are_wrong_stay_inside():
+    """Descending offsets and offsets outside the rows: nothing outside the outputs is written."""
+    rows, N, H = 50, 40, 128
+    rng = np.random.default_rng(2)
+    for off in ([-5, 20, 70], [40, 10, 50], [2 ** 31 - 1, -2 ** 31, 30], [0, 50, 0]):
+        off = np.array(off, dtype=np.int32)
+        x, xs = B.alloc_rows8(rows, H)
+        w, ws = B.alloc_weights8(2, N, H)
+        for t in (x, xs, w, ws):
+            t.view(torch.uint8).fill_(56)
+        guard = torch.full((rows + 2, N), 5.0, device="cuda")
+        B.hm_expert_matmul(x, xs, w, ws, dev(off), guard[1:rows + 1])
+        assert (guard[0] == 5).all() and (guard[-1] == 5).all()
+        blocks = rows // 128 + 2
+        room = torch.full((N * 128 * blocks + 512,), 7, dtype=torch.uint8, device="cuda")
+        scale = torch.full((blocks * N + 64,), 7, dtype=torch.uint8, device="cuda")
+        B.hm_quantize_columns(torch.ones((rows, N), device="cuda"), dev(off), room[256:-256].view(N, 128 * blocks), scale[32:-32].view(blocks, N))
+        assert (room[:256] == 7).all() and (room[-256:] == 7).all() and (scale[:32] == 7).all() and (scale[-32:] == 7).all()
+        xt, xts = B.alloc_columns8(rows, 2, N)
+        for t in (xt, xts):
+            t.view(torch.uint8).fill_(56)
+        guard = torch.full((4, N, N), 5.0, device="cuda")
+        B.hm_expert_matmul_dw(xt, xts, xt, xts, dev(off), rows, guard[1:3])
+        assert (guard[0] == 5).all() and (guard[-1] == 5).all()
+
+
+def test_nothing_to_do():
+    off = torch.zeros(3, dtype=torch.int32, device="cuda")
+    out = torch.empty((0, 40), device="cuda")
+    B.hm_expert_matmul(*B.alloc_rows8(0, 128), *B.alloc_weights8(2, 40, 128), off, out)
+    dw = torch.full((2, 40, 24), 3.0, device="cuda")
+    B.hm_expert_matmul_dw(*B.alloc_columns8(0, 2, 40), *B.alloc_columns8(0, 2, 24), off, 0, dw)
+    assert not dw.any()
+    x = torch.empty((0, 40), device="cuda")
+    B.hm_quantize_rows(x, *B.alloc_rows8(0, 40))
+    B.hm_quantize_columns(x, off, *B.alloc_columns8(0, 2, 40))
+
+
+@pytest.mark.parametrize("rows,E,N,H", [(4096, 4, 512, 1024), (300, 8, 384, 2048), (40, 16, 1024, 512), (3000, 3, 250, 640)])
+def test_a_layer_of_products_and_their_gradients(rows, E, N, H):
+    """y = x w, dx = gy w and dw = gy^T x of the values that the quantised operands stand for; on a stream of the caller's."""
+    rng = np.random.default_rng(rows)
+    off = np.sort(rng.integers(0, rows + 1, E - 1))
+    off = np.concatenate([[0], off, [rows]]).astype(np.int32)
+    x, w, gy = (torch.from_numpy(rng.standard_normal(s, dtype=np.float32)).cuda() for s in ((rows, H), (E, N, H), (rows, N)))
+    d_off, stream = dev(off), torch.cuda.Stream()
+    q = {k: poisoned(v) for k, v in {"x": B.alloc_rows8(rows, H), "gy": B.alloc_rows8(rows, N), "xt": B.alloc_columns8(rows, E, H),
+                                     "gyt": B.alloc_columns8(rows, E, N), "w": B.alloc_weights8(E, N, H), "wt": B.alloc_weights8(E, H, N)}.items()}
+    y, dx, dw = torch.empty((rows, N), dtype=torch.bfloat16, device="cuda"), torch.empty((rows, H), device="cuda"), torch.empty((E, N, H), device="cuda")
+    torch.cuda.synchronize()
+    B.hm_quantize_rows(x, *q["x"], stream=stream)
+    B.hm_quantize_rows(gy, *q["gy"], stream=stream)
+    B.hm_quantize_columns(x, d_off, *q["xt"], stream=stream)
+    B.hm_quantize_columns(gy, d_off, *q["gyt"], stream=stream)
+    B.hm_quantize_weights(w, *q["w"], *q["wt"], stream=stream)
+    B.hm_expert_matmul(*q["x"], *q["w"], d_off, y, stream=stream)
+    B.hm_expert_matmul(*q["gy"], *q["wt"], d_off, dx, stream=stream)
+    B.hm_expert_matmul_dw(*q["gyt"], *q["xt"], d_off, rows, dw, stream=stream)
+    stream.synchronize()
+    vx, vg = R.row_values(numbers(q["x"][0]), codes(q["x"][1]))[:, :H], R.row_values(numbers(q["gy"][0]), codes(q["gy"][1]))[:, :N]
+    vw = R.weight_values(numbers(q["w"][0]), codes(q["w"][1]))[:, :, :H]
+    near = lambda a, b, tol: np.linalg.norm(a - b) <= tol * np.linalg.norm(b)
+    cols = [R.column_values(numbers(q[k][0]), codes(q[k][1])) for k in ("gyt", "xt")]
+    for e in range(E):
+        r = slice(off[e], off[e + 1])
+        if off[e] == off[e + 1]:
+            assert not dw[e].any()
+            continue
+        # rounding to bf16 is at most 2^-9 of each result; sums in 32 bits: sqrt(terms) 2^-24, with room
+        assert near(y[r].double().cpu().numpy(), vx[r] @ vw[e].T, 2.0 ** -9 + 5e-5)
+        assert near(dx[r].double().cpu().numpy(), vg[r] @ vw[e], 1e-5)
+        first = 128 * (off[e] // 128 + e)
+        a, b = (c[first:first + off[e + 1] - off[e]] for c in cols)
+        assert near(dw[e].double().cpu().numpy(), a.T @ b, 1e-5)
+        # the 8 bits themselves: e4m3 is good to 2^-4 of a value, and a sum of such errors averages out
+        assert near(dw[e].double().cpu().numpy(), gy[r].double().cpu().numpy().T @ x[r].double().cpu().numpy(), 0.1)
+
+
+def test_results_do_not_depend_on_what_ran_before():
+    """The same call into poisoned outputs: the same bits."""
+    rng = np.random.default_rng(8)
+    off = dev(offsets_of([500, 0, 12, 300]))
+    x, xs = f8(operand(rng, 812, 1024)).cuda(), dev(rng.integers(120, 130, (812, 8), dtype=np.uint8))
+    w, ws = f8(operand(rng, 4, 384, 1024)).cuda(), dev(rng.integers(120, 130, (4, 3, 8), dtype=np.uint8))
+    for dtype in DTYPES:
+        outs = [torch.full((812, 384), fill, dtype=dtype, device="cuda") for fill in (1.0, float("nan"))]
+        for o in outs:
+            B.hm_expert_matmul(x, xs, w, ws, off, o)
+        assert torch.equal(*[o.view(torch.uint8) for o in outs])
+
+
+def test_replayed_in_a_graph():
+    rng = np.random.default_rng(6)
+    rows, E, N, H = 700, 4, 256, 512
+    off = dev(offsets_of([300, 0, 150, 250]))
+    x = torch.empty((rows, H), device="cuda")
+    w = B.hm_quantize_weights(torch.randn((E, N, H), device="cuda"), *B.alloc_weights8(E, N, H))
+    q, qt, y = B.alloc_rows8(rows, H), B.alloc_columns8(rows, E, H), torch.empty((rows, N), dtype=torch.bfloat16, device="cuda")
+    dw = torch.empty((E, H, H), device="cuda")
+
+    def calls():
+        B.hm_quantize_rows(x, *q)
+        B.hm_quantize_columns(x, off, *qt)
+        B.hm_expert_matmul(*q, *w, off, y)
+        B.hm_expert_matmul_dw(*qt, *qt, off, rows, dw)
+
+    x.normal_()
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(3):
+        x.normal_()
+        calls()
+        want = [y.clone(), dw.clone()]
+        y.fill_(7)
+        dw.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(dw, want[1])
