@@ -79,29 +79,61 @@ __device__ __forceinline__ void store4(OUT *at, int n, const f32x4 &v) {
   }
 }
 
-// Eight values of a block as bf16, times the block's power of two.
-__device__ __forceinline__ bf16x8 widen(int lo, int hi, float power) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true);
-  return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+// What a lane holds of a fragment's row for one part of a step, and its products.
+template <bool FULL>
+struct Slice;
+template <>
+struct Slice<false> {   // 32 values: one instruction, half a step
+  i32x8 v;
+  __device__ __forceinline__ void read(const uint8_t *lds, const uint32_t (&at)[4], int fragment, int part) {
+    const i32x4 lo = *(const i32x4 *)(lds + at[2 * part] + fragment), hi = *(const i32x4 *)(lds + at[2 * part + 1] + fragment);
+    v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  }
+  __device__ __forceinline__ void times(const Slice &q, uint32_t code_p, uint32_t code_q, f32x16 &acc) const {
+    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v, q.v, acc, 0, 0, 0, (int)code_p, 0, (int)code_q);   // 0, 0: e4m3
+  }
+};
+template <>
+struct Slice<true> {   // 16 values: two instructions, a quarter of a step
+  i32x4 v;
+  __device__ __forceinline__ void read(const uint8_t *lds, const uint32_t (&at)[4], int fragment, int part) { v = *(const i32x4 *)(lds + at[part] + fragment); }
+  // Eight values as bf16, times their block's power of two.
+  static __device__ __forceinline__ bf16x8 widen(int lo, int hi, uint32_t code) {
+    const float power = __builtin_bit_cast(float, (code & 0xFFu) << 23);
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true);
+    return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+  __device__ __forceinline__ void times(const Slice &q, uint32_t code_p, uint32_t code_q, f32x16 &acc) const {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(v[0], v[1], code_p), widen(q.v[0], q.v[1], code_q), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(v[2], v[3], code_p), widen(q.v[2], q.v[3], code_q), acc, 0, 0, 0);
+  }
+};
+
+// A buffer from `at` on, as far as an offset of 32 bits goes: kernels keep their rows inside by themselves.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_resource(const uint8_t *at) {
+  return __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, (int)0xFFFFFFFFu, 0x00027000);
 }
 
 // FQ x FP fragments of 32 x 32 in a wave, WQ x WP waves.  LDS holds two steps of 128 bytes of the tile's rows, filled
-// straight from memory while the other is multiplied; a row's eight 16-byte pieces are stored at places exchanged by the row
-// number, so that the rows of a fragment spread over all banks.  Lane l has
+// straight from memory while the other is multiplied; a row's eight 16-byte pieces are stored at places exchanged by half
+// the row number, so that sixteen rows of a fragment, which are read together, spread over all 64 banks.  Lane l has
 // row l % 32 of a fragment and its pieces 4 (l / 32) to 4 (l / 32) + 3; which values meet in an instruction does not matter as
 // long as both operands' lanes hold the same ones.
 template <int FQ, int FP, int WQ, int WP, bool DW, typename OUT>
 __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams p) {
   constexpr int kWaves = WQ * WP, TQ = FQ * WQ * 32, TP = FP * WP * 32;
   constexpr bool kFull = sizeof(OUT) == 4;
+  constexpr int kSlices = kFull ? 4 : 2;
+  static_assert(kWaves % 2 == 0, "the pieces' places go by it");
   constexpr int kLoadsQ = TQ / 8 / kWaves, kLoadsP = TP / 8 / kWaves;
   __shared__ __attribute__((aligned(128))) uint8_t stage[2][(TQ + TP) * 128];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wq = wave / WP, wp = wave % WP;
   Tile t;
   int steps, q_rows, p_rows;
   const uint8_t *q, *ps;
-  int64_t q_pitch, p_pitch;
+  int64_t pitch;
+  const int64_t scale_pitch = scale8_bytes(p.H);
   int block0 = 0;
   if constexpr (DW) {
     const int e = (int)blockIdx.z;
@@ -109,7 +141,7 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
     steps = (s.to - s.from + 127) / 128;
     block0 = first_block8(s.from, e);
     t = {e, (int)blockIdx.y * TQ, p.N, (int)blockIdx.x * TP};
-    q_pitch = p_pitch = column8_blocks(p.rows, p.experts) * 128;
+    pitch = column8_blocks(p.rows, p.experts) * 128;
     q = p.q + (int64_t)block0 * 128;
     ps = p.p + (int64_t)block0 * 128;
     q_rows = p.N;
@@ -118,42 +150,48 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
     t = tile_of_rows<TQ, TP>(p);
     if (t.q0 >= t.q_end) return;
     steps = (int)blocks8(p.H);
-    q_pitch = p_pitch = row8_bytes(p.H);
+    pitch = row8_bytes(p.H);
     q = p.q;
-    ps = p.p + (int64_t)t.expert * p.N * p_pitch;
+    ps = p.p + (int64_t)t.expert * p.N * pitch;
     q_rows = t.q_end;
     p_rows = p.N;
   }
   // places of this lane's pieces; rows behind the last are read from the last, their products are not stored
-  const uint8_t *from_q[kLoadsQ], *from_p[kLoadsP];
-  const int row8 = lane >> 3, piece = ((lane & 7) ^ row8) * 16;
+  uint32_t from_q[kLoadsQ], from_p[kLoadsP];
+  const int row8 = lane >> 3, piece = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16;   // of row 8 (wave + i kWaves) + row8: half the row, modulo 8
 #pragma unroll
-  for (int i = 0; i < kLoadsQ; ++i) from_q[i] = q + (int64_t)min(t.q0 + (wave + i * kWaves) * 8 + row8, q_rows - 1) * q_pitch + piece;
+  for (int i = 0; i < kLoadsQ; ++i) from_q[i] = (uint32_t)min((wave + i * kWaves) * 8 + row8, q_rows - 1 - t.q0) * (uint32_t)pitch + piece;
 #pragma unroll
-  for (int i = 0; i < kLoadsP; ++i) from_p[i] = ps + (int64_t)min(t.p0 + (wave + i * kWaves) * 8 + row8, p_rows - 1) * p_pitch + piece;
+  for (int i = 0; i < kLoadsP; ++i) from_p[i] = (uint32_t)min((wave + i * kWaves) * 8 + row8, p_rows - 1 - t.p0) * (uint32_t)pitch + piece;
+  // uniform bases and 32-bit offsets: addresses of 64 bits per piece would not fit beside the sums
+  const auto base_q = tile_resource(q + (int64_t)t.q0 * pitch), base_p = tile_resource(ps + (int64_t)t.p0 * pitch);
   auto load = [&](int s, int k) {
 #pragma unroll
     for (int i = 0; i < kLoadsQ; ++i)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from_q[i] + (int64_t)k * 128),
-                                       (__attribute__((address_space(3))) void *)(stage[s] + (wave + i * kWaves) * 1024), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(base_q, (__attribute__((address_space(3))) void *)(stage[s] + (wave + i * kWaves) * 1024), 16,
+                                               (int)from_q[i], k * 128, 0, 0);
 #pragma unroll
     for (int i = 0; i < kLoadsP; ++i)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from_p[i] + (int64_t)k * 128),
-                                       (__attribute__((address_space(3))) void *)(stage[s] + (TQ / 8 + wave + i * kWaves) * 1024), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(base_p, (__attribute__((address_space(3))) void *)(stage[s] + (TQ / 8 + wave + i * kWaves) * 1024), 16,
+                                               (int)from_p[i], k * 128, 0, 0);
   };
-  // scales of this lane's row of each fragment
-  const int64_t scale_q = DW ? 0 : scale8_bytes(p.H);
-  const uint8_t *sq[FQ], *sp[FP];
+  // scales of this lane's row of each fragment; codes of a step in the lowest byte, rows: those of four steps are loaded together
+  uint32_t from_sq[FQ], from_sp[FP], scale_of_q[FQ], scale_of_p[FP], next_q[FQ], next_p[FP];
 #pragma unroll
-  for (int i = 0; i < FQ; ++i) {
-    const int r = min(t.q0 + (wq * FQ + i) * 32 + (lane & 31), q_rows - 1);
-    sq[i] = p.q_scale + (DW ? (int64_t)block0 * p.N + r : (int64_t)r * scale_q);
-  }
+  for (int i = 0; i < FQ; ++i) from_sq[i] = (uint32_t)min((wq * FQ + i) * 32 + (lane & 31), q_rows - 1 - t.q0) * (uint32_t)(DW ? 1 : scale_pitch);
 #pragma unroll
   for (int i = 0; i < FP; ++i) {
-    const int r = min(t.p0 + (wp * FP + i) * 32 + (lane & 31), p_rows - 1);
-    sp[i] = p.p_scale + (DW ? (int64_t)block0 * p.H + r : ((int64_t)t.expert * blocks8(p.N) + r / 128) * scale_q);
+    const int r = min((wp * FP + i) * 32 + (lane & 31), p_rows - 1 - t.p0);
+    from_sp[i] = DW ? (uint32_t)r : (uint32_t)(r / 128) * (uint32_t)scale_pitch;   // t.p0 is a multiple of 128
   }
+  auto load_scales = [&](int k) {
+    const uint8_t *sq = p.q_scale + (DW ? (int64_t)(block0 + k) * p.N + t.q0 : (int64_t)t.q0 * scale_pitch + k);
+    const uint8_t *sp = p.p_scale + (DW ? (int64_t)(block0 + k) * p.H + t.p0 : ((int64_t)t.expert * blocks8(p.N) + t.p0 / 128) * scale_pitch + k);
+#pragma unroll
+    for (int i = 0; i < FQ; ++i) next_q[i] = DW ? sq[from_sq[i]] : *(const uint32_t *)(sq + from_sq[i]);
+#pragma unroll
+    for (int i = 0; i < FP; ++i) next_p[i] = DW ? sp[from_sp[i]] : *(const uint32_t *)(sp + from_sp[i]);
+  };
   f32x16 acc[FQ][FP];
 #pragma unroll
   for (int i = 0; i < FQ; ++i)
@@ -161,64 +199,69 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
     for (int j = 0; j < FP; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-  if (steps > 0) load(0, 0);
-  const int at = (lane & 31) * 128 + (((lane >> 5) * 4) ^ (lane & 7)) * 16;   // piece 4 (l / 32); the others are exchanged with it
-  for (int k = 0; k < steps; ++k) {
-    int scale_of_q[FQ], scale_of_p[FP];
+  // A step is a row of items: part item / FQ of fragment item % FQ of Q, times all of the wave's fragments of P.  An item's
+  // operands are read two items ahead, so that the matrix unit always has some.
+  constexpr int kItems = kSlices * FQ, kAhead = 2;
+  Slice<kFull> of_q[4], of_p[2][FP];
+  // piece 4 (l / 32) of this lane's row and those exchanged with it, in the stage that is read
+  uint32_t to_q[4], to_p[4];
 #pragma unroll
-    for (int i = 0; i < FQ; ++i) scale_of_q[i] = sq[i][DW ? (int64_t)k * p.N : k];
+  for (int v = 0; v < 4; ++v) {
+    const uint32_t at = (uint32_t)((lane & 31) * 128 + (((lane >> 5) * 4) ^ (lane >> 1 & 7) ^ v) * 16);
+    to_q[v] = at + (uint32_t)(wq * FQ * 4096);
+    to_p[v] = at + (uint32_t)(TQ * 128 + wp * FP * 4096);
+  }
+  auto read = [&](int item) {
+    const int part = item / FQ;
+    if (item % FQ == 0) {
 #pragma unroll
-    for (int i = 0; i < FP; ++i) scale_of_p[i] = sp[i][DW ? (int64_t)k * p.H : k];
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): the wave's own pieces are in LDS
+      for (int j = 0; j < FP; ++j) of_p[part & 1][j].read(&stage[0][0], to_p, j * 4096, part);
+    }
+    of_q[item & 3].read(&stage[0][0], to_q, item % FQ * 4096, part);
+  };
+  auto wait = [] {   // the wave's own pieces are in LDS, then everybody's
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
-    if (k + 1 < steps) load((k + 1) & 1, k + 1);
-    const uint8_t *tile_q = stage[k & 1] + wq * FQ * 4096, *tile_p = stage[k & 1] + TQ * 128 + wp * FP * 4096;
-    if constexpr (kFull) {
-      float power_of_q[FQ], power_of_p[FP];
+  };
+  if (steps > 0) {
+    load_scales(0);
+    load(0, 0);
+    if (steps > 1) load(1, 1);
+    wait();
 #pragma unroll
-      for (int i = 0; i < FQ; ++i) power_of_q[i] = __builtin_bit_cast(float, scale_of_q[i] << 23);
+    for (int item = 0; item < kAhead; ++item) read(item);
+  }
+  for (int k = 0; k < steps; ++k) {
+    const bool fresh = DW || (k & 3) == 0;
 #pragma unroll
-      for (int j = 0; j < FP; ++j) power_of_p[j] = __builtin_bit_cast(float, scale_of_p[j] << 23);
+    for (int i = 0; i < FQ; ++i) scale_of_q[i] = fresh ? next_q[i] : scale_of_q[i] >> 8;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        i32x4 a[FQ], b[FP];
+    for (int i = 0; i < FP; ++i) scale_of_p[i] = fresh ? next_p[i] : scale_of_p[i] >> 8;
+    if (DW || (k & 3) == 3) load_scales(k + 1 < steps ? k + 1 : 0);
 #pragma unroll
-        for (int i = 0; i < FQ; ++i) a[i] = *(const i32x4 *)(tile_q + i * 4096 + (at ^ (s * 16)));
+    for (int item = 0; item < kItems; ++item) {
+      const Slice<kFull> mine = of_q[item & 3];
+      Slice<kFull> other[FP];
 #pragma unroll
-        for (int j = 0; j < FP; ++j) b[j] = *(const i32x4 *)(tile_p + j * 4096 + (at ^ (s * 16)));
+      for (int j = 0; j < FP; ++j) other[j] = of_p[(item / FQ) & 1][j];
+      // what is loaded and read ahead of the last step is not used: a branch around it would part the products from the reads
+      if (item + kAhead == kItems) {
+        wait();   // of step k nothing is left to read
+        load(k & 1, min(k + 2, steps - 1));
+        const uint32_t other_stage = (k & 1) ? 0u - (uint32_t)sizeof(stage[0]) : (uint32_t)sizeof(stage[0]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          bf16x8 wide[FP];
-#pragma unroll
-          for (int j = 0; j < FP; ++j) wide[j] = widen(b[j][2 * h], b[j][2 * h + 1], power_of_p[j]);
-#pragma unroll
-          for (int i = 0; i < FQ; ++i) {
-            const bf16x8 row = widen(a[i][2 * h], a[i][2 * h + 1], power_of_q[i]);
-#pragma unroll
-            for (int j = 0; j < FP; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide[j], row, acc[i][j], 0, 0, 0);
-          }
+        for (int v = 0; v < 4; ++v) {
+          to_q[v] += other_stage;
+          to_p[v] += other_stage;
         }
       }
-    } else {
+      read((item + kAhead) % kItems);
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        auto piece8 = [&](const uint8_t *tile) {
-          const i32x4 lo = *(const i32x4 *)(tile + (at ^ (s * 32))), hi = *(const i32x4 *)(tile + (at ^ (s * 32 + 16)));
-          return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        };
-        i32x8 b[FP];
-#pragma unroll
-        for (int j = 0; j < FP; ++j) b[j] = piece8(tile_p + j * 4096);
-#pragma unroll
-        for (int i = 0; i < FQ; ++i) {
-          const i32x8 a = piece8(tile_q + i * 4096);
-#pragma unroll
-          for (int j = 0; j < FP; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[j], a, acc[i][j], 0, 0, 0, scale_of_p[j], 0, scale_of_q[i]);   // 0, 0: e4m3
-        }
-      }
+      for (int j = 0; j < FP; ++j) other[j].times(mine, scale_of_p[j], scale_of_q[item % FQ], acc[item % FQ][j]);
+      __builtin_amdgcn_sched_barrier(0);   // else the compiler reads all items at once and runs out of registers
     }
   }
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // nothing is on its way to LDS when the workgroup ends
   // a lane has row l % 32 of a fragment and of every eight columns the first or the last four
 #pragma unroll
   for (int i = 0; i < FQ; ++i) {
@@ -254,10 +297,16 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   if (bad != HM_OK) return bad;
   if (rows == 0) return HM_OK;
   const ProductParams p = {x, x_scale, w, w_scale, offsets, experts, (int32_t)rows, N, H, out};
-  const int64_t tiles = (rows / 128 + experts) * ((N + 127) / 128) + 8;
+  const int TS = rows / experts >= 256 ? 256 : 128;
+  const int64_t tiles = (rows / TS + experts) * ((N + TS - 1) / TS) + 8;
   if (tiles > (1 << 23)) return HM_ERR_SHAPE;
+  if (TS == 256) {
+  const auto kernel = out_dtype == HM_BF16 ? product_kernel<4, 2, 2, 4, false, uint16_t> : product_kernel<4, 2, 2, 4, false, float>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(512), 0, (hipStream_t)hip_stream, p);
+  } else {
   const auto kernel = out_dtype == HM_BF16 ? product_kernel<2, 2, 2, 2, false, uint16_t> : product_kernel<2, 2, 2, 2, false, float>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(256), 0, (hipStream_t)hip_stream, p);
+  }
   return hm_launch_status();
 }
 
@@ -269,7 +318,7 @@ extern "C" hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_sc
   const hm_status bad = check_products(gy, gy_scale, x, x_scale, offsets, experts, rows, N, H, dw, dw_dtype, false);
   if (bad != HM_OK) return bad;
   const ProductParams p = {gy, gy_scale, x, x_scale, offsets, experts, (int32_t)rows, N, H, dw};
-  const auto kernel = dw_dtype == HM_BF16 ? product_kernel<2, 2, 2, 2, true, uint16_t> : product_kernel<2, 2, 2, 2, true, float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((H + 127) / 128), (unsigned)((N + 127) / 128), (unsigned)experts), dim3(256), 0, (hipStream_t)hip_stream, p);
+  const auto kernel = dw_dtype == HM_BF16 ? product_kernel<4, 2, 2, 4, true, uint16_t> : product_kernel<4, 2, 2, 4, true, float>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((H + 255) / 256), (unsigned)((N + 255) / 256), (unsigned)experts), dim3(512), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
