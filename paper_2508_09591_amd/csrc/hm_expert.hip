@@ -115,19 +115,41 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_resource(const uint8_t *a
   return __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, (int)0xFFFFFFFFu, 0x00027000);
 }
 
-// FQ x FP fragments of 32 x 32 in a wave, WQ x WP waves.  LDS holds two steps of 128 bytes of the tile's rows, filled
-// straight from memory while the other is multiplied; a row's eight 16-byte pieces are stored at places exchanged by half
-// the row number, so that sixteen rows of a fragment, which are read together, spread over all 64 banks.  Lane l has
-// row l % 32 of a fragment and its pieces 4 (l / 32) to 4 (l / 32) + 3; which values meet in an instruction does not matter as
-// long as both operands' lanes hold the same ones.
+// All but the last LATER of the wave's loads have arrived in LDS, and then everybody's have; nobody has reads of LDS left.
+template <int LATER>
+__device__ __forceinline__ void arrived() {
+  static_assert(LATER < 64, "the counter's range");
+  __asm__ volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (LATER & 15) | (LATER >> 4) << 14);   // vmcnt(LATER) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  __asm__ volatile("" ::: "memory");
+}
+
+// One code of scale, or four.
+template <bool ONE>
+__device__ __forceinline__ uint32_t codes_at(__amdgpu_buffer_rsrc_t base, uint32_t at) {
+  if constexpr (ONE) return __builtin_amdgcn_raw_buffer_load_b8(base, (int)at, 0, 0);
+  else return __builtin_amdgcn_raw_buffer_load_b32(base, (int)at, 0, 0);
+}
+
+// FQ x FP fragments of 32 x 32 in a wave, WQ x WP waves.
+//
+// LDS is a ring of five units, a unit being one operand's rows of the tile for one step: Q0 P0 Q1 P1 Q2, then P2 in place of Q0
+// and so on, filled straight from memory.  Behind a step its two units are free; the next P is loaded into the one, the Q
+// after the next into the other, so that the one has a step's time to arrive and the other two.  Whole rows of 128
+// bytes: of half the size (and twice the stages) they took the L2 nearly twice the requests.  A row's eight 16-byte
+// pieces are stored at places exchanged by half the row number, so that sixteen rows of a fragment, which are read
+// together, spread over all 64 banks.  Lane l has row l % 32 of a fragment and its pieces 4 (l / 32) to 4 (l / 32) + 3; which
+// values meet in an instruction does not matter as long as both operands' lanes hold the same ones.
+constexpr int kUnits = 5;
 template <int FQ, int FP, int WQ, int WP, bool DW, typename OUT>
 __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams p) {
   constexpr int kWaves = WQ * WP, TQ = FQ * WQ * 32, TP = FP * WP * 32;
   constexpr bool kFull = sizeof(OUT) == 4;
-  constexpr int kSlices = kFull ? 4 : 2;
-  static_assert(kWaves % 2 == 0, "the pieces' places go by it");
-  constexpr int kLoadsQ = TQ / 8 / kWaves, kLoadsP = TP / 8 / kWaves;
-  __shared__ __attribute__((aligned(128))) uint8_t stage[2][(TQ + TP) * 128];
+  constexpr int kSlices = kFull ? 4 : 2, kUnitBytes = TQ * 128;
+  static_assert(TQ == TP && kWaves % 2 == 0, "units of one size; the pieces' places go by the wave's number");
+  constexpr int kLoads = TQ / 8 / kWaves;   // of a wave for a unit
+  __shared__ __attribute__((aligned(128))) uint8_t ring[kUnits * kUnitBytes];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wq = wave / WP, wp = wave % WP;
   Tile t;
   int steps, q_rows, p_rows;
@@ -157,23 +179,23 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
     p_rows = p.N;
   }
   // places of this lane's pieces; rows behind the last are read from the last, their products are not stored
-  uint32_t from_q[kLoadsQ], from_p[kLoadsP];
+  uint32_t from_q[kLoads], from_p[kLoads];
   const int row8 = lane >> 3, piece = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16;   // of row 8 (wave + i kWaves) + row8: half the row, modulo 8
 #pragma unroll
-  for (int i = 0; i < kLoadsQ; ++i) from_q[i] = (uint32_t)min((wave + i * kWaves) * 8 + row8, q_rows - 1 - t.q0) * (uint32_t)pitch + piece;
-#pragma unroll
-  for (int i = 0; i < kLoadsP; ++i) from_p[i] = (uint32_t)min((wave + i * kWaves) * 8 + row8, p_rows - 1 - t.p0) * (uint32_t)pitch + piece;
+  for (int i = 0; i < kLoads; ++i) {
+    from_q[i] = (uint32_t)min((wave + i * kWaves) * 8 + row8, q_rows - 1 - t.q0) * (uint32_t)pitch + piece;
+    from_p[i] = (uint32_t)min((wave + i * kWaves) * 8 + row8, p_rows - 1 - t.p0) * (uint32_t)pitch + piece;
+  }
   // uniform bases and 32-bit offsets: addresses of 64 bits per piece would not fit beside the sums
   const auto base_q = tile_resource(q + (int64_t)t.q0 * pitch), base_p = tile_resource(ps + (int64_t)t.p0 * pitch);
-  auto load = [&](int s, int k) {
-#pragma unroll
-    for (int i = 0; i < kLoadsQ; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(base_q, (__attribute__((address_space(3))) void *)(stage[s] + (wave + i * kWaves) * 1024), 16,
-                                               (int)from_q[i], k * 128, 0, 0);
-#pragma unroll
-    for (int i = 0; i < kLoadsP; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(base_p, (__attribute__((address_space(3))) void *)(stage[s] + (TQ / 8 + wave + i * kWaves) * 1024), 16,
-                                               (int)from_p[i], k * 128, 0, 0);
+  // the i-th load of a unit; behind the last step the last again, which nobody reads
+  auto load_q = [&](int at, int k, int i) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(base_q, (__attribute__((address_space(3))) void *)(ring + at + (wave + i * kWaves) * 1024), 16, (int)from_q[i],
+                                             min(k, steps - 1) * 128, 0, 0);
+  };
+  auto load_p = [&](int at, int k, int i) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(base_p, (__attribute__((address_space(3))) void *)(ring + at + (wave + i * kWaves) * 1024), 16, (int)from_p[i],
+                                             min(k, steps - 1) * 128, 0, 0);
   };
   // scales of this lane's row of each fragment; codes of a step in the lowest byte, rows: those of four steps are loaded together
   uint32_t from_sq[FQ], from_sp[FP], scale_of_q[FQ], scale_of_p[FP], next_q[FQ], next_p[FP];
@@ -188,9 +210,9 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
     const uint8_t *sq = p.q_scale + (DW ? (int64_t)(block0 + k) * p.N + t.q0 : (int64_t)t.q0 * scale_pitch + k);
     const uint8_t *sp = p.p_scale + (DW ? (int64_t)(block0 + k) * p.H + t.p0 : ((int64_t)t.expert * blocks8(p.N) + t.p0 / 128) * scale_pitch + k);
 #pragma unroll
-    for (int i = 0; i < FQ; ++i) next_q[i] = DW ? sq[from_sq[i]] : *(const uint32_t *)(sq + from_sq[i]);
+    for (int i = 0; i < FQ; ++i) next_q[i] = codes_at<DW>(tile_resource(sq), from_sq[i]);
 #pragma unroll
-    for (int i = 0; i < FP; ++i) next_p[i] = DW ? sp[from_sp[i]] : *(const uint32_t *)(sp + from_sp[i]);
+    for (int i = 0; i < FP; ++i) next_p[i] = codes_at<DW>(tile_resource(sp), from_sp[i]);
   };
   f32x16 acc[FQ][FP];
 #pragma unroll
@@ -203,41 +225,53 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
   // operands are read two items ahead, so that the matrix unit always has some.
   constexpr int kItems = kSlices * FQ, kAhead = 2;
   Slice<kFull> of_q[4], of_p[2][FP];
-  // piece 4 (l / 32) of this lane's row and those exchanged with it, in the stage that is read
-  uint32_t to_q[4], to_p[4];
+  uint32_t to_q[4], to_p[4];   // piece 4 (l / 32) of this lane's row and those exchanged with it, in the units that are read
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     const uint32_t at = (uint32_t)((lane & 31) * 128 + (((lane >> 5) * 4) ^ (lane >> 1 & 7) ^ v) * 16);
     to_q[v] = at + (uint32_t)(wq * FQ * 4096);
-    to_p[v] = at + (uint32_t)(TQ * 128 + wp * FP * 4096);
+    to_p[v] = at + (uint32_t)(kUnitBytes + wp * FP * 4096);
   }
   auto read = [&](int item) {
     const int part = item / FQ;
     if (item % FQ == 0) {
 #pragma unroll
-      for (int j = 0; j < FP; ++j) of_p[part & 1][j].read(&stage[0][0], to_p, j * 4096, part);
+      for (int j = 0; j < FP; ++j) of_p[part & 1][j].read(ring, to_p, j * 4096, part);
     }
-    of_q[item & 3].read(&stage[0][0], to_q, item % FQ * 4096, part);
+    of_q[item & 3].read(ring, to_q, item % FQ * 4096, part);
   };
-  auto wait = [] {   // the wave's own pieces are in LDS, then everybody's
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-    __syncthreads();
+  auto two_on = [](int unit) { return unit + (unit >= 3 * kUnitBytes ? -3 * kUnitBytes : 2 * kUnitBytes); };
+  int q_unit = 0, p_unit = kUnitBytes, free_p = 3 * kUnitBytes, free_q = 4 * kUnitBytes;   // read; filled with the P of the next step and the Q after it
+  // The loads are spread over the items since the last turn of the ring: a wave that issues many waits for the others' before
+  // it multiplies on.  P, which is needed first, in the first half; `k`: the step of P.
+  auto fill = [&](int from, int to, int k) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int when = i * (kItems / 2) / kLoads;
+      if (when >= from && when < to) load_p(free_p, k, i);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int when = kItems / 2 + i * (kItems / 2) / kLoads;
+      if (when >= from && when < to) load_q(free_q, k + 1, i);
+    }
   };
+  constexpr int kBefore = kAhead * 2 * kLoads / kItems;   // loads due in the items before a turn of the ring
+  static_assert(kAhead * 2 * kLoads % kItems == 0 && kAhead <= kItems / 2, "whole loads, all of them P's");
   if (steps > 0) {
     load_scales(0);
-    load(0, 0);
-    if (steps > 1) load(1, 1);
-    wait();
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_q(0, 0, i);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_p(kUnitBytes, 0, i);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_q(2 * kUnitBytes, 1, i);
+    fill(0, kAhead, 1);
+    arrived<kLoads + kBefore>();
 #pragma unroll
     for (int item = 0; item < kAhead; ++item) read(item);
   }
-  for (int k = 0; k < steps; ++k) {
-    const bool fresh = DW || (k & 3) == 0;
-#pragma unroll
-    for (int i = 0; i < FQ; ++i) scale_of_q[i] = fresh ? next_q[i] : scale_of_q[i] >> 8;
-#pragma unroll
-    for (int i = 0; i < FP; ++i) scale_of_p[i] = fresh ? next_p[i] : scale_of_p[i] >> 8;
-    if (DW || (k & 3) == 3) load_scales(k + 1 < steps ? k + 1 : 0);
+  auto step = [&](int k) {
 #pragma unroll
     for (int item = 0; item < kItems; ++item) {
       const Slice<kFull> mine = of_q[item & 3];
@@ -246,22 +280,58 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
       for (int j = 0; j < FP; ++j) other[j] = of_p[(item / FQ) & 1][j];
       // what is loaded and read ahead of the last step is not used: a branch around it would part the products from the reads
       if (item + kAhead == kItems) {
-        wait();   // of step k nothing is left to read
-        load(k & 1, min(k + 2, steps - 1));
-        const uint32_t other_stage = (k & 1) ? 0u - (uint32_t)sizeof(stage[0]) : (uint32_t)sizeof(stage[0]);
+        arrived<kLoads>();   // the next step, but for the Q after it; of this one nothing is left to read
+        free_p = q_unit;     // five units: the P of step k + 2 takes the place of the Q of step k, the Q of k + 3 that of the P
+        free_q = p_unit;
+        const int next_q_unit = two_on(q_unit), next_p_unit = two_on(p_unit);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          to_q[v] += other_stage;
-          to_p[v] += other_stage;
+          to_q[v] += (uint32_t)(next_q_unit - q_unit);
+          to_p[v] += (uint32_t)(next_p_unit - p_unit);
         }
+        q_unit = next_q_unit;
+        p_unit = next_p_unit;
       }
+      const int since = (item + kAhead) % kItems;
+      fill(since, since + 1, item + kAhead < kItems ? k + 1 : k + 2);
       read((item + kAhead) % kItems);
 #pragma unroll
       for (int j = 0; j < FP; ++j) other[j].times(mine, scale_of_p[j], scale_of_q[item % FQ], acc[item % FQ][j]);
       __builtin_amdgcn_sched_barrier(0);   // else the compiler reads all items at once and runs out of registers
     }
+  };
+  constexpr int kScaled = DW ? 1 : 4;   // steps whose codes are loaded together, as long before their use
+  auto shift_codes = [&] {
+#pragma unroll
+    for (int i = 0; i < FQ; ++i) scale_of_q[i] >>= 8;
+#pragma unroll
+    for (int i = 0; i < FP; ++i) scale_of_p[i] >>= 8;
+  };
+  auto take_codes = [&] {
+#pragma unroll
+    for (int i = 0; i < FQ; ++i) scale_of_q[i] = next_q[i];
+#pragma unroll
+    for (int i = 0; i < FP; ++i) scale_of_p[i] = next_p[i];
+  };
+  int k = 0;
+  for (; k + kScaled <= steps; k += kScaled) {
+    take_codes();
+    load_scales(k + kScaled < steps ? k + kScaled : 0);
+#pragma unroll
+    for (int u = 0; u < kScaled; ++u) {
+      if (u > 0) shift_codes();
+      step(k + u);
+    }
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // nothing is on its way to LDS when the workgroup ends
+  if constexpr (!DW) {   // what is left of the last four; one loop with an exit behind each step costs copies of the sums
+    take_codes();
+#pragma unroll 1
+    for (; k < steps; ++k) {
+      step(k);
+      shift_codes();
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): nothing is on its way to LDS when the workgroup ends
   // a lane has row l % 32 of a fragment and of every eight columns the first or the last four
 #pragma unroll
   for (int i = 0; i < FQ; ++i) {
@@ -301,8 +371,8 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   const int64_t tiles = (rows / TS + experts) * ((N + TS - 1) / TS) + 8;
   if (tiles > (1 << 23)) return HM_ERR_SHAPE;
   if (TS == 256) {
-  const auto kernel = out_dtype == HM_BF16 ? product_kernel<4, 2, 2, 4, false, uint16_t> : product_kernel<4, 2, 2, 4, false, float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(512), 0, (hipStream_t)hip_stream, p);
+  const auto kernel = out_dtype == HM_BF16 ? product_kernel<4, 4, 2, 2, false, uint16_t> : product_kernel<4, 4, 2, 2, false, float>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(256), 0, (hipStream_t)hip_stream, p);
   } else {
   const auto kernel = out_dtype == HM_BF16 ? product_kernel<2, 2, 2, 2, false, uint16_t> : product_kernel<2, 2, 2, 2, false, float>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(256), 0, (hipStream_t)hip_stream, p);
@@ -318,7 +388,7 @@ extern "C" hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_sc
   const hm_status bad = check_products(gy, gy_scale, x, x_scale, offsets, experts, rows, N, H, dw, dw_dtype, false);
   if (bad != HM_OK) return bad;
   const ProductParams p = {gy, gy_scale, x, x_scale, offsets, experts, (int32_t)rows, N, H, dw};
-  const auto kernel = dw_dtype == HM_BF16 ? product_kernel<4, 2, 2, 4, true, uint16_t> : product_kernel<4, 2, 2, 4, true, float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((H + 255) / 256), (unsigned)((N + 255) / 256), (unsigned)experts), dim3(512), 0, (hipStream_t)hip_stream, p);
+  const auto kernel = dw_dtype == HM_BF16 ? product_kernel<4, 4, 2, 2, true, uint16_t> : product_kernel<4, 4, 2, 2, true, float>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((H + 255) / 256), (unsigned)((N + 255) / 256), (unsigned)experts), dim3(256), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
