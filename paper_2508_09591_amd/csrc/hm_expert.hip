@@ -63,20 +63,9 @@ __device__ __forceinline__ Tile tile_of_rows(const ProductParams &p) {
 }
 
 template <typename OUT>
-__device__ __forceinline__ void store4(OUT *at, int n, const f32x4 &v) {
-  OUT o[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(OUT) == 2) o[i] = (OUT)f32_to_bf16(v[i]);
-    else o[i] = v[i];
-  }
-  if (n >= 4) {
-    __builtin_memcpy(at, o, sizeof(o));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) at[i] = o[i];
-  }
+__device__ __forceinline__ void store4(OUT *at, const f32x4 &v) {   // at a multiple of four elements
+  if constexpr (sizeof(OUT) == 2) *(uint64_t *)at = (uint64_t)pack_bf16x2(v[2], v[3]) << 32 | pack_bf16x2(v[0], v[1]);
+  else *(f32x4 *)at = v;
 }
 
 // What a lane holds of a fragment's row for one part of a step, and its products.
@@ -143,7 +132,7 @@ __device__ __forceinline__ uint32_t codes_at(__amdgpu_buffer_rsrc_t base, uint32
 // values meet in an instruction does not matter as long as both operands' lanes hold the same ones.
 constexpr int kUnits = 5;
 template <int FQ, int FP, int WQ, int WP, bool DW, typename OUT>
-__global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams p) {
+__global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product_kernel(ProductParams p) {
   constexpr int kWaves = WQ * WP, TQ = FQ * WQ * 32, TP = FP * WP * 32;
   constexpr bool kFull = sizeof(OUT) == 4;
   constexpr int kSlices = kFull ? 4 : 2, kUnitBytes = TQ * 128;
@@ -331,20 +320,42 @@ __global__ __launch_bounds__(WQ * WP * kWave) void product_kernel(ProductParams 
       shift_codes();
     }
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): nothing is on its way to LDS when the workgroup ends
-  // a lane has row l % 32 of a fragment and of every eight columns the first or the last four
+  // The wave's part of the tile through LDS, 32 rows at a time, so that stores are whole lines: a lane has row l % 32 of a
+  // fragment and of every eight columns the first or the last four.
+  arrived<0>();   // nothing is on its way to LDS, nobody reads it
+  constexpr int kCols = FP * 32, kRowBytes = kCols * (int)sizeof(OUT), kPitch = kRowBytes + 16, kVec = 16 / (int)sizeof(OUT);
+  static_assert(kWaves * 32 * kPitch <= kUnits * kUnitBytes, "the waves' rows fit the ring");
+  uint8_t *mine = ring + wave * 32 * kPitch;
+  const int c0 = t.p0 + wp * kCols, r_first = t.q0 + wq * FQ * 32;
+  const int64_t out_pitch = DW ? p.H : p.N;
+  OUT *out = (OUT *)p.out + (DW ? (int64_t)t.expert * p.N : 0) * out_pitch + c0;
+  const bool vectors = ((uintptr_t)p.out & 15) == 0 && out_pitch % kVec == 0;   // of every row
 #pragma unroll
   for (int i = 0; i < FQ; ++i) {
-    const int r = t.q0 + (wq * FQ + i) * 32 + (lane & 31);
-    if (r >= q_rows) continue;
-    OUT *row = (OUT *)p.out + (DW ? ((int64_t)t.expert * p.N + r) * p.H : (int64_t)r * p.N);
+    const int r0 = r_first + i * 32;
 #pragma unroll
     for (int j = 0; j < FP; ++j)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int c = t.p0 + (wp * FP + j) * 32 + g * 8 + (lane >> 5) * 4;
-        if (c < p_rows) store4(row + c, p_rows - c, f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+      for (int g = 0; g < 4; ++g)
+        store4((OUT *)(mine + (lane & 31) * kPitch) + j * 32 + g * 8 + (lane >> 5) * 4,
+               f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (vectors) {
+      constexpr int kLanes = kRowBytes / 16, kRows = kWave / kLanes;   // of a row; rows stored together
+      const int c = lane % kLanes * kVec;
+#pragma unroll
+      for (int n = 0; n < 32 / kRows; ++n) {
+        const int r = n * kRows + lane / kLanes;
+        if (r0 + r < q_rows && c0 + c < p_rows) *(u32x4 *)(out + (int64_t)(r0 + r) * out_pitch + c) = *(const u32x4 *)(mine + r * kPitch + c * (int)sizeof(OUT));
       }
+    } else {
+#pragma unroll 1
+      for (int n = lane; n < 32 * kCols; n += kWave) {
+        const int r = n / kCols, c = n % kCols;
+        if (r0 + r < q_rows && c0 + c < p_rows) out[(int64_t)(r0 + r) * out_pitch + c] = ((const OUT *)(mine + r * kPitch))[c];
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
@@ -357,6 +368,31 @@ static hm_status check_products(const void *a, const void *as, const void *b, co
   return HM_OK;
 }
 
+// Rows and columns of a tile, from the tiles that there would be of 256 and of 128.  256 read the operands least often, but
+// a CU holds one, so they need 400 and segments that fill them (us, 256 against 128: 16,384 rows, 16 experts, 1,536 x 2,048 57.0 and
+// 60.5; 8,192, 8, 4,096 x 7,168 236 and 276; 8,192, 32, 2,048 x 2,048 56.3 and 48.2); with fp32 results, bound by products of 16 bits
+// and by widening, 128 are as fast or faster, two to a CU (8,192, 8, 4,096 x 7,168 453 and 416), but for the gradient of the weights
+// (32,768, 16, 1,536 x 2,048 182 and 195).  Tiles of 64 for few: 8 rows, 32, 4,096 x 7,168 35.3 and 36.0 with 128; 1,000, 1,
+// 500 x 700 7.1 and 10.5; 1,024, 8, 2,048 x 2,048 13.6 and 14.2; but 2,048, 32, 2,048 x 2,048 (512 tiles of 128) 30.0 and 24.3.
+static int tile_side(bool large, int64_t tiles128) { return large ? 256 : tiles128 >= 200 ? 128 : 64; }
+
+template <int FQ, int FP, int WQ, int WP, bool DW>
+static hm_status launch_tiles(const ProductParams &p, hm_dtype dtype, dim3 grid, void *stream) {
+  const auto kernel = dtype == HM_BF16 ? product_kernel<FQ, FP, WQ, WP, DW, uint16_t> : product_kernel<FQ, FP, WQ, WP, DW, float>;
+  hipLaunchKernelGGL(kernel, grid, dim3(WQ * WP * kWave), 0, (hipStream_t)stream, p);
+  return hm_launch_status();
+}
+template <bool DW>
+static hm_status launch_products(const ProductParams &p, int side, hm_dtype dtype, dim3 grid, void *stream) {
+  if (side == 256) {
+    if constexpr (DW) return launch_tiles<4, 4, 2, 2, true>(p, dtype, grid, stream);
+    hipLaunchKernelGGL((product_kernel<4, 4, 2, 2, false, uint16_t>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    return hm_launch_status();
+  }
+  if (side == 128) return launch_tiles<2, 2, 2, 2, DW>(p, dtype, grid, stream);
+  return launch_tiles<2, 1, 1, 2, DW>(p, dtype, grid, stream);
+}
+
 }  // namespace hm
 
 extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, const uint8_t *w, const uint8_t *w_scale, const int32_t *offsets,
@@ -367,17 +403,11 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   if (bad != HM_OK) return bad;
   if (rows == 0) return HM_OK;
   const ProductParams p = {x, x_scale, w, w_scale, offsets, experts, (int32_t)rows, N, H, out};
-  const int TS = rows / experts >= 256 ? 256 : 128;
-  const int64_t tiles = (rows / TS + experts) * ((N + TS - 1) / TS) + 8;
+  const bool large = out_dtype == HM_BF16 && rows / experts >= 512 && (rows / 256 + experts / 2) * ((N + 255) / 256) >= 400;
+  const int side = tile_side(large, (rows / 128 + experts / 2) * ((N + 127) / 128));
+  const int64_t tiles = (rows / side + experts) * ((N + side - 1) / side) + 8;
   if (tiles > (1 << 23)) return HM_ERR_SHAPE;
-  if (TS == 256) {
-  const auto kernel = out_dtype == HM_BF16 ? product_kernel<4, 4, 2, 2, false, uint16_t> : product_kernel<4, 4, 2, 2, false, float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(256), 0, (hipStream_t)hip_stream, p);
-  } else {
-  const auto kernel = out_dtype == HM_BF16 ? product_kernel<2, 2, 2, 2, false, uint16_t> : product_kernel<2, 2, 2, 2, false, float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(256), 0, (hipStream_t)hip_stream, p);
-  }
-  return hm_launch_status();
+  return launch_products<false>(p, side, out_dtype, dim3((unsigned)tiles), hip_stream);
 }
 
 extern "C" hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_scale, const uint8_t *x, const uint8_t *x_scale,
@@ -387,8 +417,9 @@ extern "C" hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_sc
   using namespace hm;
   const hm_status bad = check_products(gy, gy_scale, x, x_scale, offsets, experts, rows, N, H, dw, dw_dtype, false);
   if (bad != HM_OK) return bad;
+  if (column8_blocks(rows, experts) >= (1 << 17)) return HM_ERR_SHAPE;   // 256 rows of a tile within offsets of 32 bits
   const ProductParams p = {gy, gy_scale, x, x_scale, offsets, experts, (int32_t)rows, N, H, dw};
-  const auto kernel = dw_dtype == HM_BF16 ? product_kernel<4, 4, 2, 2, true, uint16_t> : product_kernel<4, 4, 2, 2, true, float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((H + 255) / 256), (unsigned)((N + 255) / 256), (unsigned)experts), dim3(256), 0, (hipStream_t)hip_stream, p);
-  return hm_launch_status();
+  const bool large = (int64_t)((H + 255) / 256) * ((N + 255) / 256) * experts >= 256;
+  const int side = tile_side(large, (int64_t)((H + 127) / 128) * ((N + 127) / 128) * experts);
+  return launch_products<true>(p, side, dw_dtype, dim3((unsigned)((H + side - 1) / side), (unsigned)((N + side - 1) / side), (unsigned)experts), hip_stream);
 }
