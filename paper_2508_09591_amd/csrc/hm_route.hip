@@ -1,4 +1,6 @@
 // The router in front of the dispatch: logits -> expert ids and weights, and the way back.
+#include <type_traits>
+
 #include "hm_block8.h"
 
 namespace hm {
@@ -129,6 +131,216 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteParams p) {
   if (lane < K) {
     p.ids[t * K + lane] = id;
     p.weights[t * K + lane] = by > 0.0f ? score / by * p.r.scale : 0.0f;
+  }
+}
+
+// ---- choice by sorted lists ----------------------------------------------------------------------------
+// A choice and its expert as one number of 64 bits that orders as the definition does: the fp32 choice is the high word
+// of a double, whose order is that of the floats (a float's bits with anything behind them are a finite double, -inf's and +inf's
+// too), and the low word puts the lower of two equal experts first.  The largest and the smaller of two are one
+// instruction each.
+__device__ __forceinline__ double key_of(float choice, int e) {
+  const int32_t high = __builtin_bit_cast(int32_t, choice + 0.0f);   // -0 is 0
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)high << 32 | (uint32_t)(high < 0 ? e : ~e));
+}
+__device__ __forceinline__ float choice_of(double key) { return __builtin_bit_cast(float, (uint32_t)(__builtin_bit_cast(uint64_t, key) >> 32)); }
+__device__ __forceinline__ int expert_of(double key) {
+  const uint64_t k = __builtin_bit_cast(uint64_t, key);
+  return (int64_t)k < 0 ? (int)(uint32_t)k : ~(int)(uint32_t)k;
+}
+__device__ __forceinline__ double none_key() { return __builtin_bit_cast(double, (uint64_t)0xFF800000u << 32); }   // -inf
+__device__ __forceinline__ double larger(double a, double b) {   // as it is, without the compiler's care for signalling NaN
+  double r;
+  __asm__("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ double smaller(double a, double b) {
+  double r;
+  __asm__("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ void order(double &a, double &b) {
+  const double high = larger(a, b);
+  b = smaller(a, b);
+  a = high;
+}
+// N keys, descending; N a power of two.  Merge exchange (Batcher), then a bitonic merge of what rises and falls.
+template <int N>
+__device__ __forceinline__ void sort(double (&k)[N]) {
+#pragma unroll
+  for (int p = 1; p < N; p *= 2)
+#pragma unroll
+    for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < N; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; ++i)
+          if (i + j + q < N && (i + j) / (2 * p) == (i + j + q) / (2 * p)) order(k[i + j], k[i + j + q]);
+}
+// The N largest of two descending lists, descending, in `k`.
+template <int N>
+__device__ __forceinline__ void merge(double (&k)[N], const double (&other)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) k[i] = larger(k[i], other[N - 1 - i]);
+#pragma unroll
+  for (int d = N / 2; d >= 1; d /= 2)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (!(i & d)) order(k[i], k[i + d]);
+}
+// From a lane of the other half of 2 D lanes, D = 1, 2, 4, 8, where all lanes of a half hold the same.
+template <int D>
+__device__ __forceinline__ int other_half(int v) {
+  constexpr int kControl = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x140;   // quads 1 0 3 2 and 2 3 0 1; mirrors of eight and sixteen
+  return __builtin_amdgcn_update_dpp(0, v, kControl, 0xF, 0xF, true);
+}
+template <int D>
+__device__ __forceinline__ float other_half(float v) { return __builtin_bit_cast(float, other_half<D>(__builtin_bit_cast(int, v))); }
+template <int D>
+__device__ __forceinline__ double other_half(double v) {
+  const uint64_t k = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)other_half<D>((int)(k >> 32)) << 32 | (uint32_t)other_half<D>((int)k));
+}
+// op(v, what the other half has) for halves of FROM up to half of UPTO lanes.
+template <int FROM, int UPTO, typename OP>
+__device__ __forceinline__ void over_halves(OP op) {
+  if constexpr (FROM < UPTO) {
+    op(std::integral_constant<int, FROM>());
+    over_halves<2 * FROM, UPTO>(op);
+  }
+}
+
+// N consecutive elements, none's from the n-th on.
+template <int N, typename IN>
+__device__ __forceinline__ void load_logits(const IN *p, int n, float (&v)[N]) {
+  if (n >= N) {
+    IN raw[N];
+    __builtin_memcpy(raw, p, sizeof(raw));
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = logit_at(raw, i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < n ? logit_at(p, i) : kNone();
+  }
+}
+
+// L lanes take a token, each a run of its experts, of which it keeps the N >= K largest; the lists of the lanes are
+// then merged pairwise.  With groups the L lanes are shared among them, so that a lane's run lies in one group, and
+// the two largest of its list give the group's score: lists of groups that are not taken are emptied before the merges.
+// What bounds it are vector instructions: 25 per expert of a logistic score, 7 of keys and 13 of sorting (N = 8), against
+// 4 bytes read.
+template <typename IN, int L, int N>
+__global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteParams p, int lanes_per_group, int run) {
+  const int sub = (int)threadIdx.x & (L - 1);
+  const int64_t t = (int64_t)blockIdx.x * (kRouteThreads / L) + threadIdx.x / L;
+  const bool there = t < p.T;
+  const int E = p.r.E, K = p.r.K, per = E / p.r.groups, group = sub / lanes_per_group;
+  const IN *x = (const IN *)p.logits + (there ? t : p.T - 1) * p.ld;
+  const bool softmax = p.r.score == HM_SCORE_SOFTMAX;   // then there is no bias
+  const int e = group * per + (sub - group * lanes_per_group) * run;
+  const int end = min(e + run, (group + 1) * per);
+  double list[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) list[i] = none_key();
+  for (int first = e; first < end; first += N) {
+    float v[N];
+    load_logits<N>(x + first, end - first, v);
+    double batch[N];
+    if (p.bias) {
+      float b[N];
+      load_logits<N>(p.bias + first, end - first, b);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float u = usable(v[i]), c = logistic(u) + b[i];
+        batch[i] = u == kNone() || c != c ? none_key() : key_of(c, first + i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) batch[i] = v[i] == v[i] ? key_of(usable(v[i]), first + i) : none_key();
+    }
+    sort(batch);
+    merge(list, batch);
+  }
+  float best = choice_of(list[0]);   // the softmax's largest logit: of all experts
+  if (softmax) over_halves<1, L>([&](auto d) { best = fmaxf(best, other_half<d()>(best)); });
+  if (p.r.groups > 1) {
+    const bool pair = p.r.group_best == 2;
+    auto score_of = [&](double key) {
+      const float c = choice_of(key);
+      return c == kNone() || p.bias ? c : softmax ? expf(c - best) : logistic(c);
+    };
+    float a = score_of(list[0]), b = pair ? score_of(list[1]) : kNone();
+    over_halves<1, L>([&](auto d) {
+      if (d() < lanes_per_group) {
+        const float c = other_half<d()>(a), f = other_half<d()>(b);
+        b = fmaxf(fminf(a, c), fmaxf(b, f));
+        a = fmaxf(a, c);
+      }
+    });
+    const float mine = b != kNone() ? a + b : a;
+    int better = 0;
+    for (int g = 1; g < p.r.groups; ++g) {
+      const int other_group = (group + g) & (p.r.groups - 1);
+      const float c = __shfl(pair ? mine : a, (lane_id() & ~(L - 1)) + other_group * lanes_per_group, kWave);
+      const float m = pair ? mine : a;
+      better += c > m || (c == m && other_group < group);
+    }
+    if (better >= p.r.top_groups) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) list[i] = none_key();
+    }
+  }
+  over_halves<1, L>([&](auto d) {
+    double other[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) other[i] = other_half<d()>(list[i]);
+    merge(list, other);
+  });
+  // Slot k is lane k's; with fewer lanes than slots a lane has several.
+  constexpr int kMine = N > L ? N / L : 1;
+  float score[kMine], total = 0.0f;
+  int id[kMine];
+#pragma unroll
+  for (int m = 0; m < kMine; ++m) {
+    const int k = sub + m * L;
+    double key = none_key();
+#pragma unroll
+    for (int i = m * L; i < min(N, (m + 1) * L); ++i) key = i == k ? list[i] : key;
+    const float c = choice_of(key);
+    const bool chosen = k < K && c != kNone();
+    id[m] = chosen ? expert_of(key) : -1;
+    const float logit = p.bias ? (chosen ? usable(logit_at(x, id[m])) : kNone()) : c;
+    score[m] = !chosen ? 0.0f : softmax ? expf(logit - choice_of(list[0])) : logistic(logit);
+    total += score[m];
+  }
+  float by = 1.0f;
+  if (p.r.renormalise) {
+    over_halves<1, L>([&](auto d) { total += other_half<d()>(total); });
+    by = total;
+  } else if (softmax) {   // over all experts, once more through them; scores are relative to the largest of all
+    const float first = choice_of(list[0]), shift = first == kNone() ? 1.0f : expf(first - best);
+    float sum = 0.0f;
+    for (int at = e; at < end; at += N) {
+      float v[N];
+      load_logits<N>(x + at, end - at, v);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float u = usable(v[i]);
+        sum += u == kNone() ? 0.0f : expf(u - best);
+      }
+    }
+    over_halves<1, L>([&](auto d) { sum += other_half<d()>(sum); });
+    by = sum;
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) score[m] *= shift;
+  }
+#pragma unroll
+  for (int m = 0; m < kMine; ++m) {
+    const int k = sub + m * L;
+    if (there && k < K) {
+      p.ids[t * K + k] = id[m];
+      p.weights[t * K + k] = by > 0.0f ? score[m] / by * p.r.scale : 0.0f;
+    }
   }
 }
 
@@ -263,6 +475,23 @@ static hm_status check_router(const hm_router *r) {
   if (r->K > r->E / r->groups * r->top_groups) return HM_ERR_SHAPE;
   return HM_OK;
 }
+// Lanes of a token for the choice by lists, 0 where it is not made: groups share the lanes, and a softmax with a bias needs its
+// sum before the choice.
+static int list_lanes(const hm_router &r, bool biased, int64_t T) {
+  if (r.K > 16 || (r.groups & (r.groups - 1)) || r.groups > 16 || (biased && r.score == HM_SCORE_SOFTMAX)) return 0;
+  const int lanes = T >= 16384 && r.groups <= 8 ? 8 : 16;
+  return r.E <= 64 * lanes ? lanes : 0;
+}
+template <typename IN, int L>
+static void launch_lists(const RouteParams &p, hipStream_t stream) {
+  const int K = p.r.K, lanes_per_group = L / p.r.groups, run = (p.r.E / p.r.groups + lanes_per_group - 1) / lanes_per_group;
+  const auto kernel = K <= 2   ? route_lists_kernel<IN, L, 2>
+                      : K <= 4 ? route_lists_kernel<IN, L, 4>
+                      : K <= 8 ? route_lists_kernel<IN, L, 8>
+                               : route_lists_kernel<IN, L, 16>;
+  const int64_t per_block = kRouteThreads / L;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.T + per_block - 1) / per_block)), dim3(kRouteThreads), 0, stream, p, lanes_per_group, run);
+}
 // Tokens of a workgroup whose rows of `floats` fit 64 KiB.
 static int tokens_per_group(int floats) {
   int n = kRouteWaves;
@@ -284,6 +513,12 @@ extern "C" hm_status hm_route(const void *logits, hm_dtype dtype, int64_t ld, co
   if (T == 0) return HM_OK;
   if (!logits || !topk_ids || !topk_weights) return HM_ERR_NULL;
   const RouteParams p = {logits, ld, bias, T, *router, topk_ids, topk_weights};
+  if (const int lanes = list_lanes(p.r, bias != nullptr, T)) {
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (dtype == HM_BF16) lanes == 8 ? launch_lists<uint16_t, 8>(p, stream) : launch_lists<uint16_t, 16>(p, stream);
+    else lanes == 8 ? launch_lists<float, 8>(p, stream) : launch_lists<float, 16>(p, stream);
+    return hm_launch_status();
+  }
   const int floats = router->E + (router->groups > 1 ? router->groups : 0), n = tokens_per_group(floats);
   const auto kernel = dtype == HM_BF16 ? route_kernel<uint16_t> : route_kernel<float>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((T + (int64_t)n - 1) / n)), dim3((unsigned)(n * kWave)), (size_t)n * floats * 4, (hipStream_t)hip_stream, p);
