@@ -63,6 +63,11 @@ _NATIVE = ("hm_plan", "hm_plan_mapped", "hm_dispatch_pack", "hm_combine", "hm_co
            "hm_swap_select", "hm_swap_apply")
 
 
+# The same for the router's and the experts' calls: its Layer struct.
+_NATIVE_LAYER = ("hm_route", "hm_route_backward", "hm_combine_weight_grad", "hm_quantize_rows", "hm_quantize_columns", "hm_quantize_weights",
+                 "hm_expert_matmul", "hm_expert_matmul_dw")
+
+
 class hm_topology(ctypes.Structure):
     _fields_ = [("nodes", ctypes.c_int32), ("ranks_per_node", ctypes.c_int32)]
 
@@ -182,6 +187,7 @@ def lib():
         L.hm_status_string.restype = ctypes.c_char_p
         L.hm_status_string.argtypes = [ctypes.c_int]
         _native.bind(*[ctypes.cast(getattr(L, name), vp).value for name in _NATIVE])
+        _native.bind_layer(*[ctypes.cast(getattr(L, name), vp).value for name in _NATIVE_LAYER])
         _lib = L
     return _lib
 
@@ -691,6 +697,10 @@ def alloc_weights8(experts: int, N: int, C: int, device="cuda"):
 def hm_route(logits: torch.Tensor, router: Router, topk_ids: torch.Tensor, topk_weights: torch.Tensor,
              bias: Optional[torch.Tensor] = None, stream=None):
     """Expert ids and weights of every token, as hm_plan takes them."""
+    rc = _native.route(logits, router, topk_ids, topk_weights, bias) if stream is None else None
+    if rc is not None:
+        _check("hm_route", rc)
+        return topk_ids, topk_weights
     at, ld = _rows_of(logits, "logits")
     T, E = logits.shape
     if E != router.E:
@@ -706,6 +716,10 @@ def hm_route(logits: torch.Tensor, router: Router, topk_ids: torch.Tensor, topk_
 
 def hm_route_backward(logits: torch.Tensor, router: Router, topk_ids: torch.Tensor, grad_weights: torch.Tensor,
                       grad_logits: torch.Tensor, stream=None) -> torch.Tensor:
+    rc = _native.route_backward(logits, router, topk_ids, grad_weights, grad_logits) if stream is None else None
+    if rc is not None:
+        _check("hm_route_backward", rc)
+        return grad_logits
     at, ld = _rows_of(logits, "logits")
     T, E = logits.shape
     if E != router.E:
@@ -722,6 +736,10 @@ def hm_route_backward(logits: torch.Tensor, router: Router, topk_ids: torch.Tens
 
 
 def hm_combine_weight_grad(gout: torch.Tensor, y: torch.Tensor, plan: Plan, grad_weights: torch.Tensor, stream=None) -> torch.Tensor:
+    rc = _native.combine_weight_grad(gout, y, plan, grad_weights) if stream is None else None
+    if rc is not None:
+        _check("hm_combine_weight_grad", rc)
+        return grad_weights
     T, H = gout.shape
     _rows_call_shape(plan, T, grad_weights, "gout")
     if y.shape[1] != H:
@@ -733,6 +751,10 @@ def hm_combine_weight_grad(gout: torch.Tensor, y: torch.Tensor, plan: Plan, grad
 
 
 def hm_quantize_rows(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, stream=None):
+    rc = _native.quantize_rows(x, q, scale) if stream is None else None
+    if rc is not None:
+        _check("hm_quantize_rows", rc)
+        return q, scale
     at, ld = _rows_of(x, "x")
     rows, C = x.shape
     rc = lib().hm_quantize_rows(at, _floats(x, "x"), ld, rows, C, _codes(q, (rows, row8_bytes(C)), "q"),
@@ -743,6 +765,10 @@ def hm_quantize_rows(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, stre
 
 def hm_quantize_columns(x: torch.Tensor, offsets: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, stream=None):
     """offsets [segments + 1]: a plan's dest_offset."""
+    rc = _native.quantize_columns(x, offsets, q, scale) if stream is None else None
+    if rc is not None:
+        _check("hm_quantize_columns", rc)
+        return q, scale
     at, ld = _rows_of(x, "x")
     rows, C = x.shape
     segments = offsets.numel() - 1
@@ -756,6 +782,10 @@ def hm_quantize_columns(x: torch.Tensor, offsets: torch.Tensor, q: torch.Tensor,
 def hm_quantize_weights(w: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, qt: Optional[torch.Tensor] = None,
                         scale_t: Optional[torch.Tensor] = None, stream=None):
     """With qt and scale_t the transposed weights too."""
+    rc = _native.quantize_weights(w, q, scale, qt, scale_t) if stream is None else None
+    if rc is not None:
+        _check("hm_quantize_weights", rc)
+        return (q, scale) if qt is None else (q, scale, qt, scale_t)
     E, N, C = w.shape
     if qt is not None:
         _shaped(qt, (E, C, row8_bytes(N)), "qt")
@@ -773,6 +803,10 @@ def hm_expert_matmul(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_
                      out: torch.Tensor, stream=None) -> torch.Tensor:
     """out [rows, N]: every row times the weights of its expert.  x and w hold as many blocks of 128 columns, the columns
     themselves are told from them: zeros fill the last block, so its end does not matter."""
+    rc = _native.expert_matmul(x, x_scale, w, w_scale, offsets, out) if stream is None else None
+    if rc is not None:
+        _check("hm_expert_matmul", rc)
+        return out
     E, N, width = w.shape
     rows = x.shape[0]
     rc = lib().hm_expert_matmul(_codes(x, (rows, width), "x"), _scales(x_scale, (rows, scale8_bytes(width)), "x_scale"),
@@ -786,6 +820,10 @@ def hm_expert_matmul(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_
 def hm_expert_matmul_dw(gy: torch.Tensor, gy_scale: torch.Tensor, x: torch.Tensor, x_scale: torch.Tensor, offsets: torch.Tensor,
                         rows: int, dw: torch.Tensor, stream=None) -> torch.Tensor:
     """dw [experts, N, H] from the columns of gy [N, ...] and x [H, ...] over `rows` rows ordered by expert."""
+    rc = _native.expert_matmul_dw(gy, gy_scale, x, x_scale, offsets, rows, dw) if stream is None else None
+    if rc is not None:
+        _check("hm_expert_matmul_dw", rc)
+        return dw
     E, N, H = dw.shape
     blocks = rows // 128 + E
     rc = lib().hm_expert_matmul_dw(_codes(gy, (N, 128 * blocks), "gy"), _scales(gy_scale, (blocks, N), "gy_scale"),

@@ -399,9 +399,186 @@ PyObject *swap_apply(PyObject *, PyObject *const *a, Py_ssize_t n) {   // expert
   });
 }
 
-// bind(addresses): the entry points, in the order of Library.
-PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  constexpr int kEntries = sizeof(Library) / sizeof(void *);
+// ---- the router in front of the dispatch, the experts behind it ----
+// Bound apart from the calls above.
+struct Layer {
+  decltype(&hm_route) route;
+  decltype(&hm_route_backward) route_backward;
+  decltype(&hm_combine_weight_grad) combine_weight_grad;
+  decltype(&hm_quantize_rows) quantize_rows;
+  decltype(&hm_quantize_columns) quantize_columns;
+  decltype(&hm_quantize_weights) quantize_weights;
+  decltype(&hm_expert_matmul) expert_matmul;
+  decltype(&hm_expert_matmul_dw) expert_matmul_dw;
+} layer;
+bool layer_bound = false;
+
+template <typename Body>
+PyObject *layer_answer(Py_ssize_t given, Py_ssize_t wanted, Body body) {
+  if (layer_bound && given == wanted) {
+    try {
+      return PyLong_FromLong(body());
+    } catch (...) {   // as in answer()
+      PyErr_Clear();
+    }
+  }
+  Py_RETURN_NONE;
+}
+
+// A Router of the binding: the host struct the C calls take.
+class Router {
+ public:
+  explicit Router(PyObject *o) {
+    const Ref c(PyObject_GetAttr(o, name_c));
+    if (PyObject_GetBuffer(c.get(), &view_, PyBUF_SIMPLE) != 0) throw NotOrdinary();
+    if (view_.len != static_cast<Py_ssize_t>(sizeof(hm_router))) {
+      PyBuffer_Release(&view_);
+      throw NotOrdinary();
+    }
+  }
+  ~Router() { PyBuffer_Release(&view_); }
+  Router(const Router &) = delete;
+  Router &operator=(const Router &) = delete;
+  const hm_router *c() const { return static_cast<const hm_router *>(view_.buf); }
+
+ private:
+  Py_buffer view_;
+};
+
+hm_dtype floats(const at::Tensor &t) {
+  if (t.scalar_type() == at::kBFloat16) return HM_BF16;
+  if (t.scalar_type() == at::kFloat) return HM_F32;
+  throw NotOrdinary();
+}
+// A dense matrix of floats.
+const at::Tensor &matrix(PyObject *o, int32_t &rows, int32_t &cols) {
+  const at::Tensor &t = tensor(o);
+  if (!t.is_cuda() || !t.is_contiguous()) throw NotOrdinary();
+  floats(t);
+  shape(t, rows, cols);
+  return t;
+}
+template <typename T>
+T *shaped(PyObject *o, at::ScalarType type, std::initializer_list<int64_t> sizes) {
+  const at::Tensor &t = checked(o, type);
+  if (t.sizes() != at::IntArrayRef(sizes)) throw NotOrdinary();
+  return static_cast<T *>(t.data_ptr());
+}
+uint8_t *values8(PyObject *o, std::initializer_list<int64_t> sizes) { return shaped<uint8_t>(o, at::kFloat8_e4m3fn, sizes); }
+uint8_t *scales8(PyObject *o, std::initializer_list<int64_t> sizes) { return shaped<uint8_t>(o, at::kByte, sizes); }
+int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+
+PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {   // logits, router, ids, weights, bias
+  return layer_answer(n, 5, [&] {
+    int32_t T, E;
+    const at::Tensor &logits = matrix(a[0], T, E);
+    const Router r(a[1]);
+    const int64_t K = r.c()->K;
+    if (E != r.c()->E) throw NotOrdinary();
+    auto *ids = shaped<int32_t>(a[2], at::kInt, {T, K});
+    auto *weights = shaped<float>(a[3], at::kFloat, {T, K});
+    const auto *bias = a[4] == Py_None ? nullptr : shaped<const float>(a[4], at::kFloat, {E});
+    return launched([&](void *s) { return layer.route(logits.data_ptr(), floats(logits), E, bias, T, r.c(), ids, weights, s); });
+  });
+}
+
+PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {   // logits, router, ids, grad_weights, grad_logits
+  return layer_answer(n, 5, [&] {
+    int32_t T, E;
+    const at::Tensor &logits = matrix(a[0], T, E);
+    const Router r(a[1]);
+    const int64_t K = r.c()->K;
+    if (E != r.c()->E) throw NotOrdinary();
+    const auto *ids = shaped<const int32_t>(a[2], at::kInt, {T, K});
+    const auto *grad = shaped<const float>(a[3], at::kFloat, {T, K});
+    auto *to = shaped<void>(a[4], logits.scalar_type(), {T, E});
+    return launched([&](void *s) { return layer.route_backward(logits.data_ptr(), floats(logits), E, ids, grad, T, r.c(), to, E, s); });
+  });
+}
+
+PyObject *combine_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {   // gout, y, plan, grad_weights
+  return layer_answer(n, 4, [&] {
+    int32_t T, H, rows, cols;
+    const at::Tensor &gout = matrix(a[0], T, H), &y = matrix(a[1], rows, cols);
+    if (cols != H || y.scalar_type() != gout.scalar_type()) throw NotOrdinary();
+    const Plan p(a[2]);
+    p.expect(T, a[3]);
+    auto *grad = pointer<float>(a[3], at::kFloat);
+    return launched([&](void *s) { return layer.combine_weight_grad(gout.data_ptr(), y.data_ptr(), floats(gout), rows, T, p.K, H, p.c(), grad, s); });
+  });
+}
+
+PyObject *quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, q, scale
+  return layer_answer(n, 3, [&] {
+    int32_t rows, C;
+    const at::Tensor &x = matrix(a[0], rows, C);
+    auto *q = values8(a[1], {rows, up(C, 128)}), *scale = scales8(a[2], {rows, up(C, 512) / 128});
+    return launched([&](void *s) { return layer.quantize_rows(x.data_ptr(), floats(x), C, rows, C, q, scale, s); });
+  });
+}
+
+PyObject *quantize_columns(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, offsets, q, scale
+  return layer_answer(n, 4, [&] {
+    int32_t rows, C;
+    const at::Tensor &x = matrix(a[0], rows, C);
+    const auto *offsets = pointer<const int32_t>(a[1], at::kInt);
+    const int32_t segments = size32(tensor(a[1]).numel() - 1);
+    const int64_t blocks = rows / 128 + static_cast<int64_t>(segments);
+    auto *q = values8(a[2], {C, 128 * blocks}), *scale = scales8(a[3], {blocks, C});
+    return launched([&](void *s) { return layer.quantize_columns(x.data_ptr(), floats(x), C, offsets, segments, rows, C, q, scale, s); });
+  });
+}
+
+PyObject *quantize_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {   // w, q, scale, qt, scale_t
+  return layer_answer(n, 5, [&] {
+    const at::Tensor &w = tensor(a[0]);
+    if (!w.is_cuda() || !w.is_contiguous() || w.dim() != 3) throw NotOrdinary();
+    const hm_dtype dtype = floats(w);
+    const int32_t E = size32(w.size(0)), N = size32(w.size(1)), C = size32(w.size(2));
+    auto *q = values8(a[1], {E, N, up(C, 128)}), *scale = scales8(a[2], {E, up(N, 128) / 128, up(C, 512) / 128});
+    const bool both = a[3] != Py_None;
+    if (both == (a[4] == Py_None)) throw NotOrdinary();
+    auto *qt = both ? values8(a[3], {E, C, up(N, 128)}) : nullptr;
+    auto *scale_t = both ? scales8(a[4], {E, up(C, 128) / 128, up(N, 512) / 128}) : nullptr;
+    return launched([&](void *s) { return layer.quantize_weights(w.data_ptr(), dtype, E, N, C, q, scale, qt, scale_t, s); });
+  });
+}
+
+PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, x_scale, w, w_scale, offsets, out
+  return layer_answer(n, 6, [&] {
+    const at::Tensor &w = checked(a[2], at::kFloat8_e4m3fn);
+    if (w.dim() != 3) throw NotOrdinary();
+    const int32_t E = size32(w.size(0)), N = size32(w.size(1)), H = size32(w.size(2));
+    int32_t rows, cols;
+    const at::Tensor &out = matrix(a[5], rows, cols);
+    if (cols != N) throw NotOrdinary();
+    const auto *x = values8(a[0], {rows, H}), *xs = scales8(a[1], {rows, up(H, 512) / 128});
+    const auto *ws = scales8(a[3], {E, up(N, 128) / 128, up(H, 512) / 128});
+    const auto *offsets = shaped<const int32_t>(a[4], at::kInt, {static_cast<int64_t>(E) + 1});
+    const auto *wq = static_cast<const uint8_t *>(w.data_ptr());
+    return launched([&](void *s) { return layer.expert_matmul(x, xs, wq, ws, offsets, E, rows, N, H, out.data_ptr(), floats(out), s); });
+  });
+}
+
+PyObject *expert_matmul_dw(PyObject *, PyObject *const *a, Py_ssize_t n) {   // gy, gy_scale, x, x_scale, offsets, rows, dw
+  return layer_answer(n, 7, [&] {
+    const at::Tensor &dw = tensor(a[6]);
+    if (!dw.is_cuda() || !dw.is_contiguous() || dw.dim() != 3) throw NotOrdinary();
+    const hm_dtype dtype = floats(dw);
+    const int32_t E = size32(dw.size(0)), N = size32(dw.size(1)), H = size32(dw.size(2)), rows = integer32(a[5]);
+    if (rows < 0) throw NotOrdinary();
+    const int64_t blocks = rows / 128 + static_cast<int64_t>(E);
+    const auto *gy = values8(a[0], {N, 128 * blocks}), *gs = scales8(a[1], {blocks, N});
+    const auto *x = values8(a[2], {H, 128 * blocks}), *xs = scales8(a[3], {blocks, H});
+    const auto *offsets = shaped<const int32_t>(a[4], at::kInt, {static_cast<int64_t>(E) + 1});
+    return launched([&](void *s) { return layer.expert_matmul_dw(gy, gs, x, xs, offsets, E, rows, N, H, dw.data_ptr(), dtype, s); });
+  });
+}
+
+// Takes the addresses of a struct's entry points, in its order.
+template <typename Entries>
+PyObject *take(Entries &entries, bool &done, PyObject *const *a, Py_ssize_t n) {
+  constexpr int kEntries = sizeof(Entries) / sizeof(void *);
   void *address[kEntries];
   if (n != kEntries) {
     PyErr_Format(PyExc_TypeError, "%d addresses expected", kEntries);
@@ -414,16 +591,21 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
       return nullptr;
     }
   }
-  std::memcpy(static_cast<void *>(&lib), address, sizeof(lib));
-  bound = true;
+  std::memcpy(static_cast<void *>(&entries), address, sizeof(entries));
+  done = true;
   Py_RETURN_NONE;
 }
+PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) { return take(lib, bound, a, n); }
+PyObject *bind_layer(PyObject *, PyObject *const *a, Py_ssize_t n) { return take(layer, layer_bound, a, n); }
 
 #define HM_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HM_METHOD(plan), HM_METHOD(plan_mapped), HM_METHOD(dispatch_pack), HM_METHOD(combine), HM_METHOD(combine_f32),
                          HM_METHOD(combine_mix), HM_METHOD(combine_transpose), HM_METHOD(combine_transpose_bf16),
                          HM_METHOD(expert_load), HM_METHOD(group_counts), HM_METHOD(alltoall_times), HM_METHOD(swap_counts_multi),
-                         HM_METHOD(swap_select), HM_METHOD(swap_apply), HM_METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+                         HM_METHOD(swap_select), HM_METHOD(swap_apply), HM_METHOD(bind), HM_METHOD(route), HM_METHOD(route_backward),
+                         HM_METHOD(combine_weight_grad), HM_METHOD(quantize_rows), HM_METHOD(quantize_columns),
+                         HM_METHOD(quantize_weights), HM_METHOD(expert_matmul), HM_METHOD(expert_matmul_dw), HM_METHOD(bind_layer),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hmcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
