@@ -49,31 +49,45 @@ __device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d, fl
 }
 
 typedef f32x4 f32x4_align4 __attribute__((aligned(4)));
-// Eight consecutive elements as fp32, zeros from the n-th on; any alignment of the elements.
-__device__ __forceinline__ void load8(const uint16_t *__restrict__ p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    const u32x4 w = *(const u32x4_align2 *)p;
+typedef uint32_t u32x2_align2 __attribute__((ext_vector_type(2), aligned(2)));
+// N = 4 or 8 consecutive elements as fp32; any alignment of the elements.
+template <int N>
+__device__ __forceinline__ void load_floats(const uint16_t *__restrict__ p, float (&v)[N]) {
+  uint32_t w[N / 2];
+  if constexpr (N == 8) {
+    const u32x4 t = *(const u32x4_align2 *)p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = bf16_lo(w[i]);
-      v[2 * i + 1] = bf16_hi(w[i]);
-    }
+    for (int i = 0; i < 4; ++i) w[i] = t[i];
   } else {
+    const u32x2_align2 t = *(const u32x2_align2 *)p;
+    w[0] = t[0];
+    w[1] = t[1];
+  }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_lo(p[i]) : 0.0f;
+  for (int i = 0; i < N / 2; ++i) {
+    v[2 * i] = bf16_lo(w[i]);
+    v[2 * i + 1] = bf16_hi(w[i]);
   }
 }
-__device__ __forceinline__ void load8(const float *__restrict__ p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    const f32x4 a = *(const f32x4_align4 *)p, b = *(const f32x4_align4 *)(p + 4);
+template <int N>
+__device__ __forceinline__ void load_floats(const float *__restrict__ p, float (&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = a[i];
-      v[4 + i] = b[i];
-    }
+  for (int i = 0; i < N; i += 4) {
+    const f32x4 t = *(const f32x4_align4 *)(p + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[i + j] = t[j];
+  }
+}
+__device__ __forceinline__ float load_float(const uint16_t *p) { return bf16_lo(*p); }
+__device__ __forceinline__ float load_float(const float *p) { return *p; }
+// The same of a row's end: zeros from the n-th on.
+template <int N, typename IN>
+__device__ __forceinline__ void load_floats(const IN *__restrict__ p, int n, float (&v)[N]) {
+  if (n >= N) {
+    load_floats<N>(p, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+    for (int i = 0; i < N; ++i) v[i] = i < n ? load_float(p + i) : 0.0f;
   }
 }
 

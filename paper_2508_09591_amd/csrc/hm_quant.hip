@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(RowParams 
   const int part = (int)(piece - r * p.per_row), c = part * 512 + lane * 8;
   const int64_t width = row8_bytes(p.C);
   float v[8];
-  load8((const IN *)p.x + r * p.ld + c, p.C - c, v);
+  load_floats<8>((const IN *)p.x + r * p.ld + c, p.C - c, v);
   uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) most = max(most, finite_bits(v[i]));
@@ -55,15 +55,24 @@ struct ColumnParams {
   uint8_t *q, *scale;
 };
 
-// The segment that owns block b: the last whose first block is not behind it.  Called by whole waves.
-__device__ __forceinline__ int segment_of_block8(const int32_t *__restrict__ offsets, int segments, int rows, int b) {
+// The segment that owns block b, the last whose first block is not behind it, and its rows; called by whole waves.  Both
+// offsets of a lane's segment are loaded together: what follows waits for one trip to memory.
+struct BlockOwner8 {
+  int segment;   // -1: none
+  Segment8 rows;
+};
+__device__ __forceinline__ BlockOwner8 owner_of_block8(const int32_t *__restrict__ offsets, int segments, int rows, int b) {
   const int lane = lane_id();
-  int n = 0;
+  BlockOwner8 owner = {-1, {0, 0}};
   for (int e0 = 0; e0 < segments; e0 += kWave) {
     const int e = e0 + lane;
-    n += __popcll(__ballot(e < segments && first_block8(min(max(offsets[min(e, segments - 1)], 0), rows), e) <= b));
+    const Segment8 s = segment8(offsets, min(e, segments - 1), rows);
+    const uint64_t upto = __ballot(e < segments && first_block8(s.from, e) <= b);
+    if (upto == 0) break;
+    const int l = 63 - __builtin_clzll(upto);
+    owner = {e0 + l, {read_lane(s.from, l), read_lane(s.to, l)}};
   }
-  return n - 1;
+  return owner;
 }
 
 // A workgroup takes a block of 128 rows and 64 columns: a thread eight rows of four columns, whose bytes it turns in
@@ -74,30 +83,35 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_columns_kernel(ColumnP
   __shared__ __attribute__((aligned(16))) uint8_t turned[kColumnTile * kColumnPitch];
   __shared__ uint32_t most_of[kQuantThreads / kWave][kColumnTile];
   const int b = (int)blockIdx.x;
-  const int e = segment_of_block8(p.offsets, p.segments, p.rows, b);
-  if (e < 0) return;
-  const Segment8 s = segment8(p.offsets, e, p.rows);
-  const int first = s.from + (b - first_block8(s.from, e)) * 128;
+  const BlockOwner8 owner = owner_of_block8(p.offsets, p.segments, p.rows, b);
+  if (owner.segment < 0) return;
+  const Segment8 s = owner.rows;
+  const int first = s.from + (b - first_block8(s.from, owner.segment)) * 128;
   if (first >= s.to) return;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
   const int c0 = (int)blockIdx.y * kColumnTile, cl = (tid & 15) * 4, c = c0 + cl, r0 = (tid >> 4) * 8;
   float v[8][4];
   uint32_t most[4] = {0, 0, 0, 0};
+  // rows behind the segment are read from its last and count as zeros; whole tiles without branches, so that a thread's
+  // loads are on their way together
+  const IN *from[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = first + r0 + i, n = r < s.to ? p.C - c : 0;
-    const IN *at = (const IN *)p.x + (int64_t)min(r, s.to - 1) * p.ld + c;
+  for (int i = 0; i < 8; ++i) from[i] = (const IN *)p.x + (int64_t)min(first + r0 + i, s.to - 1) * p.ld + c;
+  if (c0 + kColumnTile <= p.C) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float t = 0.0f;
-      if (j < n) {
-        if constexpr (sizeof(IN) == 2) t = bf16_lo(at[j]);
-        else t = at[j];
-      }
-      v[i][j] = t;
-      most[j] = max(most[j], finite_bits(t));
-    }
+    for (int i = 0; i < 8; ++i) load_floats<4>(from[i], v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) load_floats<4>(from[i], p.C - c, v[i]);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[i][j] = first + r0 + i < s.to ? v[i][j] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most[j] = max(most[j], finite_bits(v[i][j]));
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     most[j] = max(most[j], (uint32_t)__shfl_xor((int)most[j], 16, kWave));
@@ -143,14 +157,24 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_weights_kernel(WeightP
   const int n0 = (int)blockIdx.y * 128, c0 = (int)blockIdx.x * 128;
   const int64_t e = blockIdx.z;
   float v[8][8];
+  const IN *from[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) from[i] = (const IN *)p.w + (e * p.N + min(n0 + rl + i, p.N - 1)) * p.C + c0 + cl;
+  if (c0 + 128 <= p.C) {   // as above
+#pragma unroll
+    for (int i = 0; i < 8; ++i) load_floats<8>(from[i], v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) load_floats<8>(from[i], p.C - c0 - cl, v[i]);
+  }
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int n = n0 + rl + i;
-    load8((const IN *)p.w + (e * p.N + min(n, p.N - 1)) * p.C + c0 + cl, n < p.N ? p.C - c0 - cl : 0, v[i]);
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) most = max(most, finite_bits(v[i][j]));
-  }
+    for (int j = 0; j < 8; ++j) {
+      v[i][j] = n0 + rl + i < p.N ? v[i][j] : 0.0f;
+      most = max(most, finite_bits(v[i][j]));
+    }
   most = max16(most);
   most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
   most = max(most, (uint32_t)__shfl_xor((int)most, 32, kWave));

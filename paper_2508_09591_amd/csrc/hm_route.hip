@@ -442,42 +442,95 @@ struct WeightGradParams {
   int32_t *status;
 };
 
-// A wave takes a token and eight of its slots at a time: its gradient's row once, the eight rows beside it.
+// Eight elements as they were loaded.
 template <typename IN>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+  u32x4 w;
+  Eight() = default;
+  __device__ __forceinline__ explicit Eight(const uint16_t *p) : w(*(const u32x4_align2 *)p) {}
+  __device__ __forceinline__ float times(const Eight &v, float sum) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = fmaf(bf16_hi(w[i]), bf16_hi(v.w[i]), fmaf(bf16_lo(w[i]), bf16_lo(v.w[i]), sum));
+    return sum;
+  }
+};
+template <>
+struct Eight<float> {
+  f32x4 a, b;
+  Eight() = default;
+  __device__ __forceinline__ explicit Eight(const float *p) : a(*(const f32x4_align4 *)p), b(*(const f32x4_align4 *)(p + 4)) {}
+  __device__ __forceinline__ float times(const Eight &v, float sum) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = fmaf(b[i], v.b[i], fmaf(a[i], v.a[i], sum));
+    return sum;
+  }
+};
+
+// A wave takes a part of a token's row and eight of its slots at a time: its gradient's row once, the eight rows beside it, all
+// loads of 512 elements on their way together.  Where a row is split, the parts' sums meet in LDS.  What bounds it is
+// memory: (K + 1) rows a token.
+template <typename IN, int PARTS>
 __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(WeightGradParams p) {
-  const int lane = lane_id();
-  const int64_t t = (int64_t)blockIdx.x * kRouteWaves + threadIdx.x / kWave;
-  if (t >= p.T) return;
-  const IN *gout = (const IN *)p.gout + t * p.H;
+  __shared__ float parts[kRouteWaves][8];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), part = wave % PARTS;
+  const int64_t t = (int64_t)blockIdx.x * (kRouteWaves / PARTS) + wave / PARTS;
+  const bool there_t = t < p.T;   // the same for the waves of a token; with several parts nobody leaves before the barriers
+  if (PARTS == 1 && !there_t) return;
+  const int64_t token = there_t ? t : 0;
+  const IN *gout = (const IN *)p.gout + token * p.H;
+  constexpr int kStep = kWave * 8;
   for (int k0 = 0; k0 < p.K; k0 += 8) {
     const IN *row[8];
     bool there[8], bad = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int64_t r = k0 + j < p.K ? p.slot_row[t * p.K + k0 + j] : -1;
+      const int64_t r = k0 + j < p.K ? p.slot_row[token * p.K + k0 + j] : -1;
       there[j] = r >= 0 && r < p.y_rows;
       bad = bad || r >= p.y_rows;
-      row[j] = (const IN *)p.y + (there[j] ? r : 0) * p.H;
+      row[j] = there[j] ? (const IN *)p.y + r * p.H : gout;   // something to read in place of a row that is not there
     }
-    if (bad && lane == 0) flag(p.status, HM_ERR_CAPACITY);
+    if (bad && lane == 0 && there_t) flag(p.status, HM_ERR_CAPACITY);
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int h = lane * 8; h < p.H; h += kWave * 8) {
-      float g[8];
-      load8(gout + h, p.H - h, g);
+    int h = part * kStep + lane * 8;
+    for (int first = part * kStep; first + kStep <= p.H; first += PARTS * kStep, h += PARTS * kStep) {
+      Eight<IN> g(gout + h), v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (!there[j]) continue;
-        float v[8];
-        load8(row[j] + h, p.H - h, v);
+      for (int j = 0; j < 8; ++j)
+        if (k0 + j < p.K) v[j] = Eight<IN>(row[j] + h);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[j] = fmaf(g[i], v[i], sum[j]);
-      }
+      for (int j = 0; j < 8; ++j)
+        if (k0 + j < p.K) sum[j] = g.times(v[j], sum[j]);
     }
+    // the row's last, shorter step is the part's whose turn it is
+    if (h < p.H && h - lane * 8 < p.H && h - lane * 8 + kStep > p.H) {
+      float g[8];
+      load_floats<8>(gout + h, p.H - h, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (k0 + j < p.K) {
+          float v[8];
+          load_floats<8>(row[j] + h, p.H - h, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[j] = fmaf(g[i], v[i], sum[j]);
+        }
+    }
+    float mine = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float s = wave_sum(sum[j]);
-      if (lane == j && k0 + j < p.K) p.grad[t * p.K + k0 + j] = s;
+      mine = lane == j && there[j] ? s : mine;
     }
+    if (PARTS > 1) {
+      if (lane < 8) parts[wave][lane] = mine;
+      __syncthreads();
+      mine = 0.0f;
+      if (lane < 8)
+        for (int w = 0; w < PARTS; ++w) mine += parts[wave - part + w][lane];
+      __syncthreads();
+    }
+    if (part == 0 && there_t && lane < 8 && k0 + lane < p.K) p.grad[token * p.K + k0 + lane] = mine;
   }
 }
 
@@ -569,7 +622,10 @@ extern "C" hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_
   if (T == 0) return HM_OK;
   if (!gout || !grad_weights || (!y && y_rows > 0)) return HM_ERR_NULL;
   const WeightGradParams p = {gout, y, y_rows, plan->slot_row, T, K, H, grad_weights, plan->status};
-  const auto kernel = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t> : combine_weight_grad_kernel<float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((T + kRouteWaves - 1) / kRouteWaves)), dim3(kRouteThreads), 0, (hipStream_t)hip_stream, p);
+  // a token's row in four parts where there are few tokens
+  const int parts = T <= 4096 && H > 512 ? kRouteWaves : 1, tokens = kRouteWaves / parts;
+  const auto whole = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, 1> : combine_weight_grad_kernel<float, 1>;
+  const auto split = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, kRouteWaves> : combine_weight_grad_kernel<float, kRouteWaves>;
+  hipLaunchKernelGGL((parts == 1 ? whole : split), dim3((unsigned)((T + tokens - 1) / tokens)), dim3(kRouteThreads), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
