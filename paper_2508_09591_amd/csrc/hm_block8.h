@@ -36,16 +36,28 @@ __device__ __forceinline__ int scale_code8(uint32_t amax_bits) {
 // 2^(127 - code): what a block's values are multiplied by; normal for every code that scale_code8 gives.
 __device__ __forceinline__ float inverse_scale8(int code) { return __builtin_bit_cast(float, (uint32_t)(254 - code) << 23); }
 
-// Bits to count for a block's largest value: NaN and infinities as 0.
-__device__ __forceinline__ uint32_t finite_bits(float v) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
-  return b < kInfinityBits ? b : 0u;
+// Largest magnitude among a thread's values of a block, as bits: those order as the magnitudes do.  NaN and infinities, which
+// are seen by bits that are too large, do not count and become NaN.
+template <int N>
+__device__ __forceinline__ uint32_t largest_bits(float (&v)[N]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) most = max(most, __builtin_bit_cast(uint32_t, v[i]) & 0x7FFFFFFFu);
+  if (most >= kInfinityBits) {
+    most = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t bits = __builtin_bit_cast(uint32_t, v[i]) & 0x7FFFFFFFu;
+      if (bits >= kInfinityBits) v[i] = __builtin_nanf("");
+      else most = max(most, bits);
+    }
+  }
+  return most;
 }
-// Four values times a power of two, rounded to nearest even, in order; an infinity becomes NaN.
+// Four values times a power of two, rounded to nearest even, in order.
 __device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d, float by) {
-  auto scaled = [by](float v) { return finite_bits(v) == 0 && v != 0.0f ? __builtin_nanf("") : v * by; };
-  const int low = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(a), scaled(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(scaled(c), scaled(d), low, true);
+  const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a * by, b * by, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * by, d * by, low, true);
 }
 
 typedef f32x4 f32x4_align4 __attribute__((aligned(4)));
@@ -80,15 +92,23 @@ __device__ __forceinline__ void load_floats(const float *__restrict__ p, float (
 }
 __device__ __forceinline__ float load_float(const uint16_t *p) { return bf16_lo(*p); }
 __device__ __forceinline__ float load_float(const float *p) { return *p; }
-// The same of a row's end: zeros from the n-th on.
+// Elements c to c + N - 1 of a row of C, zeros behind its end.  A vector that would pass the end is loaded from before it and
+// moved down: loads one by one, each waited for, cost a kernel's tail 10 us.
 template <int N, typename IN>
-__device__ __forceinline__ void load_floats(const IN *__restrict__ p, int n, float (&v)[N]) {
-  if (n >= N) {
-    load_floats<N>(p, v);
-  } else {
+__device__ __forceinline__ void load_row_end(const IN *__restrict__ row, int c, int C, float (&v)[N]) {
+  if (C < N) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i < n ? load_float(p + i) : 0.0f;
+    for (int i = 0; i < N; ++i) v[i] = c + i < C ? load_float(row + c + i) : 0.0f;
+    return;
   }
+  const int at = min(c, C - N), by = c - at;
+  load_floats<N>(row + at, v);
+#pragma unroll
+  for (int bit = 1; bit < N; bit *= 2)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = by & bit ? (i + bit < N ? v[i + bit] : 0.0f) : v[i];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = by < N ? v[i] : 0.0f;
 }
 
 static inline bool buffers8_aligned(const void *q, const void *scale) { return ((uintptr_t)q & 15) == 0 && ((uintptr_t)scale & 3) == 0; }

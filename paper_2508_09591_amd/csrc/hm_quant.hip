@@ -30,11 +30,10 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(RowParams 
   const int part = (int)(piece - r * p.per_row), c = part * 512 + lane * 8;
   const int64_t width = row8_bytes(p.C);
   float v[8];
-  load_floats<8>((const IN *)p.x + r * p.ld + c, p.C - c, v);
-  uint32_t most = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) most = max(most, finite_bits(v[i]));
-  most = max16(most);
+  const IN *row = (const IN *)p.x + r * p.ld;
+  if (part * 512 + 512 <= p.C) load_floats<8>(row + c, v);   // the whole wave
+  else load_row_end<8>(row, c, p.C, v);
+  const uint32_t most = max16(largest_bits(v));
   const int code = scale_code8(most);
   const float by = inverse_scale8(code);
   if (c < width) {
@@ -51,7 +50,7 @@ struct ColumnParams {
   const void *x;
   int64_t ld;
   const int32_t *offsets;
-  int32_t segments, rows, C;
+  int32_t segments, rows, C, blocks, tiles;   // blocks of rows; tiles of columns
   uint8_t *q, *scale;
 };
 
@@ -82,36 +81,37 @@ template <typename IN>
 __global__ __launch_bounds__(kQuantThreads) void quantize_columns_kernel(ColumnParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[kColumnTile * kColumnPitch];
   __shared__ uint32_t most_of[kQuantThreads / kWave][kColumnTile];
-  const int b = (int)blockIdx.x;
+  // a die gets neighbouring tiles: they share the lines that rows off a line's alignment have in common
+  const int64_t per_die = ((int64_t)p.blocks * p.tiles + 7) / 8, at = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
+  if ((int64_t)(blockIdx.x >> 3) >= per_die || at >= (int64_t)p.blocks * p.tiles) return;
+  const int b = (int)(at / p.tiles);
   const BlockOwner8 owner = owner_of_block8(p.offsets, p.segments, p.rows, b);
   if (owner.segment < 0) return;
   const Segment8 s = owner.rows;
   const int first = s.from + (b - first_block8(s.from, owner.segment)) * 128;
   if (first >= s.to) return;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
-  const int c0 = (int)blockIdx.y * kColumnTile, cl = (tid & 15) * 4, c = c0 + cl, r0 = (tid >> 4) * 8;
-  float v[8][4];
-  uint32_t most[4] = {0, 0, 0, 0};
+  const int c0 = (int)(at - (int64_t)b * p.tiles) * kColumnTile, cl = (tid & 15) * 4, c = c0 + cl, r0 = (tid >> 4) * 8;
+  float v[8][4], column[4][8];
+  uint32_t most[4];
   // rows behind the segment are read from its last and count as zeros; whole tiles without branches, so that a thread's
   // loads are on their way together
   const IN *from[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) from[i] = (const IN *)p.x + (int64_t)min(first + r0 + i, s.to - 1) * p.ld + c;
+  for (int i = 0; i < 8; ++i) from[i] = (const IN *)p.x + (int64_t)min(first + r0 + i, s.to - 1) * p.ld;
   if (c0 + kColumnTile <= p.C) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load_floats<4>(from[i], v[i]);
+    for (int i = 0; i < 8; ++i) load_floats<4>(from[i] + c, v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load_floats<4>(from[i], p.C - c, v[i]);
+    for (int i = 0; i < 8; ++i) load_row_end<4>(from[i], c, p.C, v[i]);
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int j = 0; j < 4; ++j) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[i][j] = first + r0 + i < s.to ? v[i][j] : 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) most[j] = max(most[j], finite_bits(v[i][j]));
+    for (int i = 0; i < 8; ++i) column[j][i] = first + r0 + i < s.to ? v[i][j] : 0.0f;
+    most[j] = largest_bits(column[j]);
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     most[j] = max(most[j], (uint32_t)__shfl_xor((int)most[j], 16, kWave));
@@ -128,7 +128,8 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_columns_kernel(ColumnP
     const int code = scale_code8(m);
     by[j] = inverse_scale8(code);
     if (tid < 16 && c + j < p.C) p.scale[(int64_t)b * p.C + c + j] = (uint8_t)code;
-    const uint64_t out = (uint64_t)pack8(v[4][j], v[5][j], v[6][j], v[7][j], by[j]) << 32 | pack8(v[0][j], v[1][j], v[2][j], v[3][j], by[j]);
+    const float (&u)[8] = column[j];
+    const uint64_t out = (uint64_t)pack8(u[4], u[5], u[6], u[7], by[j]) << 32 | pack8(u[0], u[1], u[2], u[3], by[j]);
     *(uint64_t *)(turned + (cl + j) * kColumnPitch + r0) = out;
   }
   __syncthreads();
@@ -159,22 +160,21 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_weights_kernel(WeightP
   float v[8][8];
   const IN *from[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) from[i] = (const IN *)p.w + (e * p.N + min(n0 + rl + i, p.N - 1)) * p.C + c0 + cl;
+  for (int i = 0; i < 8; ++i) from[i] = (const IN *)p.w + (e * p.N + min(n0 + rl + i, p.N - 1)) * p.C;
   if (c0 + 128 <= p.C) {   // as above
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load_floats<8>(from[i], v[i]);
+    for (int i = 0; i < 8; ++i) load_floats<8>(from[i] + c0 + cl, v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load_floats<8>(from[i], p.C - c0 - cl, v[i]);
+    for (int i = 0; i < 8; ++i) load_row_end<8>(from[i], c0 + cl, p.C, v[i]);
   }
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 8; ++i) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[i][j] = n0 + rl + i < p.N ? v[i][j] : 0.0f;
-      most = max(most, finite_bits(v[i][j]));
-    }
+    for (int j = 0; j < 8; ++j) v[i][j] = n0 + rl + i < p.N ? v[i][j] : 0.0f;
+    most = max(most, largest_bits(v[i]));
+  }
   most = max16(most);
   most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
   most = max(most, (uint32_t)__shfl_xor((int)most, 32, kWave));
@@ -262,8 +262,11 @@ extern "C" hm_status hm_quantize_columns(const void *x, hm_dtype dtype, int64_t 
   p.q = q;
   p.scale = scale;
   const auto kernel = dtype == HM_BF16 ? quantize_columns_kernel<uint16_t> : quantize_columns_kernel<float>;
-  const dim3 grid((unsigned)column8_blocks(rows, segments), (unsigned)((C + kColumnTile - 1) / kColumnTile));
-  hipLaunchKernelGGL(kernel, grid, dim3(kQuantThreads), 0, (hipStream_t)hip_stream, p);
+  p.blocks = (int32_t)column8_blocks(rows, segments);
+  p.tiles = (C + kColumnTile - 1) / kColumnTile;
+  const int64_t workgroups = ((int64_t)p.blocks * p.tiles + 7) / 8 * 8;
+  if (workgroups > (1 << 23)) return HM_ERR_SHAPE;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)workgroups), dim3(kQuantThreads), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
 

@@ -450,6 +450,7 @@ struct Eight<uint16_t> {
   u32x4 w;
   Eight() = default;
   __device__ __forceinline__ explicit Eight(const uint16_t *p) : w(*(const u32x4_align2 *)p) {}
+  __device__ __forceinline__ float at(int i) const { return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
   __device__ __forceinline__ float times(const Eight &v, float sum) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum = fmaf(bf16_hi(w[i]), bf16_hi(v.w[i]), fmaf(bf16_lo(w[i]), bf16_lo(v.w[i]), sum));
@@ -461,6 +462,7 @@ struct Eight<float> {
   f32x4 a, b;
   Eight() = default;
   __device__ __forceinline__ explicit Eight(const float *p) : a(*(const f32x4_align4 *)p), b(*(const f32x4_align4 *)(p + 4)) {}
+  __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
   __device__ __forceinline__ float times(const Eight &v, float sum) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum = fmaf(b[i], v.b[i], fmaf(a[i], v.a[i], sum));
@@ -503,18 +505,32 @@ __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(Weig
       for (int j = 0; j < 8; ++j)
         if (k0 + j < p.K) sum[j] = g.times(v[j], sum[j]);
     }
-    // the row's last, shorter step is the part's whose turn it is
-    if (h < p.H && h - lane * 8 < p.H && h - lane * 8 + kStep > p.H) {
-      float g[8];
-      load_floats<8>(gout + h, p.H - h, g);
+    // The row's last, shorter step is the part's whose turn it is: vectors that would pass the end lie before it, and what
+    // the vector before them has had counts as zero.
+    const int begin = h - lane * 8;
+    if (begin < p.H && begin + kStep > p.H) {
+      if (p.H >= 8) {
+        if (h < p.H) {
+          const int at = min(h, p.H - 8), had = h - at;
+          float g[8];
+          load_floats<8>(gout + at, g);
+          Eight<IN> v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (k0 + j < p.K) {
-          float v[8];
-          load_floats<8>(row[j] + h, p.H - h, v);
+          for (int j = 0; j < 8; ++j)
+            if (k0 + j < p.K) v[j] = Eight<IN>(row[j] + at);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum[j] = fmaf(g[i], v[i], sum[j]);
+          for (int j = 0; j < 8; ++j)
+            if (k0 + j < p.K) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) sum[j] = i < had ? sum[j] : fmaf(g[i], v[j].at(i), sum[j]);
+            }
         }
+      } else if (lane < p.H) {
+        const float g = load_float(gout + lane);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k0 + j < p.K) sum[j] = fmaf(g, load_float(row[j] + lane), sum[j]);
+      }
     }
     float mine = 0.0f;
 #pragma unroll
