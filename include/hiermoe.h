@@ -504,7 +504,7 @@ hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype
  * are data errors: no access leaves the buffers, the results are unspecified.
  *
  * x: dtype HM_F32 or HM_BF16, row r from element r*ld on, any alignment of the elements; fastest with whole 16-byte
- * vectors.  hm_quantize_weights takes dense [experts, N, C]; with qt and scale_t it also writes the transposed weights
+ * vectors; calls of more than about 2^34 values are refused (HM_ERR_SHAPE).  hm_quantize_weights takes dense [experts, N, C]; with qt and scale_t it also writes the transposed weights
  * [experts, C, up(N,128)], [experts, ceil(C/128), up(N,512)/128]: the same values, for the gradient of the rows.
  */
 hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld, int64_t rows, int32_t C, uint8_t *q, uint8_t *scale,

@@ -359,6 +359,78 @@ __global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product
   }
 }
 
+// ---- few rows ------------------------------------------------------------------------------------------
+// The weights are all there is to read, once: 16 of their rows a workgroup, straight from memory into the operands of
+// products of 16 x 16 x 128, no LDS between; its four waves take every fourth group of four steps (512 bytes of a row, four codes of
+// scale) and add up in LDS.  A lane has row l % 16 of the weights and of the segment, bytes 32 (l / 16) to 32 (l / 16) + 31 of a
+// step.
+constexpr int kThinWaves = 4, kGroupSteps = 4;
+template <typename OUT>
+__global__ __launch_bounds__(kThinWaves * kWave) void thin_product_kernel(ProductParams p) {
+  constexpr bool kFull = sizeof(OUT) == 4;
+  __shared__ f32x4 sums[kThinWaves][kWave];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Tile t = tile_of_rows<16, 16>(p);
+  if (t.q0 >= t.q_end) return;
+  const int steps = (int)blocks8(p.H), groups = (steps + kGroupSteps - 1) / kGroupSteps;
+  const int64_t pitch = row8_bytes(p.H), scale_pitch = scale8_bytes(p.H);
+  const int row = min(t.q0 + (lane & 15), t.q_end - 1), col = min(t.p0 + (lane & 15), p.N - 1);
+  const uint8_t *q = p.q + (int64_t)row * pitch + (lane >> 4) * 32, *w = p.p + ((int64_t)t.expert * p.N + col) * pitch + (lane >> 4) * 32;
+  const uint8_t *sq = p.q_scale + (int64_t)row * scale_pitch, *sp = p.p_scale + ((int64_t)t.expert * blocks8(p.N) + t.p0 / 128) * scale_pitch;
+  struct Group {
+    i32x8 q[kGroupSteps], w[kGroupSteps];
+    uint32_t sq, sp;
+  };
+  auto load = [&](Group &g, int group) {   // steps behind the last are the last: their products are left out
+#pragma unroll
+    for (int s = 0; s < kGroupSteps; ++s) {
+      const int64_t at = (int64_t)min(group * kGroupSteps + s, steps - 1) * 128;
+      __builtin_memcpy(&g.w[s], __builtin_assume_aligned(w + at, 16), 32);
+      __builtin_memcpy(&g.q[s], __builtin_assume_aligned(q + at, 16), 32);
+    }
+    g.sq = *(const uint32_t *)(sq + group * kGroupSteps);
+    g.sp = *(const uint32_t *)(sp + group * kGroupSteps);
+  };
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  auto multiply = [&](const Group &g, int group) {
+#pragma unroll
+    for (int s = 0; s < kGroupSteps; ++s) {
+      if (group * kGroupSteps + s >= steps) break;
+      if constexpr (kFull) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Slice<true>::widen(g.w[s][2 * i], g.w[s][2 * i + 1], g.sp >> 8 * s),
+                                                        Slice<true>::widen(g.q[s][2 * i], g.q[s][2 * i + 1], g.sq >> 8 * s), acc, 0, 0, 0);
+      } else {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(g.w[s], g.q[s], acc, 0, 0, 0, (int)(g.sp >> 8 * s), 0, (int)(g.sq >> 8 * s));
+      }
+    }
+  };
+  Group a, b;   // one on its way while the other is multiplied
+  int group = wave;
+  if (group < groups) load(a, group);
+  for (; group < groups; group += 2 * kThinWaves) {
+    if (group + kThinWaves < groups) load(b, group + kThinWaves);
+    multiply(a, group);
+    if (group + kThinWaves < groups) {
+      if (group + 2 * kThinWaves < groups) load(a, group + 2 * kThinWaves);
+      multiply(b, group + kThinWaves);
+    }
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  // thread: row / 16, column % 16 of the tile; lane l had row l % 16 and columns 4 (l / 16) to 4 (l / 16) + 3
+  const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
+  float sum = 0.0f;
+#pragma unroll
+  for (int v = 0; v < kThinWaves; ++v) sum += ((const float *)&sums[v][(c >> 2) * 16 + r])[c & 3];
+  if (t.q0 + r < t.q_end && t.p0 + c < p.N) {
+    OUT *out = (OUT *)p.out + (int64_t)(t.q0 + r) * p.N + t.p0 + c;
+    if constexpr (kFull) *out = sum;
+    else *out = (OUT)f32_to_bf16(sum);
+  }
+}
+
 static hm_status check_products(const void *a, const void *as, const void *b, const void *bs, const int32_t *offsets, int32_t experts, int64_t rows,
                                 int32_t N, int32_t H, const void *out, hm_dtype dtype, bool none) {
   if (!dtype_known(dtype) || !segments8_ok(experts, rows) || N < 1 || N > kMostColumns8 || H < 1 || H > kMostColumns8) return HM_ERR_SHAPE;
@@ -403,6 +475,13 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   if (bad != HM_OK) return bad;
   if (rows == 0) return HM_OK;
   const ProductParams p = {x, x_scale, w, w_scale, offsets, experts, (int32_t)rows, N, H, out};
+  if (rows < 16LL * experts) {
+    const int64_t tiles = (rows / 16 + (rows < experts ? rows : experts)) * ((N + 15) / 16) + 8;
+    if (tiles > (1 << 23)) return HM_ERR_SHAPE;
+    const auto kernel = out_dtype == HM_BF16 ? thin_product_kernel<uint16_t> : thin_product_kernel<float>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(kThinWaves * kWave), 0, (hipStream_t)hip_stream, p);
+    return hm_launch_status();
+  }
   const bool large = out_dtype == HM_BF16 && rows / experts >= 512 && (rows / 256 + experts / 2) * ((N + 255) / 256) >= 400;
   const int side = tile_side(large, (rows / 128 + experts / 2) * ((N + 127) / 128));
   const int64_t tiles = (rows / side + experts) * ((N + side - 1) / side) + 8;

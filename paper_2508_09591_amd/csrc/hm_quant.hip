@@ -238,7 +238,7 @@ extern "C" hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld,
   p.q = q;
   p.scale = scale;
   const int64_t blocks = (p.pieces + kQuantThreads / kWave - 1) / (kQuantThreads / kWave);
-  if (blocks > 2147483647LL) return HM_ERR_SHAPE;
+  if (blocks > (1 << 23)) return HM_ERR_SHAPE;
   const auto kernel = dtype == HM_BF16 ? quantize_rows_kernel<uint16_t> : quantize_rows_kernel<float>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
