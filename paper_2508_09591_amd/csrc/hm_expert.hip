@@ -475,7 +475,9 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   if (bad != HM_OK) return bad;
   if (rows == 0) return HM_OK;
   const ProductParams p = {x, x_scale, w, w_scale, offsets, experts, (int32_t)rows, N, H, out};
-  if (rows < 16LL * experts) {
+  // Few rows: up to four an expert, or a strip's 16 in all (us, thin against tiles: 32 experts of 4,096 x 7,168, 32 rows 93 and 128,
+  // 128 rows 164 and 162, 512 rows 292 and 164; one expert, 16 rows 9.1 and 14.1, 40 rows 20.4 and 14.3).
+  if (rows <= 4LL * experts || rows <= 16) {
     const int64_t tiles = (rows / 16 + (rows < experts ? rows : experts)) * ((N + 15) / 16) + 8;
     if (tiles > (1 << 23)) return HM_ERR_SHAPE;
     const auto kernel = out_dtype == HM_BF16 ? thin_product_kernel<uint16_t> : thin_product_kernel<float>;

@@ -33,11 +33,17 @@ __device__ __forceinline__ float reciprocal(float y) {   // of y >= 1
 }
 __device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + expf(-x)); }
 
+// Over all lanes, the result in each: within rows of sixteen by rotations, then the four rows.
 template <typename OP>
 __device__ __forceinline__ float wave_all(float v, OP op) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v = op(v, __shfl_xor(v, d, kWave));
-  return v;
+  auto turned = [](float x, auto control) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), control(), 0xF, 0xF, true));
+  };
+  v = op(v, turned(v, std::integral_constant<int, 0x128>()));
+  v = op(v, turned(v, std::integral_constant<int, 0x124>()));
+  v = op(v, turned(v, std::integral_constant<int, 0x122>()));
+  v = op(v, turned(v, std::integral_constant<int, 0x121>()));
+  return op(op(read_lane(v, 0), read_lane(v, 16)), op(read_lane(v, 32), read_lane(v, 48)));
 }
 __device__ __forceinline__ float wave_max(float v) { return wave_all(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float wave_sum(float v) { return wave_all(v, [](float a, float b) { return a + b; }); }
