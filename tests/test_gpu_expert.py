@@ -302,6 +302,128 @@ def test_a_layer_of_products_and_their_gradients(rows, E, N, H):
         assert near(dw[e].double().cpu().numpy(), gy[r].double().cpu().numpy().T @ x[r].double().cpu().numpy(), 0.1)
 
 
+def gpu_values(q, power):
+    """[rows, k] values in 64 bits of operands [rows, k] and codes [rows, blocks]."""
+    p = torch.ldexp(torch.ones((), dtype=torch.float64), power.cpu().int() - 127).cuda()   # exact on the host
+    return (q.double().view(q.shape[0], -1, 128) * p[:, :, None]).view(q.shape[0], -1)
+
+
+def same_in_every_patch(got, a, b, dtype):
+    """The 2-norm of the error of a b^T in each 32 x 32 patch.  bf16: rounding is at most 2^-9 of a value, and of the 64 products
+    of a step each may lose 2^-13 of the largest, which is no more than the largest of either block's values multiplied: twice
+    64 * 2^-13 of that a block.  fp32: sums of some thousand terms in 32 bits, below 1e-5 of the patch."""
+    want = a @ b.t().contiguous()
+    R, C = got.shape
+    cut = lambda t: torch.nn.functional.pad(t.double(), (0, -C % 32, 0, -R % 32)).view(-(-R // 32), 32, -(-C // 32), 32).square().sum(dim=(1, 3)).sqrt()
+    most = lambda t: t.abs().view(t.shape[0], -1, 128).amax(dim=2)
+    off, size = cut(got.double() - want), cut(want)
+    bound = 2.0 ** -9 * size + 2.0 ** -6 * cut(most(a) @ most(b).t().contiguous()) if dtype == torch.bfloat16 else 1e-5 * size
+    assert (off <= bound + 1e-30).all(), float((off / (bound + 1e-30)).max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("H", [1, 129, 384, 512, 600, 1024, 1400])
+@pytest.mark.parametrize("rows,E,N", [(2000, 5, 1500), (8300, 8, 2900), (2100, 1, 1541)])
+def test_many_rows(rows, E, N, H, dtype):
+    """Sizes whose tiles are large, with as many steps as end inside, at and behind a group of four; odd N cannot be stored in vectors."""
+    rng = np.random.default_rng(rows + H)
+    cuts = np.sort(rng.integers(0, rows - 3, E - 1)) if E > 1 else np.zeros(0, dtype=np.int64)
+    if E > 5:
+        cuts[2] = cuts[1]   # an expert without rows
+    off = np.concatenate([[0], cuts, [rows - 3]]).astype(np.int32)   # three rows at the end are nobody's
+    W = R.up(H, 128)
+    x, w = operand(rng, rows, W), operand(rng, E, N, W)
+    x[:, H:], w[:, :, H:] = 0, 0
+    x, w = f8(x).cuda(), f8(w).cuda()
+    xs = dev(rng.integers(120, 135, (rows, R.up(H, 512) // 128), dtype=np.uint8))
+    ws = dev(rng.integers(115, 130, (E, R.up(N, 128) // 128, R.up(H, 512) // 128), dtype=np.uint8))
+    out = torch.full((rows, N), -77.0, dtype=dtype, device="cuda")
+    B.hm_expert_matmul(x, xs, w, ws, dev(off), out)
+    a = gpu_values(x, xs[:, :W // 128])
+    assert (out[rows - 3:] == -77).all()
+    for e in range(E):
+        r = slice(off[e], off[e + 1])
+        if off[e] < off[e + 1]:
+            b = gpu_values(w[e], ws[e].repeat_interleave(128, dim=0)[:N, :W // 128])
+            same_in_every_patch(out[r], a[r], b, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("counts,N,H", [([700, 0, 129, 1500], 2100, 2000), ([300, 1, 250], 1000, 1541), ([128 * 11], 2050, 1030), ([5, 600], 4100, 3900)])
+def test_weights_gradient_of_many(counts, N, H, dtype):
+    rng = np.random.default_rng(N)
+    off, E = offsets_of(counts), len(counts)
+    rows = int(off[-1])
+    blocks = rows // 128 + E
+    gy, x = operand(rng, N, 128 * blocks), operand(rng, H, 128 * blocks)
+    for e in range(E):
+        first = 128 * (off[e] // 128 + e)
+        for q in (gy, x):
+            q[:, first + counts[e]:first + R.up(counts[e], 128)] = 0
+    gy, x = f8(gy).cuda(), f8(x).cuda()
+    gs, xs = dev(rng.integers(120, 135, (blocks, N), dtype=np.uint8)), dev(rng.integers(115, 130, (blocks, H), dtype=np.uint8))
+    dw = torch.full((E, N, H), -77.0, dtype=dtype, device="cuda")
+    B.hm_expert_matmul_dw(gy, gs, x, xs, dev(off), rows, dw)
+    a, b = gpu_values(gy, gs.t()), gpu_values(x, xs.t())
+    for e in range(E):
+        first = 128 * (off[e] // 128 + e)
+        k = slice(first, first + R.up(counts[e], 128))
+        if counts[e] == 0:
+            assert not dw[e].any()
+            continue
+        same_in_every_patch(dw[e], a[:, k].contiguous(), b[:, k].contiguous(), dtype)
+
+
+def test_every_call_is_taken_by_the_native_half(monkeypatch):
+    """Dense tensors on the current stream do not go through ctypes; what is out of the ordinary does, with the same result."""
+    B.lib()
+
+    class Recorder:
+        calls = []
+
+        def __getattr__(self, name):
+            def call(*args):
+                rc = getattr(native, name)(*args)
+                self.calls.append((name, rc is not None))
+                return rc
+            return call
+
+    native, rec = B._native, Recorder()
+    monkeypatch.setattr(B, "_native", rec)
+    T, E, K, H, N = 40, 16, 4, 96, 72
+    router = B.Router(E, K)
+    logits, ids, w = torch.randn((T, E), device="cuda"), torch.empty((T, K), dtype=torch.int32, device="cuda"), torch.empty((T, K), device="cuda")
+    plan = B.alloc_plan(T, K, E, 1, 1, B.HM_DEDUP_NONE, num_dest=E)
+    B.hm_route(logits, router, ids, w)
+    B.hm_plan_mapped(ids, w, torch.arange(E, dtype=torch.int32, device="cuda"), E, False, plan=plan)
+    off, rows = plan.dest_offset, T * K
+    x, y, gout, master = (torch.randn(s, device="cuda") for s in ((rows, H), (rows, N), (T, N), (E, N, H)))
+    both = {}
+    for stream in (None, torch.cuda.current_stream()):
+        x8, xt, yt = B.alloc_rows8(rows, H), B.alloc_columns8(rows, E, H), B.alloc_columns8(rows, E, N)
+        w8, wt = B.alloc_weights8(E, N, H), B.alloc_weights8(E, H, N)
+        for t in (*xt, *yt):
+            t.view(torch.uint8).zero_()
+        out, dw, gw, gl = torch.empty((rows, N), device="cuda"), torch.empty((E, N, H), device="cuda"), torch.empty((T, K), device="cuda"), torch.empty((T, E), device="cuda")
+        rec.calls.clear()
+        B.hm_route(logits, router, ids, w, stream=stream)
+        B.hm_quantize_rows(x, *x8, stream=stream)
+        B.hm_quantize_columns(x, off, *xt, stream=stream)
+        B.hm_quantize_columns(y, off, *yt, stream=stream)
+        B.hm_quantize_weights(master, *w8, *wt, stream=stream)
+        B.hm_expert_matmul(*x8, *w8, off, out, stream=stream)
+        B.hm_expert_matmul_dw(*yt, *xt, off, rows, dw, stream=stream)
+        B.hm_combine_weight_grad(gout, y, plan, gw, stream=stream)
+        B.hm_route_backward(logits, router, ids, gw, gl, stream=stream)
+        both[stream] = [t.clone().view(torch.uint8) for t in (ids, w, *x8, *xt, *w8, *wt, out, dw, gw, gl)]
+        if stream is None:
+            assert len(rec.calls) == 9 and all(taken for _, taken in rec.calls), rec.calls
+            assert {"hm_" + name for name, _ in rec.calls} == set(B._NATIVE_LAYER)
+        else:
+            assert not rec.calls
+    assert all(torch.equal(a, b) for a, b in zip(*both.values()))
+
+
 def test_results_do_not_depend_on_what_ran_before():
     """The same call into poisoned outputs: the same bits."""
     rng = np.random.default_rng(8)
