@@ -527,7 +527,8 @@ hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, in
  * hm_expert_matmul_dw -- the gradient of the weights:
  *     dw[e,n,h] = sum over the rows r of segment e of gy[r,n] x[r,h],
  * gy (C = N) and x (C = H) in the layout `columns`; dw [experts,N,H] of dw_dtype, zeros for an expert without rows.
- * Limits: experts <= 1024, rows <= 2^31-1 - 128 * experts (dw: rows / 128 + experts < 2^17), N and H up to 2^20.
+ * Limits: experts <= 1024, N and H up to 2^20, rows * experts < 2^35 and rows <= 2^31-1 - 128 * experts, about 2^37 results (dw:
+ * rows / 128 + experts < 2^17); beyond HM_ERR_SHAPE.
  */
 hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, const uint8_t *w, const uint8_t *w_scale,
                            const int32_t *offsets, int32_t experts, int64_t rows, int32_t N, int32_t H, void *out,

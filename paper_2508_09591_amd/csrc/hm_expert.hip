@@ -195,7 +195,7 @@ __global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product
 #pragma unroll
   for (int i = 0; i < FP; ++i) {
     const int r = min((wp * FP + i) * 32 + (lane & 31), p_rows - 1 - t.p0);
-    from_sp[i] = DW ? (uint32_t)r : (uint32_t)(r / 128) * (uint32_t)scale_pitch;   // t.p0 is a multiple of 128
+    from_sp[i] = DW ? (uint32_t)r : (uint32_t)(r / 128) * (uint32_t)scale_pitch;   // the tile begins with a block, or one of 64 lies inside one
   }
   auto load_scales = [&](int k) {
     const uint8_t *sq = p.q_scale + (DW ? (int64_t)(block0 + k) * p.N + t.q0 : (int64_t)t.q0 * scale_pitch + k);
@@ -249,14 +249,16 @@ __global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product
   };
   constexpr int kBefore = kAhead * 2 * kLoads / kItems;   // loads due in the items before a turn of the ring
   static_assert(kAhead * 2 * kLoads % kItems == 0 && kAhead <= kItems / 2, "whole loads, all of them P's");
-  if (steps > 0) {
+  if (steps > 0) {   // arrived() counts the loads behind those that are needed, so their order is the program's
     load_scales(0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_q(0, 0, i);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_p(kUnitBytes, 0, i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_q(2 * kUnitBytes, 1, i);
+    __builtin_amdgcn_sched_barrier(0);
     fill(0, kAhead, 1);
     arrived<kLoads + kBefore>();
 #pragma unroll
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product
       read((item + kAhead) % kItems);
 #pragma unroll
       for (int j = 0; j < FP; ++j) other[j].times(mine, scale_of_p[j], scale_of_q[item % FQ], acc[item % FQ][j]);
-      __builtin_amdgcn_sched_barrier(0);   // else the compiler reads all items at once and runs out of registers
+      __builtin_amdgcn_sched_barrier(0);   // keeps the loads' order; and else the compiler reads all items at once and runs out of registers
     }
   };
   constexpr int kScaled = DW ? 1 : 4;   // steps whose codes are loaded together, as long before their use
@@ -476,6 +478,7 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   const hm_status bad = check_products(x, x_scale, w, w_scale, offsets, experts, rows, N, H, out, out_dtype, rows == 0);
   if (bad != HM_OK) return bad;
   if (rows == 0) return HM_OK;
+  if (rows * experts >= 1LL << 35) return HM_ERR_SHAPE;   // strips of 16 rows are counted in 32 bits, also where offsets overlap
   const ProductParams p = {x, x_scale, w, w_scale, offsets, experts, (int32_t)rows, N, H, out};
   // Few rows: up to four an expert, or a strip's 16 in all (us, thin against tiles: 32 experts of 4,096 x 7,168, 32 rows 93 and 128,
   // 128 rows 164 and 162, 512 rows 292 and 164; one expert, 16 rows 9.1 and 14.1, 40 rows 20.4 and 14.3).

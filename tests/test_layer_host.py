@@ -94,6 +94,9 @@ def test_products_check_their_arguments():
                     dict(out=P(0x1002), dtype=B.HM_F32)):
             assert call(**bad) == B.HM_ERR_SHAPE, bad
     assert L.hm_expert_matmul(P(), P(), P(), P(), P(), 2, 0, 8, 16, P(), 0, None) == B.HM_OK
+    assert L.hm_expert_matmul(P(), P(), P(), P(), P(), 1024, 1 << 25, 8, 16, P(), 0, None) == B.HM_ERR_SHAPE
+    assert L.hm_expert_matmul(P(), P(), P(), P(), P(), 1, 1 << 30, 1 << 20, 16, P(), 0, None) == B.HM_ERR_SHAPE
+    assert L.hm_expert_matmul_dw(P(), P(), P(), P(), P(), 1, 1 << 24, 8, 16, P(), 0, None) == B.HM_ERR_SHAPE
 
 
 def test_the_binding_refuses_tensors_it_cannot_use():
