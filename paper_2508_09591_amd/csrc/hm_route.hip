@@ -153,9 +153,20 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteParams p) {
 // of a double, whose order is that of the floats (a float's bits with anything behind them are a finite double, -inf's and +inf's
 // too), and the low word puts the lower of two equal experts first.  The largest and the smaller of two are one
 // instruction each.
-__device__ __forceinline__ double key_of(float choice, int e) {
-  const int32_t high = __builtin_bit_cast(int32_t, choice + 0.0f);   // -0 is 0
-  return __builtin_bit_cast(double, (uint64_t)(uint32_t)high << 32 | (uint32_t)(high < 0 ? e : ~e));
+__device__ __forceinline__ double key_of(int32_t high, int e) {
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)high << 32 | (uint32_t)(~e ^ (high >> 31)));
+}
+constexpr int32_t kNoneBits = (int32_t)0xFF800000u;   // -inf
+// Of a logit: NaN and -inf are none, +inf the largest number, -0 is 0.
+__device__ __forceinline__ double key_of_logit(float x, int e) {
+  const int32_t high = min(__builtin_bit_cast(int32_t, x + 0.0f), 0x7F7FFFFF);
+  return key_of(x > kNone() ? high : kNoneBits, e);
+}
+// Of a logistic score and a bias: none where the logit is, and where the sum is none.  The sum is never -0.
+__device__ __forceinline__ double key_of_sum(float x, float bias, int e) {
+  const float c = logistic(x) + bias;
+  const int32_t high = c > kNone() ? __builtin_bit_cast(int32_t, c) : kNoneBits;   // two selects: with `and` the compiler branches
+  return key_of(x > kNone() ? high : kNoneBits, e);
 }
 __device__ __forceinline__ float choice_of(double key) { return __builtin_bit_cast(float, (uint32_t)(__builtin_bit_cast(uint64_t, key) >> 32)); }
 __device__ __forceinline__ int expert_of(double key) {
@@ -266,13 +277,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteParams 
     double batch[N];
     if (p.bias) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float u = usable(v[i]), c = logistic(u) + b[i];
-        batch[i] = u == kNone() || c != c ? none_key() : key_of(c, first + i);
-      }
+      for (int i = 0; i < N; ++i) batch[i] = key_of_sum(v[i], b[i], first + i);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) batch[i] = v[i] == v[i] ? key_of(usable(v[i]), first + i) : none_key();
+      for (int i = 0; i < N; ++i) batch[i] = key_of_logit(v[i], first + i);
     }
     sort(batch);
     merge(list, batch);
