@@ -7,7 +7,8 @@
  * send list in which every token appears at most once (the group-OR of Eq.(7)), packs the bf16
  * token rows into per-destination send buffers, and merges expert outputs coming back in that
  * layout with the router weights ("AlltoAll Combine", Section II-B).  Destinations are index
- * partitions of one buffer; the exchange itself is not part of the library.
+ * partitions of one buffer; the exchange itself is not part of the library.  In front of the plan stands the router (hm_route), between
+ * dispatch and combine the experts' products in 8 bits (hm_expert_matmul), both with their gradients.
  *
  * Conventions
  *   - Unless marked "host", every pointer is a DEVICE pointer into memory the caller owns.

@@ -132,6 +132,9 @@ __device__ __forceinline__ uint32_t codes_at(__amdgpu_buffer_rsrc_t base, uint32
 // pieces are stored at places exchanged by half the row number, so that sixteen rows of a fragment, which are read
 // together, spread over all 64 banks.  Lane l has row l % 32 of a fragment and its pieces 4 (l / 32) to 4 (l / 32) + 3; which
 // values meet in an instruction does not matter as long as both operands' lanes hold the same ones.
+//
+// 65,536 rows, 32 experts, 4,096 x 7,168, bf16 results 1,570 us (2.45 PFLOP/s; the products alone take 1,000, without loads 1,375: the
+// unit's clock falls with what the rest draws); 32,768 rows, 16 experts, gradient of 1,536 x 2,048 in fp32 189 (1.09 PFLOP/s).
 constexpr int kUnits = 5;
 template <int FQ, int FP, int WQ, int WP, bool DW, typename OUT>
 __global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product_kernel(ProductParams p) {

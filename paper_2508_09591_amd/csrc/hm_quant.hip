@@ -20,7 +20,8 @@ struct RowParams {
   uint8_t *q, *scale;
 };
 
-// A wave takes 512 columns of a row, a lane eight of them, sixteen lanes a block.
+// A wave takes 512 columns of a row, a lane eight of them, sixteen lanes a block.  Bound by memory: 8,192 x 7,168 bf16 34 us,
+// 5.2 TB/s.
 template <typename IN>
 __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(RowParams p) {
   const int lane = lane_id();
@@ -75,7 +76,8 @@ __device__ __forceinline__ BlockOwner8 owner_of_block8(const int32_t *__restrict
 }
 
 // A workgroup takes a block of 128 rows and 64 columns: a thread eight rows of four columns, whose bytes it turns in
-// registers; LDS puts a column's 128 bytes together.
+// registers; LDS puts a column's 128 bytes together.  6,001 rows of 2,056 bf16 in 16 segments 11 us, 3.3 TB/s: one generation of
+// workgroups, whose offsets, rows and stores wait for one another (23 with scalar loads, 14 with neighbouring tiles on any die).
 constexpr int kColumnTile = 64, kColumnPitch = 128 + 8;
 template <typename IN>
 __global__ __launch_bounds__(kQuantThreads) void quantize_columns_kernel(ColumnParams p) {
@@ -149,7 +151,8 @@ struct WeightParams {
   uint8_t *q, *scale, *qt, *scale_t;
 };
 
-// A workgroup takes a block of 128 x 128: a thread eight rows of eight columns.
+// A workgroup takes a block of 128 x 128: a thread eight rows of eight columns.  Bound by memory: 32 x 2,048 x 2,048 fp32, both
+// layouts, 145 us, 5.6 TB/s.
 template <typename IN>
 __global__ __launch_bounds__(kQuantThreads) void quantize_weights_kernel(WeightParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[128 * kColumnPitch];

@@ -60,7 +60,9 @@ __device__ __forceinline__ void wave_first(float &v, int &i) {
   }
 }
 
-// A wave takes a token; its choices stand in LDS and the largest is taken K times.
+// What the choice by lists (below) does not take: K > 16, groups that are no power of two up to 16, a softmax with a bias, many
+// experts.  A wave takes a token; its choices stand in LDS and the largest is taken K times: 65,536 tokens of 256 experts 178 us
+// where the lists take 30.
 template <typename IN>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteParams p) {
   extern __shared__ float choices[];
@@ -252,8 +254,9 @@ __device__ __forceinline__ void load_logits(const IN *p, int n, float (&v)[N]) {
 // L lanes take a token, each a run of its experts, of which it keeps the N >= K largest; the lists of the lanes are
 // then merged pairwise.  With groups the L lanes are shared among them, so that a lane's run lies in one group, and
 // the two largest of its list give the group's score: lists of groups that are not taken are emptied before the merges.
-// What bounds it are vector instructions: 25 per expert of a logistic score, 7 of keys and 13 of sorting (N = 8), against
-// 4 bytes read.
+// What bounds it are vector instructions: about 27 an expert for a logistic score, 4 for its key and 9 for sorting (N = 8), against 4
+// bytes read.  us: 65,536 tokens, 256 experts, logistic with bias and groups 30 (2.4 TB/s), softmax 24, bf16 18; one token 5.3.
+// 8 lanes a token from 16,384 tokens on: 65,536 x 64 8.4 and, with 16 lanes, 14.7; 8,192 x 256 8.3 and 6.9.
 template <typename IN, int L, int N>
 __global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteParams p, int lanes_per_group, int run) {
   const int sub = (int)threadIdx.x & (L - 1);
@@ -386,7 +389,7 @@ struct RouteBackParams {
 __device__ __forceinline__ void put(uint16_t *x, float v) { *x = (uint16_t)f32_to_bf16(v); }
 __device__ __forceinline__ void put(float *x, float v) { *x = v; }
 
-// A wave takes a token, a lane a slot; the row is put together in LDS.
+// A wave takes a token, a lane a slot; the row is put together in LDS.  8,192 x 256 fp32 6 us, the stores of 8 MB and a launch.
 template <typename IN>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteBackParams p) {
   extern __shared__ float rows[];
@@ -486,7 +489,8 @@ struct Eight<float> {
 
 // A wave takes a part of a token's row and eight of its slots at a time: its gradient's row once, the eight rows beside it, all
 // loads of 512 elements on their way together.  Where a row is split, the parts' sums meet in LDS.  What bounds it is
-// memory: (K + 1) rows a token.
+// memory, (K + 1) rows a token: 8,192 tokens, K = 8, 7,168 bf16 180 us, 5.9 TB/s; few tokens wait for one trip after the
+// other (1,237 tokens, K = 6, 1,030 fp32 11 us).
 template <typename IN, int PARTS>
 __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(WeightGradParams p) {
   __shared__ float parts[kRouteWaves][8];
