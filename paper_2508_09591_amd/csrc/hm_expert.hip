@@ -80,7 +80,8 @@ struct Slice<false> {   // 32 values: one instruction, half a step
     const i32x4 lo = *(const i32x4 *)(lds + at[2 * part] + fragment), hi = *(const i32x4 *)(lds + at[2 * part + 1] + fragment);
     v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
   }
-  __device__ __forceinline__ void times(const Slice &q, uint32_t code_p, uint32_t code_q, f32x16 &acc) const {
+  static constexpr int kProducts = 1;
+  __device__ __forceinline__ void times(const Slice &q, uint32_t code_p, uint32_t code_q, f32x16 &acc, int) const {
     acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v, q.v, acc, 0, 0, 0, (int)code_p, 0, (int)code_q);   // 0, 0: e4m3
   }
 };
@@ -95,9 +96,9 @@ struct Slice<true> {   // 16 values: two instructions, a quarter of a step
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true);
     return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   }
-  __device__ __forceinline__ void times(const Slice &q, uint32_t code_p, uint32_t code_q, f32x16 &acc) const {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(v[0], v[1], code_p), widen(q.v[0], q.v[1], code_q), acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(v[2], v[3], code_p), widen(q.v[2], q.v[3], code_q), acc, 0, 0, 0);
+  static constexpr int kProducts = 2;
+  __device__ __forceinline__ void times(const Slice &q, uint32_t code_p, uint32_t code_q, f32x16 &acc, int h) const {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(v[2 * h], v[2 * h + 1], code_p), widen(q.v[2 * h], q.v[2 * h + 1], code_q), acc, 0, 0, 0);
   }
 };
 
@@ -291,8 +292,11 @@ __global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product
       const int since = (item + kAhead) % kItems;
       fill(since, since + 1, item + kAhead < kItems ? k + 1 : k + 2);
       read((item + kAhead) % kItems);
+      // one product after the other with other sums: one that waits for its own sum's last leaves the unit idle
 #pragma unroll
-      for (int j = 0; j < FP; ++j) other[j].times(mine, scale_of_p[j], scale_of_q[item % FQ], acc[item % FQ][j]);
+      for (int h = 0; h < Slice<kFull>::kProducts; ++h)
+#pragma unroll
+        for (int j = 0; j < FP; ++j) other[j].times(mine, scale_of_p[j], scale_of_q[item % FQ], acc[item % FQ][j], h);
       __builtin_amdgcn_sched_barrier(0);   // keeps the loads' order; and else the compiler reads all items at once and runs out of registers
     }
   };
