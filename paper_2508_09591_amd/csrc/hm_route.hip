@@ -487,13 +487,13 @@ struct Eight<float> {
   }
 };
 
-// A wave takes a part of a token's row and eight of its slots at a time: its gradient's row once, the eight rows beside it, all
+// A wave takes a part of a token's row and SLOTS of its slots at a time: its gradient's row once, the slots' rows beside it, all
 // loads of 512 elements on their way together.  Where a row is split, the parts' sums meet in LDS.  What bounds it is
 // memory, (K + 1) rows a token: 8,192 tokens, K = 8, 7,168 bf16 180 us, 5.9 TB/s; few tokens wait for one trip after the
-// other (1,237 tokens, K = 6, 1,030 fp32 11 us).
-template <typename IN, int PARTS>
+// other (1,237 tokens, K = 6, 1,030 fp32 9 us).
+template <typename IN, int PARTS, int SLOTS>
 __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(WeightGradParams p) {
-  __shared__ float parts[kRouteWaves][8];
+  __shared__ float parts[kRouteWaves][SLOTS];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), part = wave % PARTS;
   const int64_t t = (int64_t)blockIdx.x * (kRouteWaves / PARTS) + wave / PARTS;
   const bool there_t = t < p.T;   // the same for the waves of a token; with several parts nobody leaves before the barriers
@@ -501,26 +501,28 @@ __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(Weig
   const int64_t token = there_t ? t : 0;
   const IN *gout = (const IN *)p.gout + token * p.H;
   constexpr int kStep = kWave * 8;
-  for (int k0 = 0; k0 < p.K; k0 += 8) {
-    const IN *row[8];
-    bool there[8], bad = false;
+  for (int k0 = 0; k0 < p.K; k0 += SLOTS) {
+    const IN *row[SLOTS];
+    bool there[SLOTS], bad = false;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < SLOTS; ++j) {
       const int64_t r = k0 + j < p.K ? p.slot_row[token * p.K + k0 + j] : -1;
       there[j] = r >= 0 && r < p.y_rows;
       bad = bad || r >= p.y_rows;
       row[j] = there[j] ? (const IN *)p.y + r * p.H : gout;   // something to read in place of a row that is not there
     }
     if (bad && lane == 0 && there_t) flag(p.status, HM_ERR_CAPACITY);
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    float sum[SLOTS];
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) sum[j] = 0.0f;
     int h = part * kStep + lane * 8;
     for (int first = part * kStep; first + kStep <= p.H; first += PARTS * kStep, h += PARTS * kStep) {
-      Eight<IN> g(gout + h), v[8];
+      Eight<IN> g(gout + h), v[SLOTS];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < SLOTS; ++j)
         if (k0 + j < p.K) v[j] = Eight<IN>(row[j] + h);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < SLOTS; ++j)
         if (k0 + j < p.K) sum[j] = g.times(v[j], sum[j]);
     }
     // The row's last, shorter step is the part's whose turn it is: vectors that would pass the end lie before it, and what
@@ -532,12 +534,12 @@ __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(Weig
           const int at = min(h, p.H - 8), had = h - at;
           float g[8];
           load_floats<8>(gout + at, g);
-          Eight<IN> v[8];
+          Eight<IN> v[SLOTS];
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
+          for (int j = 0; j < SLOTS; ++j)
             if (k0 + j < p.K) v[j] = Eight<IN>(row[j] + at);
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
+          for (int j = 0; j < SLOTS; ++j)
             if (k0 + j < p.K) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) sum[j] = i < had ? sum[j] : fmaf(g[i], v[j].at(i), sum[j]);
@@ -546,25 +548,25 @@ __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(Weig
       } else if (lane < p.H) {
         const float g = load_float(gout + lane);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < SLOTS; ++j)
           if (k0 + j < p.K) sum[j] = fmaf(g, load_float(row[j] + lane), sum[j]);
       }
     }
     float mine = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < SLOTS; ++j) {
       const float s = wave_sum(sum[j]);
       mine = lane == j && there[j] ? s : mine;
     }
     if (PARTS > 1) {
-      if (lane < 8) parts[wave][lane] = mine;
+      if (lane < SLOTS) parts[wave][lane] = mine;
       __syncthreads();
       mine = 0.0f;
-      if (lane < 8)
+      if (lane < SLOTS)
         for (int w = 0; w < PARTS; ++w) mine += parts[wave - part + w][lane];
       __syncthreads();
     }
-    if (part == 0 && there_t && lane < 8 && k0 + lane < p.K) p.grad[token * p.K + k0 + lane] = mine;
+    if (part == 0 && there_t && lane < SLOTS && k0 + lane < p.K) p.grad[token * p.K + k0 + lane] = mine;
   }
 }
 
@@ -656,10 +658,14 @@ extern "C" hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_
   if (T == 0) return HM_OK;
   if (!gout || !grad_weights || (!y && y_rows > 0)) return HM_ERR_NULL;
   const WeightGradParams p = {gout, y, y_rows, plan->slot_row, T, K, H, grad_weights, plan->status};
-  // a token's row in four parts where there are few tokens
+  // A token's row in four parts where there are few tokens.  Eight slots at a time read the gradient's row once for most K; fp32
+  // rows take the registers of four waves a SIMD for that, so they go four at a time (8,192 x 2,048, K = 8: 125 us and 137) but where
+  // rows are long (8,192 x 7,168: 395 and 356).
   const int parts = T <= 4096 && H > 512 ? kRouteWaves : 1, tokens = kRouteWaves / parts;
-  const auto whole = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, 1> : combine_weight_grad_kernel<float, 1>;
-  const auto split = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, kRouteWaves> : combine_weight_grad_kernel<float, kRouteWaves>;
+  const auto whole = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, 1, 8>
+                     : H >= 4096      ? combine_weight_grad_kernel<float, 1, 8>
+                                      : combine_weight_grad_kernel<float, 1, 4>;
+  const auto split = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, kRouteWaves, 8> : combine_weight_grad_kernel<float, kRouteWaves, 4>;
   hipLaunchKernelGGL((parts == 1 ? whole : split), dim3((unsigned)((T + tokens - 1) / tokens)), dim3(kRouteThreads), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
