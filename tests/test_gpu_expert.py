@@ -224,6 +224,24 @@ def test_a_nan_stays_in_its_row_and_column():
         assert np.array_equal(bad, want)
 
 
+@pytest.mark.parametrize("low", [0, 1, 2, 3, 5])
+@pytest.mark.parametrize("rows", [8, 300])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_the_least_scales(low, rows, dtype):
+    """Codes from 0 on; fp32 results round values to multiples of 2^-133, which only codes below 3 have need of."""
+    N, H = 64, 256
+    rng = np.random.default_rng(rows + low)
+    x, w = operand(rng, rows, H), operand(rng, 1, N, H)
+    xs, ws = np.full((rows, 4), low, dtype=np.uint8), np.full((1, 1, 4), 240, dtype=np.uint8)
+    out = torch.zeros((rows, N), dtype=dtype, device="cuda")
+    B.hm_expert_matmul(f8(x).cuda(), dev(xs), f8(w).cuda(), dev(ws), dev(np.array([0, rows], dtype=np.int32)), out)
+    a = R.row_values(f8(x).float().numpy().astype(np.float64), xs.astype(np.int64))
+    b = R.weight_values(f8(w).float().numpy().astype(np.float64), ws.astype(np.int64))[0]
+    want, size, largest = R.product(a, b, H // 128)
+    lost = 2.0 ** -133 * np.abs(b).sum(axis=1)[None, :] if dtype == torch.float32 and low < 3 else 0.0
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound(want, size, largest, H, dtype) + lost)
+
+
 def test_offsets_that_are_wrong_stay_inside():
     """Descending offsets and offsets outside the rows: nothing outside the outputs is written."""
     rows, N, H = 50, 40, 128
