@@ -224,6 +224,30 @@ def test_a_nan_stays_in_its_row_and_column():
         assert np.array_equal(bad, want)
 
 
+@pytest.mark.parametrize("rows,E,N,H", [(1, 1, 40, 128), (3, 1, 17, 129), (8, 32, 64, 640), (16, 1, 33, 2056), (24, 8, 100, 300)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_few_rows_are_summed_in_32_bits(rows, E, N, H, dtype):
+    """Whole numbers beside products of 448 x 448 that cancel: every partial sum lies below 2^24 and the results below 2^8, so
+    that sums in 32 bits, in any order, and their rounding to bf16 are exact."""
+    rng = np.random.default_rng(rows + N + H)
+    x, w = rng.integers(-2, 3, (rows, H)).astype(np.float32), rng.integers(-2, 3, (E, N, H)).astype(np.float32)
+    x[:, 64:], w[:, :, 64:] = 0, 0   # at most 64 products of at most 4
+    for first in range(0, H - 1, 128):   # two that cancel in each block
+        a, b = first + rng.permutation(min(128, H - first))[:2]
+        x[:, a], x[:, b] = 448, -448
+        w[:, :, a], w[:, :, b] = 448, 448
+    off = offsets_of(np.bincount(rng.permutation(np.arange(rows) % E), minlength=E))
+    W = R.up(H, 128)
+    pad = lambda t: torch.nn.functional.pad(torch.from_numpy(t), (0, W - H)).to(F8).cuda()
+    xs = torch.full((rows, R.up(H, 512) // 128), 127, dtype=torch.uint8, device="cuda")
+    ws = torch.full((E, R.up(N, 128) // 128, R.up(H, 512) // 128), 127, dtype=torch.uint8, device="cuda")
+    out = torch.full((rows, N), -77.0, dtype=dtype, device="cuda")
+    B.hm_expert_matmul(pad(x), xs, pad(w), ws, dev(off), out)
+    expert = np.repeat(np.arange(E), np.diff(off))
+    want = np.einsum("rh,rnh->rn", x.astype(np.float64), w.astype(np.float64)[expert])
+    assert np.abs(want).max() <= 256 and np.array_equal(out.double().cpu().numpy(), want)
+
+
 @pytest.mark.parametrize("low", [0, 1, 2, 3, 5])
 @pytest.mark.parametrize("rows", [8, 300])
 @pytest.mark.parametrize("dtype", DTYPES)
