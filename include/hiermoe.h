@@ -450,7 +450,7 @@ hm_status hm_swap_apply(int32_t *expert_to_rank, int32_t E, const int32_t *best_
  * Limits: E <= 4096, K <= 64, K <= the experts of top_groups groups (else HM_ERR_SHAPE, as for top_groups > groups,
  * groups not dividing E, group_best other than 1 or 2 or above the experts of a group).
  */
-typedef enum { HM_BF16 = 0, HM_F32 = 1 } hm_dtype;
+typedef enum { HM_BF16 = 0, HM_F32 = 1, HM_BF16_SUM_F32 = 2 /* results of products only: bf16 from sums in fp32 */ } hm_dtype;
 typedef enum { HM_SCORE_SOFTMAX = 0, HM_SCORE_SIGMOID = 1 } hm_score;
 typedef struct {
   int32_t E, K;
@@ -520,12 +520,12 @@ hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, in
  * hm_expert_matmul -- every row times the weights of its expert:
  *     out[r,n] = sum_h x[r,h] w[e,n,h],   offsets[e] <= r < offsets[e+1].
  * fp32 results are sums in fp32 of the exact products, values being taken as bf16: under codes 0 to 2 (blocks within 1.1e-35) they
- * are rounded to multiples of 2^-133.  bf16 results of few rows (up to 16, or up to four an expert) are these, rounded
- * once.  Other bf16 results come from the matrix unit's products of 8 bits, which drop what lies more than 2^13 below the largest
+ * are rounded to multiples of 2^-133.  HM_BF16_SUM_F32 results are these rounded once, and so are HM_BF16 results of few rows (up
+ * to 16, or up to four an expert).  Other HM_BF16 results come from the matrix unit's products of 8 bits, twice as fast, which drop what lies more than 2^13 below the largest
  * of 64 products before they add in fp32, and are then rounded once.  The loss is at most 2^-7 of the largest product for each
  * 64; of the results' norm it was 1.5e-5 for normally distributed values and 5e-5 to 9e-5 for bytes of every exponent and for
- * columns 30 to 1,000 times as large as the others, where the rounding is 1.7e-3.  Where more products cancel than
- * that bears, take fp32 results.
+ * columns 30 to 1,000 times as large as the others, where the rounding is 1.7e-3.  Where large
+ * products cancel, little is left of the small ones.
  * x, w with their scales in the layouts `rows` and `weights` above (C = H), offsets device int32[experts + 1], out
  * [rows,N] of out_dtype; rows from offsets[experts] on are left alone.  With the rows of the output's gradient and the
  * transposed weights (N and H exchanged) the same call is the gradient of x.

@@ -39,7 +39,7 @@ except ImportError as e:
 
 HM_DEDUP_NONE, HM_DEDUP_GPU, HM_DEDUP_NODE = 0, 1, 2
 HM_RECV_INTRA_NODE, HM_RECV_LOCAL_EXPERTS = 0, 1
-HM_BF16, HM_F32 = 0, 1
+HM_BF16, HM_F32, HM_BF16_SUM_F32 = 0, 1, 2
 HM_SCORE_SOFTMAX, HM_SCORE_SIGMOID = 0, 1
 HM_OK = 0
 HM_ERR_NULL, HM_ERR_SHAPE, HM_ERR_TOPOLOGY, HM_ERR_LEVEL = -1, -2, -3, -4
@@ -637,6 +637,12 @@ def _floats(t: torch.Tensor, name: str) -> int:
     raise TypeError("%s must be torch.bfloat16 or torch.float32, got %s" % (name, t.dtype))
 
 
+def _sums(t: torch.Tensor, name: str, full: bool) -> int:
+    """The type of a product's results and how they are summed."""
+    dtype = _floats(t, name)
+    return HM_BF16_SUM_F32 if full and dtype == HM_BF16 else dtype
+
+
 def _rows_of(t: torch.Tensor, name: str):
     """(address, elements from row to row) of a matrix whose rows are dense but may lie apart."""
     if not t.is_cuda:
@@ -800,10 +806,11 @@ def hm_quantize_weights(w: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, q
 
 
 def hm_expert_matmul(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, offsets: torch.Tensor,
-                     out: torch.Tensor, stream=None) -> torch.Tensor:
+                     out: torch.Tensor, stream=None, full_sums: bool = False) -> torch.Tensor:
     """out [rows, N]: every row times the weights of its expert.  x and w hold as many blocks of 128 columns, the columns
-    themselves are told from them: zeros fill the last block, so its end does not matter."""
-    rc = _native.expert_matmul(x, x_scale, w, w_scale, offsets, out) if stream is None else None
+    themselves are told from them: zeros fill the last block, so its end does not matter.  full_sums: bf16 results are sums
+    in 32 bits too, at half the speed; fp32 results always are."""
+    rc = _native.expert_matmul(x, x_scale, w, w_scale, offsets, out, full_sums) if stream is None else None
     if rc is not None:
         _check("hm_expert_matmul", rc)
         return out
@@ -812,15 +819,16 @@ def hm_expert_matmul(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_
     rc = lib().hm_expert_matmul(_codes(x, (rows, width), "x"), _scales(x_scale, (rows, scale8_bytes(width)), "x_scale"),
                                 _codes(w, (E, N, width), "w"), _scales(w_scale, (E, (N + 127) // 128, scale8_bytes(width)), "w_scale"),
                                 _dev(_shaped(offsets, (E + 1,), "offsets"), torch.int32, "offsets"), E, rows, N, width,
-                                _dev(_shaped(out, (rows, N), "out"), out.dtype, "out"), _floats(out, "out"), _stream(stream))
+                                _dev(_shaped(out, (rows, N), "out"), out.dtype, "out"), _sums(out, "out", full_sums), _stream(stream))
     _check("hm_expert_matmul", rc)
     return out
 
 
 def hm_expert_matmul_dw(gy: torch.Tensor, gy_scale: torch.Tensor, x: torch.Tensor, x_scale: torch.Tensor, offsets: torch.Tensor,
-                        rows: int, dw: torch.Tensor, stream=None) -> torch.Tensor:
-    """dw [experts, N, H] from the columns of gy [N, ...] and x [H, ...] over `rows` rows ordered by expert."""
-    rc = _native.expert_matmul_dw(gy, gy_scale, x, x_scale, offsets, rows, dw) if stream is None else None
+                        rows: int, dw: torch.Tensor, stream=None, full_sums: bool = False) -> torch.Tensor:
+    """dw [experts, N, H] from the columns of gy [N, ...] and x [H, ...] over `rows` rows ordered by expert; full_sums as in
+    hm_expert_matmul."""
+    rc = _native.expert_matmul_dw(gy, gy_scale, x, x_scale, offsets, rows, dw, full_sums) if stream is None else None
     if rc is not None:
         _check("hm_expert_matmul_dw", rc)
         return dw
@@ -829,6 +837,6 @@ def hm_expert_matmul_dw(gy: torch.Tensor, gy_scale: torch.Tensor, x: torch.Tenso
     rc = lib().hm_expert_matmul_dw(_codes(gy, (N, 128 * blocks), "gy"), _scales(gy_scale, (blocks, N), "gy_scale"),
                                    _codes(x, (H, 128 * blocks), "x"), _scales(x_scale, (blocks, H), "x_scale"),
                                    _dev(_shaped(offsets, (E + 1,), "offsets"), torch.int32, "offsets"), E, rows, N, H,
-                                   _dev(dw, dw.dtype, "dw"), _floats(dw, "dw"), _stream(stream))
+                                   _dev(dw, dw.dtype, "dw"), _sums(dw, "dw", full_sums), _stream(stream))
     _check("hm_expert_matmul_dw", rc)
     return dw

@@ -450,6 +450,13 @@ hm_dtype floats(const at::Tensor &t) {
   if (t.scalar_type() == at::kFloat) return HM_F32;
   throw NotOrdinary();
 }
+// The type of a product's results, with their sums in 32 bits if `full` is true.
+hm_dtype sums(const at::Tensor &t, PyObject *full) {
+  const hm_dtype dtype = floats(t);
+  const int f = PyObject_IsTrue(full);
+  if (f < 0) throw NotOrdinary();
+  return f && dtype == HM_BF16 ? HM_BF16_SUM_F32 : dtype;
+}
 // A dense matrix of floats.
 const at::Tensor &matrix(PyObject *o, int32_t &rows, int32_t &cols) {
   const at::Tensor &t = tensor(o);
@@ -544,8 +551,8 @@ PyObject *quantize_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {   // 
   });
 }
 
-PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, x_scale, w, w_scale, offsets, out
-  return layer_answer(n, 6, [&] {
+PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, x_scale, w, w_scale, offsets, out, full_sums
+  return layer_answer(n, 7, [&] {
     const at::Tensor &w = checked(a[2], at::kFloat8_e4m3fn);
     if (w.dim() != 3) throw NotOrdinary();
     const int32_t E = size32(w.size(0)), N = size32(w.size(1)), H = size32(w.size(2));
@@ -556,15 +563,16 @@ PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, 
     const auto *ws = scales8(a[3], {E, up(N, 128) / 128, up(H, 512) / 128});
     const auto *offsets = shaped<const int32_t>(a[4], at::kInt, {static_cast<int64_t>(E) + 1});
     const auto *wq = static_cast<const uint8_t *>(w.data_ptr());
-    return launched([&](void *s) { return layer.expert_matmul(x, xs, wq, ws, offsets, E, rows, N, H, out.data_ptr(), floats(out), s); });
+    const hm_dtype dtype = sums(out, a[6]);
+    return launched([&](void *s) { return layer.expert_matmul(x, xs, wq, ws, offsets, E, rows, N, H, out.data_ptr(), dtype, s); });
   });
 }
 
-PyObject *expert_matmul_dw(PyObject *, PyObject *const *a, Py_ssize_t n) {   // gy, gy_scale, x, x_scale, offsets, rows, dw
-  return layer_answer(n, 7, [&] {
+PyObject *expert_matmul_dw(PyObject *, PyObject *const *a, Py_ssize_t n) {   // gy, gy_scale, x, x_scale, offsets, rows, dw, full_sums
+  return layer_answer(n, 8, [&] {
     const at::Tensor &dw = tensor(a[6]);
     if (!dw.is_cuda() || !dw.is_contiguous() || dw.dim() != 3) throw NotOrdinary();
-    const hm_dtype dtype = floats(dw);
+    const hm_dtype dtype = sums(dw, a[7]);
     const int32_t E = size32(dw.size(0)), N = size32(dw.size(1)), H = size32(dw.size(2)), rows = integer32(a[5]);
     if (rows < 0) throw NotOrdinary();
     const int64_t blocks = rows / 128 + static_cast<int64_t>(E);

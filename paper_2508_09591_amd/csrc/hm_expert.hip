@@ -9,10 +9,11 @@
 // that is 2^-7 of a step's largest product.  Measured before the rounding, as a part of the results' norm (2,048 x 1,024 sums of
 // 4,096 products): 1.5e-5 of normally distributed values, 4.5e-5, 7.1e-5 and 9.2e-5 where 8 columns are 30, 100 and 1,000 times as
 // large, 7.5e-5 of log-normal values (sigma 2), 5.1e-5 of bytes drawn evenly from all codes.  Rounding to bf16 costs 1.7e-3 in all
-// of them, so that their error with and without the loss is the same in three digits.  So bf16 results of tiles take these products,
-// which are twice as fast.
-// fp32 results, and bf16 results of few rows, which memory bounds, have their operands turned into bf16 in registers, which is
-// exact and takes the power of two along, and products of 16 bits, which are summed in 32 (1e-8 a step).
+// of them, so that their error with and without the loss is the same in three digits; but where large products cancel nothing of the
+// small ones is left.  So bf16 results of tiles take these products, which are twice as fast, unless the caller wants sums in 32 bits.
+// Those, fp32 results, and bf16 results of few rows, which memory bounds, have their operands turned into bf16 in registers, which
+// is exact and takes the power of two along, and products of 16 bits, which are summed in 32 (1e-8 a step): 65,536 rows, 32
+// experts, 4,096 x 7,168 3,110 us for 1,520.
 #include "hm_block8.h"
 
 namespace hm {
@@ -141,10 +142,9 @@ __device__ __forceinline__ uint32_t codes_at(__amdgpu_buffer_rsrc_t base, uint32
 // 65,536 rows, 32 experts, 4,096 x 7,168, bf16 results 1,570 us (2.45 PFLOP/s; the products alone take 1,000, without loads 1,375: the
 // unit's clock falls with what the rest draws); 32,768 rows, 16 experts, gradient of 1,536 x 2,048 in fp32 189 (1.09 PFLOP/s).
 constexpr int kUnits = 5;
-template <int FQ, int FP, int WQ, int WP, bool DW, typename OUT>
+template <int FQ, int FP, int WQ, int WP, bool DW, bool kFull, typename OUT>
 __global__ __launch_bounds__(WQ * WP * kWave, FQ * FP < 16 ? 2 : 1) void product_kernel(ProductParams p) {
   constexpr int kWaves = WQ * WP, TQ = FQ * WQ * 32, TP = FP * WP * 32;
-  constexpr bool kFull = sizeof(OUT) == 4;
   constexpr int kSlices = kFull ? 4 : 2, kUnitBytes = TQ * 128;
   static_assert(TQ == TP && kWaves % 2 == 0, "units of one size; the pieces' places go by the wave's number");
   constexpr int kLoads = TQ / 8 / kWaves;   // of a wave for a unit
@@ -445,7 +445,8 @@ __global__ __launch_bounds__(kThinWaves * kWave) void thin_product_kernel(Produc
 
 static hm_status check_products(const void *a, const void *as, const void *b, const void *bs, const int32_t *offsets, int32_t experts, int64_t rows,
                                 int32_t N, int32_t H, const void *out, hm_dtype dtype, bool none) {
-  if (!dtype_known(dtype) || !segments8_ok(experts, rows) || N < 1 || N > kMostColumns8 || H < 1 || H > kMostColumns8) return HM_ERR_SHAPE;
+  if (!dtype_known(dtype) && dtype != HM_BF16_SUM_F32) return HM_ERR_SHAPE;
+  if (!segments8_ok(experts, rows) || N < 1 || N > kMostColumns8 || H < 1 || H > kMostColumns8) return HM_ERR_SHAPE;
   if (!buffers8_aligned(a, as) || !buffers8_aligned(b, bs) || ((uintptr_t)out & (dtype == HM_F32 ? 3 : 1))) return HM_ERR_SHAPE;
   if (none) return HM_OK;
   if (!a || !as || !b || !bs || !offsets || !out) return HM_ERR_NULL;
@@ -462,7 +463,9 @@ static int tile_side(bool large, int64_t tiles128) { return large ? 256 : tiles1
 
 template <int FQ, int FP, int WQ, int WP, bool DW>
 static hm_status launch_tiles(const ProductParams &p, hm_dtype dtype, dim3 grid, void *stream) {
-  const auto kernel = dtype == HM_BF16 ? product_kernel<FQ, FP, WQ, WP, DW, uint16_t> : product_kernel<FQ, FP, WQ, WP, DW, float>;
+  const auto kernel = dtype == HM_F32            ? product_kernel<FQ, FP, WQ, WP, DW, true, float>
+                      : dtype == HM_BF16_SUM_F32 ? product_kernel<FQ, FP, WQ, WP, DW, true, uint16_t>
+                                                 : product_kernel<FQ, FP, WQ, WP, DW, false, uint16_t>;
   hipLaunchKernelGGL(kernel, grid, dim3(WQ * WP * kWave), 0, (hipStream_t)stream, p);
   return hm_launch_status();
 }
@@ -470,7 +473,7 @@ template <bool DW>
 static hm_status launch_products(const ProductParams &p, int side, hm_dtype dtype, dim3 grid, void *stream) {
   if (side == 256) {
     if constexpr (DW) return launch_tiles<4, 4, 2, 2, true>(p, dtype, grid, stream);
-    hipLaunchKernelGGL((product_kernel<4, 4, 2, 2, false, uint16_t>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL((product_kernel<4, 4, 2, 2, false, false, uint16_t>), grid, dim3(256), 0, (hipStream_t)stream, p);
     return hm_launch_status();
   }
   if (side == 128) return launch_tiles<2, 2, 2, 2, DW>(p, dtype, grid, stream);
@@ -493,7 +496,7 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   if (rows <= 4LL * experts || rows <= 16) {
     const int64_t tiles = (rows / 16 + (rows < experts ? rows : experts)) * ((N + 15) / 16) + 8;
     if (tiles > (1 << 23)) return HM_ERR_SHAPE;
-    const auto kernel = out_dtype == HM_BF16 ? thin_product_kernel<uint16_t> : thin_product_kernel<float>;
+    const auto kernel = out_dtype == HM_F32 ? thin_product_kernel<float> : thin_product_kernel<uint16_t>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(kThinWaves * kWave), 0, (hipStream_t)hip_stream, p);
     return hm_launch_status();
   }

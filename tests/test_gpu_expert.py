@@ -248,6 +248,81 @@ def test_few_rows_are_summed_in_32_bits(rows, E, N, H, dtype):
     assert np.abs(want).max() <= 256 and np.array_equal(out.double().cpu().numpy(), want)
 
 
+def cancelling(rng, rows, H):
+    """Whole numbers up to 2 in the first 64 columns, and 448 and -448 somewhere in every block, the same places in each row."""
+    x = rng.integers(-2, 3, (rows, H)).astype(np.float32)
+    x[:, 64:] = 0
+    for first in range(0, H - 1, 128):
+        a, b = first + rng.permutation(min(128, H - first))[:2]
+        x[:, a], x[:, b] = 448, -448
+    return x
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,E,N,H", [(40, 1, 33, 129), (300, 3, 130, 640), (2000, 5, 1500, 384), (8300, 8, 1000, 256)])
+def test_full_sums_of_rows(rows, E, N, H, dtype):
+    """Products that cancel, by tiles of each size, as in test_few_rows_are_summed_in_32_bits: exact in whatever order."""
+    rng = np.random.default_rng(rows)
+    x, w = cancelling(rng, rows, H), rng.integers(-2, 3, (E, N, H)).astype(np.float32)
+    w[:, :, np.abs(x[0]) == 448] = 448
+    off = offsets_of(np.bincount(rng.permutation(np.arange(rows) % E), minlength=E))
+    W = R.up(H, 128)
+    pad = lambda t: torch.nn.functional.pad(torch.from_numpy(t), (0, W - H)).to(F8).cuda()
+    xs = torch.full((rows, R.up(H, 512) // 128), 127, dtype=torch.uint8, device="cuda")
+    ws = torch.full((E, R.up(N, 128) // 128, R.up(H, 512) // 128), 127, dtype=torch.uint8, device="cuda")
+    x8, w8, out = pad(x), pad(w), torch.full((rows, N), -77.0, dtype=dtype, device="cuda")
+    want = [x[off[e]:off[e + 1]].astype(np.float64) @ w[e].astype(np.float64).T for e in range(E)]
+    for stream in (None, torch.cuda.current_stream()):   # by either way into the library
+        out.fill_(-77)
+        B.hm_expert_matmul(x8, xs, w8, ws, dev(off), out, stream=stream, full_sums=True)
+        assert np.array_equal(out.double().cpu().numpy(), np.concatenate(want))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("counts,N,H", [([40], 33, 129), ([130, 0, 257], 400, 300), ([300, 100, 128], 1500, 1541), ([200, 500], 4100, 3900)])
+def test_full_sums_of_columns(counts, N, H, dtype):
+    rng = np.random.default_rng(N)
+    off, E = offsets_of(counts), len(counts)
+    rows = int(off[-1])
+    blocks = rows // 128 + E
+    gy, x = np.zeros((N, 128 * blocks), dtype=np.float32), np.zeros((H, 128 * blocks), dtype=np.float32)
+    for e in range(E):
+        if counts[e]:
+            first = 128 * (off[e] // 128 + e)
+            part = slice(first, first + counts[e])
+            gy[:, part], x[:, part] = cancelling(rng, N, counts[e]), rng.integers(-2, 3, (H, counts[e]))
+            x[:, part][:, np.abs(gy[0, part]) == 448] = 448
+    one = lambda n: torch.full((blocks, n), 127, dtype=torch.uint8, device="cuda")
+    gy8, x8, dw = torch.from_numpy(gy).to(F8).cuda(), torch.from_numpy(x).to(F8).cuda(), torch.empty((E, N, H), dtype=dtype, device="cuda")
+    for stream in (None, torch.cuda.current_stream()):
+        dw.fill_(-77)
+        B.hm_expert_matmul_dw(gy8, one(N), x8, one(H), dev(off), rows, dw, stream=stream, full_sums=True)
+        for e in range(E):
+            part = slice(128 * (off[e] // 128 + e), 128 * (off[e] // 128 + e) + R.up(counts[e], 128))
+            want = torch.from_numpy(gy[:, part]).cuda().double() @ torch.from_numpy(x[:, part]).cuda().double().t().contiguous()
+            assert torch.equal(dw[e].double(), want), e
+
+
+def test_what_the_units_products_drop():
+    """bf16 results of tiles where 8 columns are 1,000 times as large as the others.  Each of the 64 products of a step loses
+    less than 2^-13 of the step's largest, either way alike: sqrt(64 / 3) 2^-13 = 2^-10.8 of it, and steps add as their squares; rounding
+    adds at most 2^-9 of a result.  Taken over a matrix, where such sums are sharp."""
+    rows, N, H = 2048, 512, 2048
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x, w = torch.randn((rows, H), generator=g, device="cuda"), torch.randn((1, N, H), generator=g, device="cuda") / H ** 0.5
+    x[:, ::256] *= 1000
+    off = dev(np.array([0, rows], dtype=np.int32))
+    x8, w8 = B.hm_quantize_rows(x, *B.alloc_rows8(rows, H)), B.hm_quantize_weights(w, *B.alloc_weights8(1, N, H))
+    out = torch.empty((rows, N), dtype=torch.bfloat16, device="cuda")
+    B.hm_expert_matmul(*x8, *w8, off, out)
+    a, b = gpu_values(x8[0], x8[1]), gpu_values(w8[0][0], w8[1][0].repeat_interleave(128, dim=0))
+    want = a @ b.t().contiguous()
+    most = lambda t: t.abs().view(t.shape[0], -1, 128).amax(dim=2).square()   # bounds the products of both steps of a block
+    loss = 2.0 ** -10.8 * (2 * (most(a) @ most(b).t().contiguous()).sum()).sqrt()
+    assert (out.double() - want).norm() <= ((2.0 ** -9 * want.norm()) ** 2 + loss ** 2).sqrt()
+
+
 @pytest.mark.parametrize("low", [0, 1, 2, 3, 5])
 @pytest.mark.parametrize("rows", [8, 300])
 @pytest.mark.parametrize("dtype", DTYPES)
