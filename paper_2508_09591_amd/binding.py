@@ -815,6 +815,8 @@ def hm_expert_matmul(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_
         _check("hm_expert_matmul", rc)
         return out
     E, N, width = w.shape
+    if width < 1 or width % 128:   # the kernels read whole blocks
+        raise ValueError("the rows of x and w must be whole blocks of 128 values, as hm_quantize_* write them, got %d" % width)
     rows = x.shape[0]
     rc = lib().hm_expert_matmul(_codes(x, (rows, width), "x"), _scales(x_scale, (rows, scale8_bytes(width)), "x_scale"),
                                 _codes(w, (E, N, width), "w"), _scales(w_scale, (E, (N + 127) // 128, scale8_bytes(width)), "w_scale"),

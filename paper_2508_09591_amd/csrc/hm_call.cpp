@@ -556,6 +556,7 @@ PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, 
     const at::Tensor &w = checked(a[2], at::kFloat8_e4m3fn);
     if (w.dim() != 3) throw NotOrdinary();
     const int32_t E = size32(w.size(0)), N = size32(w.size(1)), H = size32(w.size(2));
+    if (H < 1 || H % 128 != 0) throw NotOrdinary();   // whole blocks
     int32_t rows, cols;
     const at::Tensor &out = matrix(a[5], rows, cols);
     if (cols != N) throw NotOrdinary();

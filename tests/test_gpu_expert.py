@@ -541,6 +541,27 @@ def test_every_call_is_taken_by_the_native_half(monkeypatch):
     assert all(torch.equal(a, b) for a, b in zip(*both.values()))
 
 
+@pytest.mark.parametrize("width", [100, 300])
+def test_parts_of_blocks_are_refused_before_any_launch(width, monkeypatch):
+    """The native half leaves them to the Python code, which raises."""
+    B.lib()
+    taken, native = [], B._native
+
+    class Recorder:
+        def __getattr__(self, name):
+            return lambda *args: taken.append(getattr(native, name)(*args))
+
+    monkeypatch.setattr(B, "_native", Recorder())
+    e8 = lambda *shape: torch.zeros(shape, dtype=F8, device="cuda")
+    byte = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device="cuda")
+    operands = (e8(4, width), byte(4, B.scale8_bytes(width)), e8(2, 8, width), byte(2, 1, B.scale8_bytes(width)))
+    off, out = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros((4, 8), device="cuda")
+    for stream in (None, torch.cuda.current_stream()):
+        with pytest.raises(ValueError, match="whole blocks"):
+            B.hm_expert_matmul(*operands, off, out, stream=stream)
+    assert taken == [None]
+
+
 def test_results_do_not_depend_on_what_ran_before():
     """The same call into poisoned outputs: the same bits."""
     rng = np.random.default_rng(8)

@@ -113,6 +113,16 @@ def test_the_binding_refuses_tensors_it_cannot_use():
         B.Router(8, 2, "tanh")
 
 
+@pytest.mark.parametrize("width", [0, 1, 100, 127, 129, 300])
+def test_products_take_whole_blocks_of_values(width):
+    """The kernels read blocks of 128: operands that do not hold them whole are refused, whatever else fits."""
+    e8 = lambda *shape: torch.zeros(shape, dtype=torch.float8_e4m3fn)
+    byte = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    operands = (e8(4, width), byte(4, B.scale8_bytes(width)), e8(2, 8, width), byte(2, 1, B.scale8_bytes(width)))
+    with pytest.raises(ValueError, match="whole blocks"):
+        B.hm_expert_matmul(*operands, torch.zeros(3, dtype=torch.int32), torch.zeros((4, 8)))
+
+
 def test_sizes_of_the_layouts():
     assert [B.row8_bytes(c) for c in (1, 128, 129, 7168)] == [128, 128, 256, 7168]
     assert [B.scale8_bytes(c) for c in (1, 512, 513, 7168)] == [4, 4, 8, 56]
