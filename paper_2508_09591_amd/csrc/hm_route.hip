@@ -583,8 +583,8 @@ static hm_status check_router(const hm_router *r) {
 // sum before the choice.
 static int list_lanes(const hm_router &r, bool biased, int64_t T) {
   if (r.K > 16 || (r.groups & (r.groups - 1)) || r.groups > 16 || (biased && r.score == HM_SCORE_SOFTMAX)) return 0;
-  const int lanes = T >= 16384 && r.groups <= 8 ? 8 : 16;
-  return r.E <= 64 * lanes ? lanes : 0;
+  if (T >= 16384 && r.groups <= 8 && r.E <= 64 * 8) return 8;
+  return r.E <= 64 * 16 ? 16 : 0;
 }
 template <typename IN, int L>
 static void launch_lists(const RouteParams &p, hipStream_t stream) {

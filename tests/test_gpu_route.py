@@ -129,6 +129,30 @@ def test_experts_that_cannot_be_chosen(kind, renormalise, groups, biased):
     assert np.all(got[:2] == -1) and np.all(got_w[:2] == 0)
 
 
+def many(rng, T, E, bias, step):
+    """Logits of which a token has many that are equal; with a bias three values and a grid for the bias, as above."""
+    if bias:
+        return rng.choice(np.array([-1.5, 0.0, 0.75], dtype=np.float32), (T, E)), (rng.integers(-8, 9, E) * 0.0625).astype(np.float32)
+    return grid(rng, T, E, step), None
+
+
+def check_some(x, ids, w, bias, K, kind, **how):
+    """The first and the last tokens and some between against 64 bits."""
+    T = len(x)
+    some = np.unique(np.concatenate([np.arange(40), np.arange(T - 70, T), np.random.default_rng(T).integers(0, T, 200)]))
+    check(x[some], ids[torch.from_numpy(some).cuda()], w[torch.from_numpy(some).cuda()], bias, K, kind, **how)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind,bias", [("softmax", False), ("sigmoid", False), ("sigmoid", True)])
+@pytest.mark.parametrize("T,E,K", [(16384, 768, 8), (16385, 513, 3), (20001, 1000, 16)])
+def test_more_experts_than_eight_lanes_hold(T, E, K, kind, bias, dtype):
+    rng = np.random.default_rng(E)
+    x, b = many(rng, T, E, bias, 0.125)
+    _, ids, w = run(x, B.Router(E, K, kind), b, dtype=dtype)
+    check_some(x, ids, w, b, K, kind)
+
+
 def test_no_tokens_and_another_stream():
     router = B.Router(16, 2)
     empty = torch.empty((0, 16), device="cuda")

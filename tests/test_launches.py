@@ -171,6 +171,36 @@ for T, K, E in ((0, 8, 64), (256, 2, 16), (8192, 8, 128), (1024, 64, 4096), (102
     assert len(seen) == 2 * (1 + 1 + 1 + 3 + 2), sorted(seen)   # clear, one workgroup, added, spread, whole of two widths
 
 
+def test_routers_choose_by_lists_wherever_the_lanes_hold_their_experts(recorder):
+    """Up to 16 slots, up to 16 groups in a power of two and no softmax with a bias: 8 lanes a token from 16,384 tokens on where they hold the
+    experts (512) and the groups, 16 lanes up to 1,024; whatever the number of tokens, no such router takes the kernel of one wave a token."""
+    result = launch_recorder.run(recorder, r"""
+result = []
+for T in (1, 16383, 16384, 65536):
+    for E in (1, 64, 512, 513, 768, 1024, 1025, 4096):
+        for K in (1, 3, 8, 16, 17):
+            for groups in (1, 3, 8, 16, 32):
+                for score in (0, 1):
+                    for bias in (None, at(4)):
+                        if E % groups or K > E:
+                            continue
+                        r = B.hm_router(E, K, score, groups, groups, 1, 1, 1.0)
+                        rc = L.hm_route(at(1), 1, E, bias, T, ctypes.byref(r), at(2), at(3), None)
+                        one, = launched()
+                        result.append([T, E, K, groups, score, bias is not None, rc, one])
+""")
+    seen = set()
+    for T, E, K, groups, score, biased, rc, one in result:
+        lists = K <= 16 and groups in (1, 8, 16) and not (biased and score == 0) and E <= 1024
+        lanes = 8 if T >= 16384 and groups <= 8 and E <= 512 else 16
+        length = 2 if K <= 2 else 4 if K <= 4 else 8 if K <= 8 else 16
+        want = "route_lists_kernel<float, %d, %d>" % (lanes, length) if lists else "route_kernel<float>"
+        assert rc == 0 and one["name"] == want, (T, E, K, groups, score, biased, one["name"], want)
+        assert one["grid"][0] * (one["block"][0] // (lanes if lists else 64)) >= T and one["lds"] <= one["granted"]
+        seen.add(want)
+    assert len(seen) == 9
+
+
 def test_swap_tables_take_the_kernels_their_sizes_ask_for(recorder):
     """Matrix products with partial tables, with added ones, and atomics per slot with their tables in LDS and in memory."""
     result = launch_recorder.run(recorder, r"""
