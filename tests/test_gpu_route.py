@@ -153,6 +153,27 @@ def test_more_experts_than_eight_lanes_hold(T, E, K, kind, bias, dtype):
     check_some(x, ids, w, b, K, kind)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("renormalise", [True, False])
+@pytest.mark.parametrize("kind,bias", [("softmax", False), ("sigmoid", False), ("sigmoid", True)])
+@pytest.mark.parametrize("T,E,K,groups,top,best", [(16384, 64, 8, 1, 1, 1), (16385, 60, 1, 1, 1, 1), (20001, 128, 3, 2, 1, 2), (16384, 256, 8, 8, 4, 2),
+                                                  (17003, 96, 10, 8, 3, 2), (16390, 512, 16, 1, 1, 1), (16400, 40, 16, 4, 2, 1), (16384, 16, 2, 8, 2, 2),
+                                                  (16387, 255, 9, 1, 1, 1), (16384, 5, 4, 1, 1, 1)])
+def test_many_tokens(T, E, K, groups, top, best, kind, bias, renormalise, dtype):
+    """What goes by eight lanes a token: lists of each length, two slots a lane, groups of one lane and of more, rows of any alignment."""
+    rng = np.random.default_rng(T + E)
+    x, b = many(rng, T, E, bias, 0.125)
+    if groups > 1 and not bias:
+        x = grid(rng, T, E, span=1.5 if E == 16 else 3.0)   # group scores apart by more than rounding
+    elif groups == 1 and E > K:
+        x[::5, E - 1] = -np.inf
+    _, ids, w = run(x, B.Router(E, K, kind, groups, top, best, renormalise, 2.5), b, dtype=dtype, stride=(0, 1, 8)[E % 3])
+    check_some(x, ids, w, b, K, kind, groups=groups, top_groups=top, group_best=best, renormalise=renormalise, scale=2.5)
+    assert torch.all((ids >= 0) & (ids < E))
+    again = run(x[-17:], B.Router(E, K, kind, groups, top, best, renormalise, 2.5), b, dtype=dtype)
+    assert torch.equal(again[1], ids[-17:])   # 16 lanes a token choose alike
+
+
 def test_no_tokens_and_another_stream():
     router = B.Router(16, 2)
     empty = torch.empty((0, 16), device="cuda")
@@ -264,6 +285,45 @@ def test_gradient_of_the_weights(T, K, H, level, dtype):
         want[slot == rows - 1], bound[slot == rows - 1] = 0, 0
         assert np.all(np.abs(grad.cpu().numpy() - want) <= bound)
         assert B.hm_plan_status(plan)[0] == B.HM_ERR_CAPACITY
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,K,H", [(4097, 8, 512), (4101, 6, 1030), (4100, 9, 2049), (4099, 3, 4097), (4097, 8, 4608), (4097, 2, 520)])
+def test_gradient_of_many_tokens_weights(T, K, H, dtype):
+    """A wave to a token: rows of several steps, with a rest and without, slots in one piece and in several."""
+    E, nodes, ranks = 64, 2, 4
+    rng = np.random.default_rng(T + K + H)
+    ids = np.argsort(rng.random((T, E)), axis=1)[:, :K].astype(np.int32)
+    ids[rng.random((T, K)) < 0.1] = -1
+    plan = B.hm_plan(dev(ids), dev(np.full((T, K), 0.5, dtype=np.float32)), dev((np.arange(E) // 8).astype(np.int32)), nodes, ranks, B.HM_DEDUP_NONE)
+    status, rows = B.hm_plan_status(plan)
+    assert status == 0
+    g = torch.Generator(device="cuda")
+    g.manual_seed(H)
+    off = 1 if H % 2 else 0   # rows off a vector's alignment
+    flat = lambda n: torch.randn(n * H + off, generator=g, device="cuda").to(dtype)[off:].view(n, H)
+    gout, y, grad = flat(T), flat(rows), torch.full((T, K), float("nan"), device="cuda")
+    B.hm_combine_weight_grad(gout, y, plan, grad)
+    slot = plan.slot_row[:T * K].view(T, K).long()
+    for some in torch.arange(T, device="cuda").split(512):
+        row = slot[some]
+        a, b = gout[some].double()[:, None], torch.where((row >= 0)[:, :, None], y[row.clamp(min=0)].double(), 0.0)
+        want, size = (a * b).sum(dim=2), (a.abs() * b.abs()).sum(dim=2)
+        # as in test_gradient_of_the_weights: H / 64 additions in a lane and six after them, each rounds once
+        assert ((grad[some].double() - want).abs() <= (H / 64 + 24) * 2.0 ** -24 * size).all()
+    assert B.hm_plan_status(plan)[0] == 0
+
+
+@pytest.mark.parametrize("score,renormalise", [("softmax", False), ("softmax", True), ("sigmoid", True)])
+def test_gradient_of_the_logits_of_many_tokens(score, renormalise):
+    T, E, K = 20011, 60, 6
+    rng = np.random.default_rng(6)
+    x = grid(rng, T, E, span=4.0)
+    ids = np.argsort(-x, axis=1, kind="stable")[:, :K]
+    g = rng.standard_normal((T, K)).astype(np.float32)
+    got = back(x, ids, g, B.Router(E, K, score, renormalise=renormalise, scale=1.5))
+    want, size = R.route_backward(x, ids, g, score, renormalise, 1.5)
+    assert np.all(np.abs(got - want) <= RTOL * size + 1e-36)
 
 
 def test_the_weights_gradient_is_the_combines_derivative():
