@@ -18,10 +18,12 @@ from . import binding as hm
 class ExpertLayer:
     """gate [E, H] fp32; w13 [E, 2 F, H] and w2 [E, H, F], bf16 or fp32: the master weights, H a multiple of 512 (so that rows of
     8 bits and their scales are rows of 2-byte units).  quantize() lays the weights out in 8 bits, both ways round: call it again
-    after an optimizer step.  forward() keeps what backward() needs."""
+    after an optimizer step.  forward() keeps what backward() needs.  gone [E], bool: experts that no token may choose, say
+    those of a rank that is lost: their logits are -inf and their gradients 0, while the gate stays finite.  It may be set
+    between passes."""
 
-    def __init__(self, gate: torch.Tensor, w13: torch.Tensor, w2: torch.Tensor, router: hm.Router, bias=None):
-        self.gate, self.w13, self.w2, self.router, self.bias = gate, w13, w2, router, bias
+    def __init__(self, gate: torch.Tensor, w13: torch.Tensor, w2: torch.Tensor, router: hm.Router, bias=None, gone=None):
+        self.gate, self.w13, self.w2, self.router, self.bias, self.gone = gate, w13, w2, router, bias, gone
         self.E, self.H, self.F = w2.shape
         if self.E != router.E or self.E > 64 or self.H % 512:
             raise ValueError("at most 64 experts, as many as the router's, and rows of a multiple of 512 values")
@@ -54,6 +56,8 @@ class ExpertLayer:
         """x [T, H] bf16 -> [T, H] bf16."""
         T, K = x.shape[0], self.router.K
         self.x, self.logits = x, x.float() @ self.gate.t()
+        if self.gone is not None:
+            self.logits.masked_fill_(self.gone, float("-inf"))
         self.ids = torch.empty((T, K), dtype=torch.int32, device=x.device)
         self.weights = torch.empty((T, K), dtype=torch.float32, device=x.device)
         hm.hm_route(self.logits, self.router, self.ids, self.weights, self.bias)

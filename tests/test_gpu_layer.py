@@ -59,6 +59,27 @@ def test_layer_and_its_gradients(T, E, K, H, F, score, how):
         assert (a - b).norm() <= bound, (name, float((a - b).norm() / b.norm()))
 
 
+@pytest.mark.parametrize("score,how", [("softmax", {}), ("sigmoid", dict(scale=2.5)), ("sigmoid", dict(renormalise=False))])
+def test_gradients_where_experts_are_gone(score, how):
+    """Three of eight experts are left to four slots: every gradient is finite and right for those, and 0 for the others."""
+    T, E, K, H, F, left = 90, 8, 4, 512, 64, 3
+    layer = L.make_layer(E, K, H, F, score, seed=5, **how)
+    layer.gone = torch.arange(E, device="cuda") >= left
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    x, gout = (torch.randn((T, H), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    out = layer.forward(x)
+    grads = layer.backward(gout)
+    assert (layer.ids >= 0).sum() == T * left and int(layer.ids.max()) < left
+    want = reference(layer, x, gout)
+    for name, a, b in zip(("out", "x", "gate", "w13", "w2"), (out, *grads), want[:5]):   # bounds as above
+        a = a.double().cpu()
+        assert torch.isfinite(a).all(), name
+        bound = 3 * 0.05 * want[5] if name == "gate" else 0.12 * b.norm()
+        assert (a - b).norm() <= bound, (name, float((a - b).norm() / b.norm()))
+        assert name in ("out", "x") or not a[left:].any()
+
+
 def test_dropped_slots_leave_rows_unused():
     """Experts of a rank that is gone: their logits are -inf, tokens that find too few are left with fewer slots."""
     layer = L.make_layer(8, 4, 512, 64)
