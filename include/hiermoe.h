@@ -448,7 +448,8 @@ hm_status hm_swap_apply(int32_t *expert_to_rank, int32_t E, const int32_t *best_
  * no score above 0 to divide by all weights are 0.  Scores are fp32; a logistic score below 2^-126 may be 0.
  *   logits: dtype HM_F32 or HM_BF16, row t from element t*ld on (ld >= E).  bias [E] fp32 or NULL.
  * Limits: E <= 4096, K <= 64, K <= the experts of top_groups groups (else HM_ERR_SHAPE, as for top_groups > groups,
- * groups not dividing E, group_best other than 1 or 2 or above the experts of a group).
+ * groups not dividing E, group_best other than 1 or 2 or above the experts of a group), T <= 2^26 - 4 (up to 2^28 - 16 where K <= 16,
+ * E <= 1024, groups are a power of two up to 16 and no softmax has a bias).
  */
 typedef enum { HM_BF16 = 0, HM_F32 = 1, HM_BF16_SUM_F32 = 2 /* results of products only: bf16 from sums in fp32 */ } hm_dtype;
 typedef enum { HM_SCORE_SOFTMAX = 0, HM_SCORE_SIGMOID = 1 } hm_score;
@@ -471,7 +472,7 @@ hm_status hm_route(const void *logits, hm_dtype dtype, int64_t ld, const float *
  *     softmax, normalised  dx_k = scale u_k (g_k - sum_S g u),  u = s / sum_S s                  k in S
  * and 0 for the others and for experts hm_route never chooses.  The ids of a token are distinct, as hm_route writes
  * them.  groups, top_groups and group_best do not matter.  grad_logits has the dtype of the logits, row t from element
- * t*grad_ld on; fp32 arithmetic.  Together with hm_combine_weight_grad this is the router's way back.
+ * t*grad_ld on; fp32 arithmetic; T <= 2^26 - 4.  Together with hm_combine_weight_grad this is the router's way back.
  */
 hm_status hm_route_backward(const void *logits, hm_dtype dtype, int64_t ld, const int32_t *topk_ids,
                             const float *grad_weights, int32_t T, const hm_router *router /* host */,
@@ -482,7 +483,7 @@ hm_status hm_route_backward(const void *logits, hm_dtype dtype, int64_t ld, cons
  *     grad_weights[t,k] = sum_h gout[t,h] * y[slot_row[t,k], h],   fp32 accumulation,
  * 0 for dropped slots and for rows outside [0,y_rows) (the latter flagged HM_ERR_CAPACITY).  gout [T,H] and y [y_rows,H]
  * are both bf16 or both fp32 (dtype).  Uses plan->slot_row, status.  The slots of a token that share a row get the same
- * gradient.  Any H and any alignment of the elements.
+ * gradient.  Any H and any alignment of the elements; T <= 2^26 - 4.
  */
 hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype, int64_t y_rows, int32_t T, int32_t K,
                                  int32_t H, const hm_plan_out *plan, float *grad_weights, void *hip_stream);

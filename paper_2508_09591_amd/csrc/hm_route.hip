@@ -596,6 +596,8 @@ static void launch_lists(const RouteParams &p, hipStream_t stream) {
   const int64_t per_block = kRouteThreads / L;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((p.T + per_block - 1) / per_block)), dim3(kRouteThreads), 0, stream, p, lanes_per_group, run);
 }
+// Whether a launch has threads for T tokens of so many: it has less than 2^32, in whole workgroups.
+static bool threads_suffice(int64_t T, int each) { return T * each <= (1LL << 32) - kRouteThreads; }
 // Tokens of a workgroup whose rows of `floats` fit 64 KiB.
 static int tokens_per_group(int floats) {
   int n = kRouteWaves;
@@ -617,7 +619,9 @@ extern "C" hm_status hm_route(const void *logits, hm_dtype dtype, int64_t ld, co
   if (T == 0) return HM_OK;
   if (!logits || !topk_ids || !topk_weights) return HM_ERR_NULL;
   const RouteParams p = {logits, ld, bias, T, *router, topk_ids, topk_weights};
-  if (const int lanes = list_lanes(p.r, bias != nullptr, T)) {
+  const int lanes = list_lanes(p.r, bias != nullptr, T);
+  if (!threads_suffice(T, lanes ? lanes : kWave)) return HM_ERR_SHAPE;
+  if (lanes) {
     const hipStream_t stream = (hipStream_t)hip_stream;
     if (dtype == HM_BF16) lanes == 8 ? launch_lists<uint16_t, 8>(p, stream) : launch_lists<uint16_t, 16>(p, stream);
     else lanes == 8 ? launch_lists<float, 8>(p, stream) : launch_lists<float, 16>(p, stream);
@@ -637,7 +641,7 @@ extern "C" hm_status hm_route_backward(const void *logits, hm_dtype dtype, int64
   if (bad != HM_OK) return bad;
   const hm_status shape = hm_check_tk(T, router->K);
   if (shape != HM_OK) return shape;
-  if (!dtype_known(dtype) || ((ld < router->E || grad_ld < router->E) && T > 1)) return HM_ERR_SHAPE;
+  if (!dtype_known(dtype) || ((ld < router->E || grad_ld < router->E) && T > 1) || !threads_suffice(T, kWave)) return HM_ERR_SHAPE;
   if (T == 0) return HM_OK;
   if (!logits || !topk_ids || !grad_weights || !grad_logits) return HM_ERR_NULL;
   const RouteBackParams p = {logits, ld, grad_ld, topk_ids, grad_weights, T, *router, grad_logits};
@@ -654,7 +658,7 @@ extern "C" hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_
   if (!plan || !plan->slot_row || !plan->status) return HM_ERR_NULL;
   const hm_status shape = hm_check_tk(T, K);
   if (shape != HM_OK) return shape;
-  if (!dtype_known(dtype) || H < 1 || y_rows < 0) return HM_ERR_SHAPE;
+  if (!dtype_known(dtype) || H < 1 || y_rows < 0 || !threads_suffice(T, kWave)) return HM_ERR_SHAPE;
   if (T == 0) return HM_OK;
   if (!gout || !grad_weights || (!y && y_rows > 0)) return HM_ERR_NULL;
   const WeightGradParams p = {gout, y, y_rows, plan->slot_row, T, K, H, grad_weights, plan->status};

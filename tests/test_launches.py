@@ -201,6 +201,34 @@ for T in (1, 16383, 16384, 65536):
     assert len(seen) == 9
 
 
+def test_router_calls_of_more_tokens_than_a_launch_has_threads_for(recorder):
+    """A launch has less than 2^32 threads: what would need more is refused as a shape, before any launch; the last size that fits is made."""
+    result = launch_recorder.run(recorder, _ROWS + r"""
+result = []
+def note(what, limit, call):
+    for T in (limit - 1, limit):
+        rc = call(T)
+        result.append([what, T == limit, rc, launched()])
+def route(T, E, K, groups=1):
+    return L.hm_route(at(1), 1, E, None, T, ctypes.byref(B.hm_router(E, K, 0, groups, groups, 1, 1, 1.0)), at(2), at(3), None)
+def back(T, E):
+    return L.hm_route_backward(at(1), 1, E, at(2), at(3), T, ctypes.byref(B.hm_router(E, 1, 0, 1, 1, 1, 1, 1.0)), at(4), E, None)
+note("lists of 8 lanes", (1 << 29) - 31, lambda T: route(T, 8, 1))
+note("lists of 16 lanes", (1 << 28) - 15, lambda T: route(T, 600, 2))
+note("a wave a token", (1 << 26) - 3, lambda T: route(T, 40, 17))
+note("a wave a token, groups", (1 << 26) - 3, lambda T: route(T, 9, 1, 3))
+note("gradient of the logits", (1 << 26) - 3, lambda T: back(T, 8))
+note("gradient of the logits, rows that fill LDS", (1 << 26) - 3, lambda T: back(T, 4096))
+for dtype in (0, 1):
+    for H in (8, 5000):
+        note("gradient of the weights", (1 << 26) - 3, lambda T: L.hm_combine_weight_grad(at(1), at(2), dtype, T, T, 2, H, plan(T, 2, 2, None), at(5), None))
+""")
+    assert len(result) == 20
+    for what, beyond, rc, launches in result:
+        assert (rc, len(launches)) == ((-2, 0) if beyond else (0, 1)), (what, beyond, rc)
+        assert all(k["grid"][0] * k["block"][0] < 1 << 32 for k in launches), what
+
+
 def test_swap_tables_take_the_kernels_their_sizes_ask_for(recorder):
     """Matrix products with partial tables, with added ones, and atomics per slot with their tables in LDS and in memory."""
     result = launch_recorder.run(recorder, r"""
