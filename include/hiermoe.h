@@ -506,7 +506,9 @@ hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype
  * are data errors: no access leaves the buffers, the results are unspecified.
  *
  * x: dtype HM_F32 or HM_BF16, row r from element r*ld on, any alignment of the elements; fastest with whole 16-byte
- * vectors; calls of more than about 2^34 values are refused (HM_ERR_SHAPE).  hm_quantize_weights takes dense [experts, N, C]; with qt and scale_t it also writes the transposed weights
+ * vectors.  Limits: C and N up to 2^20, experts and segments up to 1024; hm_quantize_rows: rows * ceil(C / 512) <= 2^25;
+ * hm_quantize_columns: rows <= 2^31-1 - 128 * segments, (rows / 128 + segments) * ceil(C / 64) <= 2^23; beyond HM_ERR_SHAPE.
+ * hm_quantize_weights takes dense [experts, N, C]; with qt and scale_t it also writes the transposed weights
  * [experts, C, up(N,128)], [experts, ceil(C/128), up(N,512)/128]: the same values, for the gradient of the rows.
  */
 hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld, int64_t rows, int32_t C, uint8_t *q, uint8_t *scale,
@@ -533,8 +535,8 @@ hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, in
  * hm_expert_matmul_dw -- the gradient of the weights:
  *     dw[e,n,h] = sum over the rows r of segment e of gy[r,n] x[r,h],
  * gy (C = N) and x (C = H) in the layout `columns`; dw [experts,N,H] of dw_dtype, zeros for an expert without rows.
- * Limits: experts <= 1024, N and H up to 2^20, rows * experts < 2^35 and rows <= 2^31-1 - 128 * experts, about 2^37 results (dw:
- * rows / 128 + experts < 2^17); beyond HM_ERR_SHAPE.
+ * Limits: experts <= 1024, N and H up to 2^20, rows <= 2^31-1 - 128 * experts; hm_expert_matmul: rows * experts < 2^35 and
+ * (rows / 128 + experts) * ceil(N / 128) <= 2^23 - 8; hm_expert_matmul_dw: rows / 128 + experts < 2^17; beyond HM_ERR_SHAPE.
  */
 hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, const uint8_t *w, const uint8_t *w_scale,
                            const int32_t *offsets, int32_t experts, int64_t rows, int32_t N, int32_t H, void *out,

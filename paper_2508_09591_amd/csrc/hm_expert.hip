@@ -493,11 +493,13 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   const ProductParams p = {x, x_scale, w, w_scale, offsets, experts, (int32_t)rows, N, H, out};
   // Few rows: up to four an expert, or a strip's 16 in all (us, thin against tiles: 32 experts of 4,096 x 7,168, 32 rows 93 and 128,
   // 128 rows 164 and 162, 512 rows 292 and 164; one expert, 16 rows 9.1 and 14.1, 40 rows 20.4 and 14.3).
-  if (rows <= 4LL * experts || rows <= 16) {
-    const int64_t tiles = (rows / 16 + (rows < experts ? rows : experts)) * ((N + 15) / 16) + 8;
-    if (tiles > (1 << 23)) return HM_ERR_SHAPE;
+  // More strips than a launch has workgroups go by tiles, with the same sums.
+  const bool few = rows <= 4LL * experts || rows <= 16;
+  const int64_t strips = (rows / 16 + (rows < experts ? rows : experts)) * ((N + 15) / 16) + 8;
+  if (few && out_dtype == HM_BF16) out_dtype = HM_BF16_SUM_F32;
+  if (few && strips <= 1 << 23) {
     const auto kernel = out_dtype == HM_F32 ? thin_product_kernel<float> : thin_product_kernel<uint16_t>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(kThinWaves * kWave), 0, (hipStream_t)hip_stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)strips), dim3(kThinWaves * kWave), 0, (hipStream_t)hip_stream, p);
     return hm_launch_status();
   }
   const bool large = out_dtype == HM_BF16 && rows / experts >= 512 && (rows / 256 + experts / 2) * ((N + 255) / 256) >= 400;

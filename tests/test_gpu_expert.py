@@ -305,8 +305,8 @@ def test_full_sums_of_columns(counts, N, H, dtype):
 
 def test_what_the_units_products_drop():
     """bf16 results of tiles where 8 columns are 1,000 times as large as the others.  Each of the 64 products of a step loses
-    less than 2^-13 of the step's largest, either way alike: sqrt(64 / 3) 2^-13 = 2^-10.8 of it, and steps add as their squares; rounding
-    adds at most 2^-9 of a result.  Taken over a matrix, where such sums are sharp."""
+    less than 2^-13 of the step's largest, either way alike: sqrt(64 / 3) 2^-13 = 2^-10.8 of it, and steps add as their squares; rounding,
+    evenly within 2^-8 of a result's power of two, adds 2^-9.2 of their norm.  Taken over a matrix, where such sums are sharp."""
     rows, N, H = 2048, 512, 2048
     g = torch.Generator(device="cuda")
     g.manual_seed(3)
@@ -560,6 +560,27 @@ def test_parts_of_blocks_are_refused_before_any_launch(width, monkeypatch):
         with pytest.raises(ValueError, match="whole blocks"):
             B.hm_expert_matmul(*operands, off, out, stream=stream)
     assert taken == [None]
+
+
+def test_few_rows_of_more_strips_than_workgroups():
+    """As many columns that a launch has no workgroups for strips of 16 x 16, weights beyond 2^32 bytes: sums in 32 bits all the same."""
+    E, N, H = 1024, 131077, 128
+    rows = 2 * E
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    w8 = torch.randint(0, 0x7F, (E, N, H), generator=g, dtype=torch.uint8, device="cuda").view(F8)
+    x8 = torch.randint(0, 0x7F, (rows, H), generator=g, dtype=torch.uint8, device="cuda").view(F8)
+    xs = torch.randint(120, 135, (rows, 4), generator=g, dtype=torch.uint8, device="cuda")
+    ws = torch.randint(115, 130, (E, R.up(N, 128) // 128, 4), generator=g, dtype=torch.uint8, device="cuda")
+    out, half = (torch.full((rows, N), -77.0, dtype=dtype, device="cuda") for dtype in (torch.float32, torch.bfloat16))
+    for o in (out, half):
+        B.hm_expert_matmul(x8, xs, w8, ws, dev(np.arange(0, rows + 1, 2, dtype=np.int32)), o)
+    assert torch.equal(half, out.to(torch.bfloat16))
+    a = gpu_values(x8, xs[:, :1])
+    for e in (0, 1, 500, 1023):
+        b = gpu_values(w8[e], ws[e].repeat_interleave(128, dim=0)[:N, :1])
+        want = a[2 * e:2 * e + 2] @ b.t().contiguous()   # of numbers of one sign, so that a sum's error is its own: 2^-24 for each of 128 terms
+        assert ((out[2 * e:2 * e + 2].double() - want).abs() <= 136 * 2.0 ** -24 * want).all(), e
 
 
 def test_results_do_not_depend_on_what_ran_before():

@@ -229,6 +229,52 @@ for dtype in (0, 1):
         assert all(k["grid"][0] * k["block"][0] < 1 << 32 for k in launches), what
 
 
+def test_products_up_to_their_limit_are_launched(recorder):
+    """(rows / 128 + experts) * ceil(N / 128) up to 2^23 - 8 for every number of rows, also where few rows have more strips of 16 than a
+    launch may have workgroups; beyond, HM_ERR_SHAPE without a launch."""
+    result = launch_recorder.run(recorder, r"""
+result = []
+for dtype in (0, 1, 2):
+    for E in (1, 2, 32, 100, 1024):
+        for rows in (1, 16, 17, 4 * E, 4 * E + 1, 5000, 1 << 20, 1 << 25):
+            for N in (1, 4096, 131072, 1 << 20):
+                if rows * E < 1 << 35:
+                    rc = L.hm_expert_matmul(at(1), at(2), at(3), at(4), at(5), E, rows, N, 256, at(6), dtype, None)
+                    result.append([dtype, E, rows, N, rc, launched()])
+""")
+    seen = set()
+    for dtype, E, rows, N, rc, launches in result:
+        tiles = (rows // 128 + E) * -(-N // 128)
+        if tiles > (1 << 23) - 8:
+            assert (rc, launches) == (-2, []) or rc == 0, (dtype, E, rows, N, rc)   # tiles of 256 may fit where those of 128 would not
+        else:
+            assert rc == 0 and len(launches) == 1, (dtype, E, rows, N, rc)
+        for k in launches:
+            assert k["grid"][0] <= 1 << 23 and k["grid"][1:] == [1, 1]
+            seen.add(k["name"])
+    assert any(n.startswith("thin") for n in seen) and len(seen) == 2 + 1 + 3 + 3, sorted(seen)   # few rows; tiles of 256, of 128, of 64
+
+
+def test_values_in_8_bits_up_to_their_limit_are_launched(recorder):
+    """Rows: rows * ceil(C / 512) up to 2^25; columns: (rows / 128 + segments) * ceil(C / 64) up to 2^23; weights of any size."""
+    result = launch_recorder.run(recorder, r"""
+result = []
+for dtype in (0, 1):
+    for rows, C, fits in ((1 << 25, 512, 1), ((1 << 25) + 1, 512, 0), (1 << 25, 1, 1), (1 << 24, 513, 1), ((1 << 24) + 1, 513, 0), (1 << 14, 1 << 20, 1)):
+        rc = L.hm_quantize_rows(at(1), dtype, C, rows, C, at(2), at(3), None)
+        result.append(["rows", fits, rc, launched()])
+    for rows, S, C, fits in ((128 * ((1 << 23) - 1), 1, 64, 1), (1 << 30, 1, 64, 0), (127, 512, 1 << 20, 1), (127, 513, 1 << 20, 0)):
+        rc = L.hm_quantize_columns(at(1), dtype, C, at(4), S, rows, C, at(2), at(3), None)
+        result.append(["columns", fits, rc, launched()])
+    for E, N, C in ((1024, 1 << 20, 1 << 20), (1024, 1, 1 << 20), (1, 1 << 20, 1)):
+        rc = L.hm_quantize_weights(at(1), dtype, E, N, C, at(2), at(3), at(5), at(6), None)
+        result.append(["weights", 1, rc, launched()])
+""")
+    for what, fits, rc, launches in result:
+        assert (rc, len(launches)) == ((0, 1) if fits else (-2, 0)), (what, fits, rc, launches)
+        assert all(k["grid"][0] * k["block"][0] < 1 << 32 and max(k["grid"][1:]) < 65536 for k in launches), (what, launches)
+
+
 def test_swap_tables_take_the_kernels_their_sizes_ask_for(recorder):
     """Matrix products with partial tables, with added ones, and atomics per slot with their tables in LDS and in memory."""
     result = launch_recorder.run(recorder, r"""
