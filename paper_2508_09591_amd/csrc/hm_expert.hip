@@ -94,7 +94,8 @@ struct Slice<true> {   // 16 values: two instructions, a quarter of a step
   i32x4 v;
   __device__ __forceinline__ void read(const uint8_t *lds, const uint32_t (&at)[4], int fragment, int part) { v = *(const i32x4 *)(lds + at[part] + fragment); }
   // Eight values as bf16, times their block's power of two, of which the conversion takes the exponent (code 0 too is 2^-127).  Exact
-  // down to the least subnormal, 2^-133: values are multiples of 2^-9, so that codes from 3 on lose nothing.
+  // down to the least subnormal, 2^-133: values are multiples of 2^-9, so that codes from 3 on lose nothing.  2^128, to which what
+  // lies next to fp32's largest number is rounded (256 under code 247), is infinite.
   static __device__ __forceinline__ bf16x8 widen(int lo, int hi, uint32_t code) {
     const float power = __builtin_bit_cast(float, (code & 0xFFu) << 23);
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true);

@@ -341,6 +341,36 @@ def test_the_least_scales(low, rows, dtype):
     assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound(want, size, largest, H, dtype) + lost)
 
 
+@pytest.mark.parametrize("full", [False, True])
+@pytest.mark.parametrize("rows", [8, 300])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_the_largest_scales(rows, dtype, full):
+    """Codes 246 with any value and 247 with values up to 240 hold numbers below 2^128 and lose nothing; from 2^128 on values of sums in
+    32 bits are infinite, which the numbers next to fp32's and bf16's largest are rounded to."""
+    N, H = 64, 256
+    rng = np.random.default_rng(rows)
+    x, w = operand(rng, rows, H), operand(rng, 1, N, H)
+    x[:, 128:] = np.where((x[:, 128:] & 0x7F) > 0x77, 0, x[:, 128:])   # 0x77: 240
+    xs, ws = np.full((rows, 4), 246, dtype=np.uint8), np.full((1, 1, 4), 20, dtype=np.uint8)
+    xs[:, 1] = 247
+    off = dev(np.array([0, rows], dtype=np.int32))
+    out = torch.zeros((rows, N), dtype=dtype, device="cuda")
+    B.hm_expert_matmul(f8(x).cuda(), dev(xs), f8(w).cuda(), dev(ws), off, out, full_sums=full)
+    a = R.row_values(f8(x).float().numpy().astype(np.float64), xs.astype(np.int64))
+    b = R.weight_values(f8(w).float().numpy().astype(np.float64), ws.astype(np.int64))[0]
+    want, size, largest = R.product(a, b, H // 128)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound(want, size, largest, H, dtype))
+    lowest = np.full((rows, H), np.finfo(np.float32).min, dtype=np.float32)
+    x8 = B.hm_quantize_rows(dev(lowest), *B.alloc_rows8(rows, H))
+    assert (x8[1][:, :2] == 247).all() and (x8[0].float() == -256).all()
+    w8 = B.hm_quantize_weights(torch.full((1, N, H), 2.0 ** -20, device="cuda"), *B.alloc_weights8(1, N, H))
+    B.hm_expert_matmul(*x8, *w8, off, out, full_sums=full)
+    if dtype == torch.float32 or full or rows <= 16:
+        assert (out == float("-inf")).all()
+    else:
+        assert (out == -2.0 ** (128 - 20 + 8)).all()
+
+
 def test_offsets_that_are_wrong_stay_inside():
     """Descending offsets and offsets outside the rows: nothing outside the outputs is written."""
     rows, N, H = 50, 40, 128
