@@ -455,11 +455,13 @@ static hm_status check_products(const void *a, const void *as, const void *b, co
 }
 
 // Rows and columns of a tile, from the tiles that there would be of 256 and of 128.  256 read the operands least often, but
-// a CU holds one, so they need 400 and segments that fill them (us, 256 against 128: 16,384 rows, 16 experts, 1,536 x 2,048 57.0 and
-// 60.5; 8,192, 8, 4,096 x 7,168 236 and 276; 8,192, 32, 2,048 x 2,048 56.3 and 48.2); with fp32 results, bound by products of 16 bits
-// and by widening, 128 are as fast or faster, two to a CU (8,192, 8, 4,096 x 7,168 453 and 416), but for the gradient of the weights
-// (32,768, 16, 1,536 x 2,048 182 and 195).  Tiles of 64 for few: 8 rows, 32, 4,096 x 7,168 35.3 and 36.0 with 128; 1,000, 1,
-// 500 x 700 7.1 and 10.5; 1,024, 8, 2,048 x 2,048 13.6 and 14.2; but 2,048, 32, 2,048 x 2,048 (512 tiles of 128) 30.0 and 24.3.
+// a CU holds one, so they need 400 and segments that fill them (us, 256 against 128: 16,384 rows, 16 experts, 1,536 x 2,048
+// 60.7 and 75.9; 8,192, 8, 4,096 x 7,168 241 and 282; 8,192, 32, 2,048 x 2,048 58.6 and 62.5, but 56.3 and 48.2 where operands stay
+// in the last-level cache); with fp32 sums, bound by products of 16 bits and by widening, 128 are as fast or faster, two to a
+// CU (8,192, 8, 4,096 x 7,168 453 and 416), but for the gradient of the weights (32,768, 16, 1,536 x 2,048 191 and 207).  Tiles
+// of 64 for few (64 against 128): 300 rows, 1, 4,096 x 7,168 39.3 and 44.0; 1,000, 1, 500 x 700 8.9 and 11.8; 2,048, 4,
+// 1,024 x 2,048 14.8 and 15.9; 1,024, 8, 2,048 x 2,048 17.5 and 16.9; but 4,096, 2, 1,000 x 2,056 (256 tiles of 128) 27.5 and
+// 19.4, 2,048, 32, 2,048 x 2,048 (512) 41.5 and 28.8.  Measured with operands in turn, so that they come from memory.
 static int tile_side(bool large, int64_t tiles128) { return large ? 256 : tiles128 >= 200 ? 128 : 64; }
 
 template <int FQ, int FP, int WQ, int WP, bool DW>
@@ -492,10 +494,12 @@ extern "C" hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, 
   if (rows == 0) return HM_OK;
   if (rows * experts >= 1LL << 35) return HM_ERR_SHAPE;   // strips of 16 rows are counted in 32 bits, also where offsets overlap
   const ProductParams p = {x, x_scale, w, w_scale, offsets, experts, (int32_t)rows, N, H, out};
-  // Few rows: up to four an expert, or a strip's 16 in all (us, thin against tiles: 32 experts of 4,096 x 7,168, 32 rows 93 and 128,
-  // 128 rows 164 and 162, 512 rows 292 and 164; one expert, 16 rows 9.1 and 14.1, 40 rows 20.4 and 14.3).
+  // Few rows: up to four an expert, or 32 in all (us, strips against tiles with sums in 32 bits and in the unit's 8-bit products, operands
+  // from memory: 32 experts of 4,096 x 7,168, 32 rows 94, 137 and 126; 128 rows 165, 212 and 158; 256 rows 190, 213 and
+  // 158; 32 of 2,048 x 2,048, 128 rows 34, 33 and 27; one of 4,096 x 7,168, 32 rows 17.7, 43 and 38; 64 rows 28.8, 43 and 38; one of
+  // 7,168 x 2,048, 32 rows 11.9, 15 and 13; 48 rows 15.8, 15 and 13).
   // More strips than a launch has workgroups go by tiles, with the same sums.
-  const bool few = rows <= 4LL * experts || rows <= 16;
+  const bool few = rows <= 4LL * experts || rows <= 32;
   const int64_t strips = (rows / 16 + (rows < experts ? rows : experts)) * ((N + 15) / 16) + 8;
   if (few && out_dtype == HM_BF16) out_dtype = HM_BF16_SUM_F32;
   if (few && strips <= 1 << 23) {

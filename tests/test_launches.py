@@ -255,6 +255,28 @@ for dtype in (0, 1, 2):
     assert any(n.startswith("thin") for n in seen) and len(seen) == 2 + 1 + 3 + 3, sorted(seen)   # few rows; tiles of 256, of 128, of 64
 
 
+def test_products_take_the_kernel_their_sizes_ask_for(recorder):
+    """Strips for up to 32 rows or four an expert; tiles of 64, 128 or, for the unit's 8-bit products, 256; sums as the result's type says."""
+    result = launch_recorder.run(recorder, r"""
+result = []
+for dtype in (0, 1, 2):
+    for E, rows, N, side in ((1, 32, 4096, 0), (1, 33, 4096, 64), (8, 32, 2048, 0), (8, 33, 2048, 64), (32, 128, 4096, 0), (32, 129, 4096, 128), (2, 4096, 1000, 128),
+                             (4, 2048, 1024, 64), (16, 16384, 1536, 256), (32, 8192, 2048, 128), (32, 65536, 4096, 256)):
+        rc = L.hm_expert_matmul(at(1), at(2), at(3), at(4), at(5), E, rows, N, 2048, at(6), dtype, None)
+        result.append([dtype, False, side, rc, launched()[0]["name"]])
+    for E, N, H, side in ((16, 1536, 2048, 256), (8, 512, 1024, 128), (4, 512, 512, 64)):
+        rc = L.hm_expert_matmul_dw(at(1), at(2), at(3), at(4), at(5), E, 4096, N, H, at(6), dtype, None)
+        result.append([dtype, True, side, rc, launched()[0]["name"]])
+""")
+    shape = {64: "2, 1, 1, 2", 128: "2, 2, 2, 2", 256: "4, 4, 2, 2"}
+    for dtype, dw, side, rc, name in result:
+        out, full = ("float", "true") if dtype == 1 else ("unsigned short", "true" if dtype == 2 else "false")
+        if side == 256 and full == "true" and not dw:
+            side = 128
+        want = "thin_product_kernel<%s>" % out if side == 0 else "product_kernel<%s, %s, %s, %s>" % (shape[side], "true" if dw else "false", full, out)
+        assert rc == 0 and name == want, (dtype, dw, side, name, want)
+
+
 def test_values_in_8_bits_up_to_their_limit_are_launched(recorder):
     """Rows: rows * ceil(C / 512) up to 2^25; columns: (rows / 128 + segments) * ceil(C / 64) up to 2^23; weights of any size."""
     result = launch_recorder.run(recorder, r"""
