@@ -7,8 +7,9 @@
  * send list in which every token appears at most once (the group-OR of Eq.(7)), packs the bf16
  * token rows into per-destination send buffers, and merges expert outputs coming back in that
  * layout with the router weights ("AlltoAll Combine", Section II-B).  Destinations are index
- * partitions of one buffer; the exchange itself is not part of the library.  In front of the plan stands the router (hm_route), between
- * dispatch and combine the experts' products in 8 bits (hm_expert_matmul), both with their gradients.
+ * partitions of one buffer; the exchange itself is not part of the library.  In front of the plan stands the router
+ * (hm_route), between dispatch and combine the experts' products in 8 bits (hm_expert_matmul), both with their
+ * gradients.
  *
  * Conventions
  *   - Unless marked "host", every pointer is a DEVICE pointer into memory the caller owns.
@@ -213,9 +214,9 @@ hm_status hm_combine(const void *y_bf16, int64_t y_rows, const float *topk_weigh
  * no cap).  weights_from_plan != 0 asks about the topk_weights == NULL form.
  * For tests and tuning: it shows what plan->expected_rows / max_rows_per_token select.  With the
  * caller's weights only expected_rows counts, and T and the bytes of a row too: H counts elements
- * of two bytes, so ask with 2 H for hm_combine_f32.  (Narrow rows in the topk_weights == NULL form, and rows that are few,
- * short or no whole 16-byte vectors in either, may take a kernel of a lane per vector or per
- * element; those have no such choice.)
+ * of two bytes, so ask with 2 H for hm_combine_f32.  (Narrow rows in the topk_weights == NULL form, and rows that are
+ * few, short or no whole 16-byte vectors in either, may take a kernel of a lane per vector or per element; those have
+ * no such choice.)
  */
 hm_status hm_combine_launch_shape(int32_t T, int32_t K, int32_t H, const hm_plan_out *plan, int32_t weights_from_plan,
                                   int32_t *vectors_per_lane /* host */, int32_t *rows_in_flight /* host */,
@@ -323,8 +324,8 @@ hm_status hm_plan_mapped(const int32_t *row_ids, const float *row_weights, const
  * row it returns for a received token is the weight-normalised mixture of what came back for
  * that token's slots,
  *     out[i,:] = bf16( (sum_k w[i,k] * y[slot_row[i,k], :]) / (sum_k w[i,k]) ),   valid slots only,
- * fp32 accumulation, then a multiply by the fp32 reciprocal of the weight sum.  With these mixtures as the packed-layout y of the
- * previous hop, hm_combine at the source yields sum_k w_k f_k(x) (Section II-A).  A row without
+ * fp32 accumulation, then a multiply by the fp32 reciprocal of the weight sum.  With these mixtures as the
+ * packed-layout y of the previous hop, hm_combine at the source yields sum_k w_k f_k(x) (Section II-A).  A row without
  * a valid slot gives zeros.  Arguments as hm_combine (T = number of received rows).
  */
 hm_status hm_combine_mix(const void *y_bf16, int64_t y_rows, const float *row_weights, int32_t T, int32_t K,
@@ -448,10 +449,14 @@ hm_status hm_swap_apply(int32_t *expert_to_rank, int32_t E, const int32_t *best_
  * no score above 0 to divide by all weights are 0.  Scores are fp32; a logistic score below 2^-126 may be 0.
  *   logits: dtype HM_F32 or HM_BF16, row t from element t*ld on (ld >= E).  bias [E] fp32 or NULL.
  * Limits: E <= 4096, K <= 64, K <= the experts of top_groups groups (else HM_ERR_SHAPE, as for top_groups > groups,
- * groups not dividing E, group_best other than 1 or 2 or above the experts of a group), T <= 2^26 - 4 (up to 2^28 - 16 where K <= 16,
- * E <= 1024, groups are a power of two up to 16 and no softmax has a bias).
+ * groups not dividing E, group_best other than 1 or 2 or above the experts of a group), T <= 2^26 - 4 (up to 2^28 - 16
+ * where K <= 16, E <= 1024, groups are a power of two up to 16 and no softmax has a bias).
  */
-typedef enum { HM_BF16 = 0, HM_F32 = 1, HM_BF16_SUM_F32 = 2 /* results of products only: bf16 from sums in fp32 */ } hm_dtype;
+typedef enum {
+  HM_BF16 = 0,
+  HM_F32 = 1,
+  HM_BF16_SUM_F32 = 2 /* results of hm_expert_matmul and hm_expert_matmul_dw only: bf16 from sums in fp32 */
+} hm_dtype;
 typedef enum { HM_SCORE_SOFTMAX = 0, HM_SCORE_SIGMOID = 1 } hm_score;
 typedef struct {
   int32_t E, K;
@@ -481,9 +486,9 @@ hm_status hm_route_backward(const void *logits, hm_dtype dtype, int64_t ld, cons
 /*
  * hm_combine_weight_grad -- gradient of hm_combine's output for the router weights:
  *     grad_weights[t,k] = sum_h gout[t,h] * y[slot_row[t,k], h],   fp32 accumulation,
- * 0 for dropped slots and for rows outside [0,y_rows) (the latter flagged HM_ERR_CAPACITY).  gout [T,H] and y [y_rows,H]
- * are both bf16 or both fp32 (dtype).  Uses plan->slot_row, status.  The slots of a token that share a row get the same
- * gradient.  Any H and any alignment of the elements; T <= 2^26 - 4.
+ * 0 for dropped slots and for rows outside [0,y_rows) (the latter flagged HM_ERR_CAPACITY).  gout [T,H] and y
+ * [y_rows,H] are both bf16 or both fp32 (dtype).  Uses plan->slot_row, status.  The slots of a token that share a row
+ * get the same gradient.  Any H and any alignment of the elements; T <= 2^26 - 4.
  */
 hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype, int64_t y_rows, int32_t T, int32_t K,
                                  int32_t H, const hm_plan_out *plan, float *grad_weights, void *hip_stream);
@@ -492,27 +497,30 @@ hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype
  * ---- The experts behind it: products in 8 bits -------------------------------------------------
  * Values are e4m3 (no infinities, largest 448) with one power of two for each block of 128 values, a byte whose code
  * - 127 is the exponent (code 255: NaN).  hm_quantize_*: the least exponent with which no value of the block exceeds
- * 448, at least -127; values are divided by it, which is exact, and rounded to nearest even.  NaN and infinities become NaN and
- * do not count for the exponent.  Powers of two lose at most one bit of the scale, cost the matrix unit nothing and make every
- * byte reproducible.  Layouts, with up(n,m) the multiple of m from n on:
- *   rows     [rows, up(C,128)], zeros behind the C values; a block is 128 columns of a row; scales [rows, up(C,512)/128],
+ * 448, at least -127; values are divided by it, which is exact, and rounded to nearest even.  NaN and infinities become
+ * NaN and do not count for the exponent.  Powers of two lose at most one bit of the scale, cost the matrix unit nothing
+ * and make every byte reproducible.  Layouts, with up(n,m) the multiple of m from n on:
+ *   rows     [rows, up(C,128)], zeros behind the C values; a block is 128 columns of a row; scales
+ *            [rows, up(C,512)/128],
  *            zeros behind the ceil(C/128) codes (so both travel through hm_dispatch_pack as rows of 2-byte units)
  *   weights  [experts, N, up(C,128)] likewise; a block is 128 x 128; scales [experts, ceil(N/128), up(C,512)/128]
  *   columns  of rows ordered by expert (segment e: rows offsets[e] .. offsets[e+1] - 1, as in hm_plan_mapped's
- *            dest_offset), transposed: [C, 128 B] with B = rows/128 (rounded down) + segments blocks; segment e owns the blocks from
- *            offsets[e]/128 + e on, its rows in order, zeros behind them up to a whole block; a block is 128 rows of one
+ *            dest_offset), transposed: [C, 128 B] with B = rows/128 (rounded down) + segments blocks; segment e owns
+ *            the blocks from offsets[e]/128 + e on, its rows in order, zeros behind them up to a whole block; a block
+ *            is 128 rows of one
  *            column; scales [B, C].  Blocks that no segment needs are not written
- * 8-bit buffers are 16-byte aligned, scales 4-byte aligned (HM_ERR_SHAPE otherwise).  offsets that descend or lie outside [0,rows]
- * are data errors: no access leaves the buffers, the results are unspecified.
+ * 8-bit buffers are 16-byte aligned, scales 4-byte aligned (HM_ERR_SHAPE otherwise).  offsets that descend or lie
+ * outside [0,rows] are data errors: no access leaves the buffers, the results are unspecified.
  *
  * x: dtype HM_F32 or HM_BF16, row r from element r*ld on, any alignment of the elements; fastest with whole 16-byte
- * vectors.  Limits: C and N up to 2^20, experts and segments up to 1024; hm_quantize_rows: rows * ceil(C / 512) <= 2^25;
- * hm_quantize_columns: rows <= 2^31-1 - 128 * segments, (rows / 128 + segments) * ceil(C / 64) <= 2^23; beyond HM_ERR_SHAPE.
- * hm_quantize_weights takes dense [experts, N, C]; with qt and scale_t it also writes the transposed weights
- * [experts, C, up(N,128)], [experts, ceil(C/128), up(N,512)/128]: the same values, for the gradient of the rows.
+ * vectors.  Limits: C and N up to 2^20, experts and segments up to 1024; hm_quantize_rows: rows * ceil(C / 512) <=
+ * 2^25; hm_quantize_columns: rows <= 2^31-1 - 128 * segments, (rows / 128 + segments) * ceil(C / 64) <= 2^23; beyond
+ * HM_ERR_SHAPE.  hm_quantize_weights takes dense [experts, N, C]; with qt and scale_t it also writes the transposed
+ * weights [experts, C, up(N,128)], [experts, ceil(C/128), up(N,512)/128]: the same values, for the gradient of the
+ * rows.
  */
-hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld, int64_t rows, int32_t C, uint8_t *q, uint8_t *scale,
-                           void *hip_stream);
+hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld, int64_t rows, int32_t C, uint8_t *q,
+                           uint8_t *scale, void *hip_stream);
 hm_status hm_quantize_columns(const void *x, hm_dtype dtype, int64_t ld, const int32_t *offsets, int32_t segments,
                               int64_t rows, int32_t C, uint8_t *q, uint8_t *scale, void *hip_stream);
 hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, int32_t N, int32_t C, uint8_t *q,
@@ -522,22 +530,23 @@ hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, in
 /*
  * hm_expert_matmul -- every row times the weights of its expert:
  *     out[r,n] = sum_h x[r,h] w[e,n,h],   offsets[e] <= r < offsets[e+1].
- * fp32 results are sums in fp32 of the exact products, values being taken as bf16: under codes 0 to 2 (blocks within 1.1e-35) they
- * are rounded to multiples of 2^-133, and from 2^128 on (256 and more under code 247, as numbers from 3.3e38 on are rounded) they
- * are infinite.  HM_BF16_SUM_F32 results are these rounded once, and so are HM_BF16 results of few rows (up
- * to 32, or up to four an expert).  Other HM_BF16 results come from the matrix unit's products of 8 bits, twice as fast, which drop what lies more than 2^13 below the largest
- * of 64 products before they add in fp32, and are then rounded once.  The loss is at most 2^-7 of the largest product for each
- * 64; of the results' norm it was 1.5e-5 for normally distributed values and 5e-5 to 9e-5 for bytes of every exponent and for
- * columns 30 to 1,000 times as large as the others, where the rounding is 1.7e-3.  Where large
- * products cancel, little is left of the small ones.
+ * fp32 results are sums in fp32 of the exact products, values being taken as bf16: under codes 0 to 2 (blocks within
+ * 1.1e-35) they are rounded to multiples of 2^-133, and from 2^128 on (256 and more under code 247, as numbers from
+ * 3.3e38 on are rounded) they are infinite.  HM_BF16_SUM_F32 results are these rounded once, and so are HM_BF16 results
+ * of few rows (up to 32, or up to four an expert).  Other HM_BF16 results come from the matrix unit's products of 8
+ * bits, twice as fast, which drop what lies more than 2^13 below the largest of 64 products before they add in fp32,
+ * and are then rounded once.  The loss is at most 2^-7 of the largest product for each 64; of the results' norm it was
+ * 1.5e-5 for normally distributed values and 5e-5 to 9e-5 for bytes of every exponent and for columns 30 to 1,000 times
+ * as large as the others, where the rounding is 1.7e-3.  Where large products cancel, little is left of the small ones.
  * x, w with their scales in the layouts `rows` and `weights` above (C = H), offsets device int32[experts + 1], out
  * [rows,N] of out_dtype; rows from offsets[experts] on are left alone.  With the rows of the output's gradient and the
  * transposed weights (N and H exchanged) the same call is the gradient of x.
  * hm_expert_matmul_dw -- the gradient of the weights:
  *     dw[e,n,h] = sum over the rows r of segment e of gy[r,n] x[r,h],
  * gy (C = N) and x (C = H) in the layout `columns`; dw [experts,N,H] of dw_dtype, zeros for an expert without rows.
- * Limits: experts <= 1024, N and H up to 2^20, rows <= 2^31-1 - 128 * experts; hm_expert_matmul: rows * experts < 2^35 and
- * (rows / 128 + experts) * ceil(N / 128) <= 2^23 - 8; hm_expert_matmul_dw: rows / 128 + experts < 2^17; beyond HM_ERR_SHAPE.
+ * Limits: experts <= 1024, N and H up to 2^20, rows <= 2^31-1 - 128 * experts; hm_expert_matmul: rows * experts < 2^35
+ * and (rows / 128 + experts) * ceil(N / 128) <= 2^23 - 8; hm_expert_matmul_dw: rows / 128 + experts < 2^17; beyond
+ * HM_ERR_SHAPE.
  */
 hm_status hm_expert_matmul(const uint8_t *x, const uint8_t *x_scale, const uint8_t *w, const uint8_t *w_scale,
                            const int32_t *offsets, int32_t experts, int64_t rows, int32_t N, int32_t H, void *out,

@@ -1,5 +1,5 @@
-// Values in 8 bits (e4m3) with a power of two for each block of 128, as hm_quantize_* write and the experts' products read
-// them: where things lie, and the rounding.
+// Values in 8 bits (e4m3) with a power of two for each block of 128, as hm_quantize_* write and the experts' products
+// read them: where things lie, and the rounding.
 #pragma once
 
 #include "hm_device.h"
@@ -14,7 +14,9 @@ __host__ __device__ static inline int64_t scale8_bytes(int64_t C) { return (C + 
 __host__ __device__ static inline int64_t blocks8(int64_t C) { return (C + 127) / 128; }
 // Blocks in the columns layout of `rows` rows in `segments` segments, and a segment's first: never below the blocks of
 // the segments before it, whose ceilings add up to at most offset / 128 + segment.
-__host__ __device__ static inline int64_t column8_blocks(int64_t rows, int64_t segments) { return rows / 128 + segments; }
+__host__ __device__ static inline int64_t column8_blocks(int64_t rows, int64_t segments) {
+  return rows / 128 + segments;
+}
 __device__ __forceinline__ int first_block8(int offset, int segment) { return offset / 128 + segment; }
 
 // Rows of a segment, kept inside [0,rows] whatever the offsets say.
@@ -34,10 +36,12 @@ __device__ __forceinline__ int scale_code8(uint32_t amax_bits) {
   return max((int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0), 0);
 }
 // 2^(127 - code): what a block's values are multiplied by; normal for every code that scale_code8 gives.
-__device__ __forceinline__ float inverse_scale8(int code) { return __builtin_bit_cast(float, (uint32_t)(254 - code) << 23); }
+__device__ __forceinline__ float inverse_scale8(int code) {
+  return __builtin_bit_cast(float, (uint32_t)(254 - code) << 23);
+}
 
-// Largest magnitude among a thread's values of a block, as bits: those order as the magnitudes do.  NaN and infinities, which
-// are seen by bits that are too large, do not count and become NaN.
+// Largest magnitude among a thread's values of a block, as bits: those order as the magnitudes do.  NaN and infinities,
+// which are seen by bits that are too large, do not count and become NaN.
 template <int N>
 __device__ __forceinline__ uint32_t largest_bits(float (&v)[N]) {
   uint32_t most = 0;
@@ -92,8 +96,8 @@ __device__ __forceinline__ void load_floats(const float *__restrict__ p, float (
 }
 __device__ __forceinline__ float load_float(const uint16_t *p) { return bf16_lo(*p); }
 __device__ __forceinline__ float load_float(const float *p) { return *p; }
-// Elements c to c + N - 1 of a row of C, zeros behind its end.  A vector that would pass the end is loaded from before it and
-// moved down: loads one by one, each waited for, cost a kernel's tail 10 us.
+// Elements c to c + N - 1 of a row of C, zeros behind its end.  A vector that would pass the end is loaded from before
+// it and moved down: loads one by one, each waited for, cost a kernel's tail 10 us.
 template <int N, typename IN>
 __device__ __forceinline__ void load_row_end(const IN *__restrict__ row, int c, int C, float (&v)[N]) {
   if (C < N) {
@@ -111,7 +115,9 @@ __device__ __forceinline__ void load_row_end(const IN *__restrict__ row, int c, 
   for (int i = 0; i < N; ++i) v[i] = by < N ? v[i] : 0.0f;
 }
 
-static inline bool buffers8_aligned(const void *q, const void *scale) { return ((uintptr_t)q & 15) == 0 && ((uintptr_t)scale & 3) == 0; }
+static inline bool buffers8_aligned(const void *q, const void *scale) {
+  return ((uintptr_t)q & 15) == 0 && ((uintptr_t)scale & 3) == 0;
+}
 static inline bool dtype_known(hm_dtype dtype) { return dtype == HM_BF16 || dtype == HM_F32; }
 constexpr int kMostSegments8 = 1024, kMostColumns8 = 1 << 20;
 // Sizes of rows ordered by expert, common to the calls that take offsets.

@@ -20,8 +20,8 @@ struct RowParams {
   uint8_t *q, *scale;
 };
 
-// A wave takes 512 columns of a row, a lane eight of them, sixteen lanes a block.  Bound by memory: 8,192 x 7,168 bf16 34 us,
-// 5.2 TB/s.
+// A wave takes 512 columns of a row, a lane eight of them, sixteen lanes a block.  Bound by memory: 8,192 x 7,168 bf16
+// 34 us, 5.2 TB/s.
 template <typename IN>
 __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(RowParams p) {
   const int lane = lane_id();
@@ -42,8 +42,8 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(RowParams 
     *(uint64_t *)(p.q + r * width + c) = out;
   }
   const uint32_t mine = c < width ? (uint32_t)code : 0u;   // behind the last block zeros
-  const uint32_t codes = (uint32_t)read_lane((int)mine, 0) | (uint32_t)read_lane((int)mine, 16) << 8 | (uint32_t)read_lane((int)mine, 32) << 16 |
-                         (uint32_t)read_lane((int)mine, 48) << 24;
+  const uint32_t codes = (uint32_t)read_lane((int)mine, 0) | (uint32_t)read_lane((int)mine, 16) << 8 |
+                         (uint32_t)read_lane((int)mine, 32) << 16 | (uint32_t)read_lane((int)mine, 48) << 24;
   if (lane == 0) *(uint32_t *)(p.scale + r * scale8_bytes(p.C) + part * 4) = codes;
 }
 
@@ -55,13 +55,14 @@ struct ColumnParams {
   uint8_t *q, *scale;
 };
 
-// The segment that owns block b, the last whose first block is not behind it, and its rows; called by whole waves.  Both
-// offsets of a lane's segment are loaded together: what follows waits for one trip to memory.
+// The segment that owns block b, the last whose first block is not behind it, and its rows; called by whole waves.
+// Both offsets of a lane's segment are loaded together: what follows waits for one trip to memory.
 struct BlockOwner8 {
   int segment;   // -1: none
   Segment8 rows;
 };
-__device__ __forceinline__ BlockOwner8 owner_of_block8(const int32_t *__restrict__ offsets, int segments, int rows, int b) {
+__device__ __forceinline__ BlockOwner8 owner_of_block8(const int32_t *__restrict__ offsets, int segments, int rows,
+                                                       int b) {
   const int lane = lane_id();
   BlockOwner8 owner = {-1, {0, 0}};
   for (int e0 = 0; e0 < segments; e0 += kWave) {
@@ -76,8 +77,9 @@ __device__ __forceinline__ BlockOwner8 owner_of_block8(const int32_t *__restrict
 }
 
 // A workgroup takes a block of 128 rows and 64 columns: a thread eight rows of four columns, whose bytes it turns in
-// registers; LDS puts a column's 128 bytes together.  6,001 rows of 2,056 bf16 in 16 segments 11 us, 3.3 TB/s: one generation of
-// workgroups, whose offsets, rows and stores wait for one another (23 with scalar loads, 14 with neighbouring tiles on any die).
+// registers; LDS puts a column's 128 bytes together.  6,001 rows of 2,056 bf16 in 16 segments 11 us, 3.3 TB/s: one
+// generation of workgroups, whose offsets, rows and stores wait for one another (23 with scalar loads, 14 with
+// neighbouring tiles on any die).
 constexpr int kColumnTile = 64, kColumnPitch = 128 + 8;
 template <typename IN>
 __global__ __launch_bounds__(kQuantThreads) void quantize_columns_kernel(ColumnParams p) {
@@ -151,8 +153,8 @@ struct WeightParams {
   uint8_t *q, *scale, *qt, *scale_t;
 };
 
-// A workgroup takes a block of 128 x 128: a thread eight rows of eight columns.  Bound by memory: 32 x 2,048 x 2,048 fp32, both
-// layouts, 145 us, 5.6 TB/s.
+// A workgroup takes a block of 128 x 128: a thread eight rows of eight columns.  Bound by memory: 32 x 2,048 x 2,048
+// fp32, both layouts, 145 us, 5.6 TB/s.
 template <typename IN>
 __global__ __launch_bounds__(kQuantThreads) void quantize_weights_kernel(WeightParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[128 * kColumnPitch];
@@ -191,23 +193,28 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_weights_kernel(WeightP
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (n0 + rl + i >= p.N) continue;
-    const uint64_t out = (uint64_t)pack8(v[i][4], v[i][5], v[i][6], v[i][7], by) << 32 | pack8(v[i][0], v[i][1], v[i][2], v[i][3], by);
+    const uint64_t out = (uint64_t)pack8(v[i][4], v[i][5], v[i][6], v[i][7], by) << 32 |
+                         pack8(v[i][0], v[i][1], v[i][2], v[i][3], by);
     *(uint64_t *)(p.q + (e * p.N + n0 + rl + i) * width + c0 + cl) = out;
   }
   // a row's scales end with zeros up to a multiple of four; the last block of a row writes them
-  const int blocks_n = (int)blocks8(p.N), blocks_c = (int)blocks8(p.C), wide = (int)scale8_bytes(p.C), wide_t = (int)scale8_bytes(p.N);
+  const int blocks_n = (int)blocks8(p.N), blocks_c = (int)blocks8(p.C);
+  const int wide = (int)scale8_bytes(p.C), wide_t = (int)scale8_bytes(p.N);
   if (tid < 4) {
     const int k = (int)blockIdx.x + tid;
-    if (tid == 0 || ((int)blockIdx.x == blocks_c - 1 && k < wide)) p.scale[(e * blocks_n + blockIdx.y) * wide + k] = tid == 0 ? (uint8_t)code : 0;
+    if (tid == 0 || ((int)blockIdx.x == blocks_c - 1 && k < wide))
+      p.scale[(e * blocks_n + blockIdx.y) * wide + k] = tid == 0 ? (uint8_t)code : 0;
   }
   if (!p.qt) return;
   if (tid < 4) {
     const int k = (int)blockIdx.y + tid;
-    if (tid == 0 || ((int)blockIdx.y == blocks_n - 1 && k < wide_t)) p.scale_t[(e * blocks_c + blockIdx.x) * wide_t + k] = tid == 0 ? (uint8_t)code : 0;
+    if (tid == 0 || ((int)blockIdx.y == blocks_n - 1 && k < wide_t))
+      p.scale_t[(e * blocks_c + blockIdx.x) * wide_t + k] = tid == 0 ? (uint8_t)code : 0;
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const uint64_t out = (uint64_t)pack8(v[4][j], v[5][j], v[6][j], v[7][j], by) << 32 | pack8(v[0][j], v[1][j], v[2][j], v[3][j], by);
+    const uint64_t out = (uint64_t)pack8(v[4][j], v[5][j], v[6][j], v[7][j], by) << 32 |
+                         pack8(v[0][j], v[1][j], v[2][j], v[3][j], by);
     *(uint64_t *)(turned + (cl + j) * kColumnPitch + rl) = out;
   }
   __syncthreads();
@@ -224,12 +231,12 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_weights_kernel(WeightP
 
 }  // namespace hm
 
-extern "C" hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld, int64_t rows, int32_t C, uint8_t *q, uint8_t *scale,
-                                      void *hip_stream) {
+extern "C" hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld, int64_t rows, int32_t C, uint8_t *q,
+                                      uint8_t *scale, void *hip_stream) {
   HM_ENTRY_SCOPE;
   using namespace hm;
-  if (!dtype_known(dtype) || C < 1 || C > kMostColumns8 || rows < 0 || rows > 2147483647LL || (ld < C && rows > 1) || !buffers8_aligned(q, scale))
-    return HM_ERR_SHAPE;
+  if (!dtype_known(dtype) || C < 1 || C > kMostColumns8 || rows < 0 || rows > 2147483647LL) return HM_ERR_SHAPE;
+  if ((ld < C && rows > 1) || !buffers8_aligned(q, scale)) return HM_ERR_SHAPE;
   if (rows == 0) return HM_OK;
   if (!x || !q || !scale) return HM_ERR_NULL;
   RowParams p;
@@ -247,12 +254,13 @@ extern "C" hm_status hm_quantize_rows(const void *x, hm_dtype dtype, int64_t ld,
   return hm_launch_status();
 }
 
-extern "C" hm_status hm_quantize_columns(const void *x, hm_dtype dtype, int64_t ld, const int32_t *offsets, int32_t segments, int64_t rows,
-                                         int32_t C, uint8_t *q, uint8_t *scale, void *hip_stream) {
+extern "C" hm_status hm_quantize_columns(const void *x, hm_dtype dtype, int64_t ld, const int32_t *offsets,
+                                         int32_t segments, int64_t rows, int32_t C, uint8_t *q, uint8_t *scale,
+                                         void *hip_stream) {
   HM_ENTRY_SCOPE;
   using namespace hm;
-  if (!dtype_known(dtype) || C < 1 || C > kMostColumns8 || !segments8_ok(segments, rows) || (ld < C && rows > 1) || !buffers8_aligned(q, scale))
-    return HM_ERR_SHAPE;
+  if (!dtype_known(dtype) || C < 1 || C > kMostColumns8 || !segments8_ok(segments, rows)) return HM_ERR_SHAPE;
+  if ((ld < C && rows > 1) || !buffers8_aligned(q, scale)) return HM_ERR_SHAPE;
   if (rows == 0) return HM_OK;
   if (!x || !offsets || !q || !scale) return HM_ERR_NULL;
   ColumnParams p;
@@ -273,16 +281,18 @@ extern "C" hm_status hm_quantize_columns(const void *x, hm_dtype dtype, int64_t 
   return hm_launch_status();
 }
 
-extern "C" hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, int32_t N, int32_t C, uint8_t *q, uint8_t *scale,
-                                         uint8_t *qt, uint8_t *scale_t, void *hip_stream) {
+extern "C" hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, int32_t N, int32_t C,
+                                         uint8_t *q, uint8_t *scale, uint8_t *qt, uint8_t *scale_t,
+                                         void *hip_stream) {
   HM_ENTRY_SCOPE;
   using namespace hm;
   if (!w || !q || !scale || (!qt != !scale_t)) return HM_ERR_NULL;
-  if (!dtype_known(dtype) || experts < 1 || experts > kMostSegments8 || N < 1 || N > kMostColumns8 || C < 1 || C > kMostColumns8 || !buffers8_aligned(q, scale) ||
-      !buffers8_aligned(qt, scale_t))
-    return HM_ERR_SHAPE;
+  if (!dtype_known(dtype) || experts < 1 || experts > kMostSegments8) return HM_ERR_SHAPE;
+  if (N < 1 || N > kMostColumns8 || C < 1 || C > kMostColumns8) return HM_ERR_SHAPE;
+  if (!buffers8_aligned(q, scale) || !buffers8_aligned(qt, scale_t)) return HM_ERR_SHAPE;
   WeightParams p = {w, N, C, q, scale, qt, scale_t};
   const auto kernel = dtype == HM_BF16 ? quantize_weights_kernel<uint16_t> : quantize_weights_kernel<float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks8(C), (unsigned)blocks8(N), (unsigned)experts), dim3(kQuantThreads), 0, (hipStream_t)hip_stream, p);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks8(C), (unsigned)blocks8(N), (unsigned)experts), dim3(kQuantThreads),
+                     0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }

@@ -23,9 +23,9 @@ __device__ __forceinline__ float logit_at(const float *x, int64_t i) { return x[
 // What an expert that is never chosen has in place of its logit and its choice.
 __device__ __forceinline__ float kNone() { return -__builtin_inff(); }
 __device__ __forceinline__ float usable(float x) { return x == x ? fminf(x, 3.402823466e38f) : kNone(); }
-// 1 / (1 + exp(-x)), the quotient rounded as a division rounds it: one Newton step from a reciprocal good to a unit in the
-// last place (Markstein), compared with the division for every y from 1 to 2^126; beyond scores are 0.  The division takes
-// eight instructions more for each of a token's experts: 65,536 x 256 with a bias 43 -> 31 us.
+// 1 / (1 + exp(-x)), the quotient rounded as a division rounds it: one Newton step from a reciprocal good to a unit in
+// the last place (Markstein), compared with the division for every y from 1 to 2^126; beyond scores are 0.  The
+// division takes eight instructions more for each of a token's experts: 65,536 x 256 with a bias 43 -> 31 us.
 __device__ __forceinline__ float reciprocal(float y) {   // of y >= 1
   const float r = __builtin_amdgcn_rcpf(y);
   const float better = __builtin_fmaf(__builtin_fmaf(-y, r, 1.0f), r, r);
@@ -37,7 +37,8 @@ __device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + ex
 template <typename OP>
 __device__ __forceinline__ float wave_all(float v, OP op) {
   auto turned = [](float x, auto control) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), control(), 0xF, 0xF, true));
+    const int from = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), control(), 0xF, 0xF, true);
+    return __builtin_bit_cast(float, from);
   };
   v = op(v, turned(v, std::integral_constant<int, 0x128>()));
   v = op(v, turned(v, std::integral_constant<int, 0x124>()));
@@ -60,9 +61,9 @@ __device__ __forceinline__ void wave_first(float &v, int &i) {
   }
 }
 
-// What the choice by lists (below) does not take: K > 16, groups that are no power of two up to 16, a softmax with a bias, many
-// experts.  A wave takes a token; its choices stand in LDS and the largest is taken K times: 65,536 tokens of 256 experts 178 us
-// where the lists take 30.
+// What the choice by lists (below) does not take: K > 16, groups that are no power of two up to 16, a softmax with a
+// bias, many experts.  A wave takes a token; its choices stand in LDS and the largest is taken K times: 65,536 tokens
+// of 256 experts 178 us where the lists take 30.
 template <typename IN>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteParams p) {
   extern __shared__ float choices[];
@@ -152,9 +153,9 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteParams p) {
 
 // ---- choice by sorted lists ----------------------------------------------------------------------------
 // A choice and its expert as one number of 64 bits that orders as the definition does: the fp32 choice is the high word
-// of a double, whose order is that of the floats (a float's bits with anything behind them are a finite double, -inf's and +inf's
-// too), and the low word puts the lower of two equal experts first.  The largest and the smaller of two are one
-// instruction each.
+// of a double, whose order is that of the floats (a float's bits with anything behind them are a finite double, -inf's
+// and +inf's too), and the low word puts the lower of two equal experts first.  The largest and the smaller of two are
+// one instruction each.
 __device__ __forceinline__ double key_of(int32_t high, int e) {
   return __builtin_bit_cast(double, (uint64_t)(uint32_t)high << 32 | (uint32_t)(~e ^ (high >> 31)));
 }
@@ -167,16 +168,21 @@ __device__ __forceinline__ double key_of_logit(float x, int e) {
 // Of a logistic score and a bias: none where the logit is, and where the sum is none.  The sum is never -0.
 __device__ __forceinline__ double key_of_sum(float x, float bias, int e) {
   const float c = logistic(x) + bias;
-  const int32_t high = c > kNone() ? __builtin_bit_cast(int32_t, c) : kNoneBits;   // two selects: with `and` the compiler branches
+  // two selects: with `and` the compiler branches
+  const int32_t high = c > kNone() ? __builtin_bit_cast(int32_t, c) : kNoneBits;
   return key_of(x > kNone() ? high : kNoneBits, e);
 }
-__device__ __forceinline__ float choice_of(double key) { return __builtin_bit_cast(float, (uint32_t)(__builtin_bit_cast(uint64_t, key) >> 32)); }
+__device__ __forceinline__ float choice_of(double key) {
+  return __builtin_bit_cast(float, (uint32_t)(__builtin_bit_cast(uint64_t, key) >> 32));
+}
 __device__ __forceinline__ int expert_of(double key) {
   const uint64_t k = __builtin_bit_cast(uint64_t, key);
   return (int64_t)k < 0 ? (int)(uint32_t)k : ~(int)(uint32_t)k;
 }
-__device__ __forceinline__ double none_key() { return __builtin_bit_cast(double, (uint64_t)0xFF800000u << 32); }   // -inf
-__device__ __forceinline__ double larger(double a, double b) {   // as it is, without the compiler's care for signalling NaN
+// -inf
+__device__ __forceinline__ double none_key() { return __builtin_bit_cast(double, (uint64_t)0xFF800000u << 32); }
+// as it is, without the compiler's care for signalling NaN
+__device__ __forceinline__ double larger(double a, double b) {
   double r;
   __asm__("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
   return r;
@@ -218,15 +224,19 @@ __device__ __forceinline__ void merge(double (&k)[N], const double (&other)[N]) 
 // From a lane of the other half of 2 D lanes, D = 1, 2, 4, 8, where all lanes of a half hold the same.
 template <int D>
 __device__ __forceinline__ int other_half(int v) {
-  constexpr int kControl = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x140;   // quads 1 0 3 2 and 2 3 0 1; mirrors of eight and sixteen
+  // quads 1 0 3 2 and 2 3 0 1; mirrors of eight and sixteen
+  constexpr int kControl = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x140;
   return __builtin_amdgcn_update_dpp(0, v, kControl, 0xF, 0xF, true);
 }
 template <int D>
-__device__ __forceinline__ float other_half(float v) { return __builtin_bit_cast(float, other_half<D>(__builtin_bit_cast(int, v))); }
+__device__ __forceinline__ float other_half(float v) {
+  return __builtin_bit_cast(float, other_half<D>(__builtin_bit_cast(int, v)));
+}
 template <int D>
 __device__ __forceinline__ double other_half(double v) {
   const uint64_t k = __builtin_bit_cast(uint64_t, v);
-  return __builtin_bit_cast(double, (uint64_t)(uint32_t)other_half<D>((int)(k >> 32)) << 32 | (uint32_t)other_half<D>((int)k));
+  const uint32_t high = (uint32_t)other_half<D>((int)(k >> 32)), low = (uint32_t)other_half<D>((int)k);
+  return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
 }
 // op(v, what the other half has) for halves of FROM up to half of UPTO lanes.
 template <int FROM, int UPTO, typename OP>
@@ -254,9 +264,10 @@ __device__ __forceinline__ void load_logits(const IN *p, int n, float (&v)[N]) {
 // L lanes take a token, each a run of its experts, of which it keeps the N >= K largest; the lists of the lanes are
 // then merged pairwise.  With groups the L lanes are shared among them, so that a lane's run lies in one group, and
 // the two largest of its list give the group's score: lists of groups that are not taken are emptied before the merges.
-// What bounds it are vector instructions: about 27 an expert for a logistic score, 4 for its key and 9 for sorting (N = 8), against 4
-// bytes read.  us: 65,536 tokens, 256 experts, logistic with bias and groups 30 (2.4 TB/s), softmax 24, bf16 18; one token 5.3.
-// 8 lanes a token from 16,384 tokens on: 65,536 x 64 8.4 and, with 16 lanes, 14.7; 8,192 x 256 8.3 and 6.9.
+// What bounds it are vector instructions: about 27 an expert for a logistic score, 4 for its key and 9 for sorting (N =
+// 8), against 4 bytes read.  us: 65,536 tokens, 256 experts, logistic with bias and groups 30 (2.4 TB/s), softmax 24,
+// bf16 18; one token 5.3. 8 lanes a token from 16,384 tokens on: 65,536 x 64 8.4 and, with 16 lanes, 14.7; 8,192 x 256
+// 8.3 and 6.9.
 template <typename IN, int L, int N>
 __global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteParams p, int lanes_per_group, int run) {
   const int sub = (int)threadIdx.x & (L - 1);
@@ -389,7 +400,8 @@ struct RouteBackParams {
 __device__ __forceinline__ void put(uint16_t *x, float v) { *x = (uint16_t)f32_to_bf16(v); }
 __device__ __forceinline__ void put(float *x, float v) { *x = v; }
 
-// A wave takes a token, a lane a slot; the row is put together in LDS.  8,192 x 256 fp32 6 us, the stores of 8 MB and a launch.
+// A wave takes a token, a lane a slot; the row is put together in LDS.  8,192 x 256 fp32 6 us, the stores of 8 MB and a
+// launch.
 template <typename IN>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteBackParams p) {
   extern __shared__ float rows[];
@@ -478,7 +490,8 @@ template <>
 struct Eight<float> {
   f32x4 a, b;
   Eight() = default;
-  __device__ __forceinline__ explicit Eight(const float *p) : a(*(const f32x4_align4 *)p), b(*(const f32x4_align4 *)(p + 4)) {}
+  __device__ __forceinline__ explicit Eight(const float *p)
+      : a(*(const f32x4_align4 *)p), b(*(const f32x4_align4 *)(p + 4)) {}
   __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
   __device__ __forceinline__ float times(const Eight &v, float sum) const {
 #pragma unroll
@@ -487,16 +500,17 @@ struct Eight<float> {
   }
 };
 
-// A wave takes a part of a token's row and SLOTS of its slots at a time: its gradient's row once, the slots' rows beside it, all
-// loads of 512 elements on their way together.  Where a row is split, the parts' sums meet in LDS.  What bounds it is
-// memory, (K + 1) rows a token: 8,192 tokens, K = 8, 7,168 bf16 180 us, 5.9 TB/s; few tokens wait for one trip after the
-// other (1,237 tokens, K = 6, 1,030 fp32 9 us).
+// A wave takes a part of a token's row and SLOTS of its slots at a time: its gradient's row once, the slots' rows
+// beside it, all loads of 512 elements on their way together.  Where a row is split, the parts' sums meet in LDS.  What
+// bounds it is memory, (K + 1) rows a token: 8,192 tokens, K = 8, 7,168 bf16 180 us, 5.9 TB/s; few tokens wait for one
+// trip after the other (1,237 tokens, K = 6, 1,030 fp32 9 us).
 template <typename IN, int PARTS, int SLOTS>
 __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(WeightGradParams p) {
   __shared__ float parts[kRouteWaves][SLOTS];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), part = wave % PARTS;
   const int64_t t = (int64_t)blockIdx.x * (kRouteWaves / PARTS) + wave / PARTS;
-  const bool there_t = t < p.T;   // the same for the waves of a token; with several parts nobody leaves before the barriers
+  // the same for the waves of a token; with several parts nobody leaves before the barriers
+  const bool there_t = t < p.T;
   if (PARTS == 1 && !there_t) return;
   const int64_t token = there_t ? t : 0;
   const IN *gout = (const IN *)p.gout + token * p.H;
@@ -525,8 +539,8 @@ __global__ __launch_bounds__(kRouteThreads) void combine_weight_grad_kernel(Weig
       for (int j = 0; j < SLOTS; ++j)
         if (k0 + j < p.K) sum[j] = g.times(v[j], sum[j]);
     }
-    // The row's last, shorter step is the part's whose turn it is: vectors that would pass the end lie before it, and what
-    // the vector before them has had counts as zero.
+    // The row's last, shorter step is the part's whose turn it is: vectors that would pass the end lie before it, and
+    // what the vector before them has had counts as zero.
     const int begin = h - lane * 8;
     if (begin < p.H && begin + kStep > p.H) {
       if (p.H >= 8) {
@@ -574,13 +588,14 @@ static hm_status check_router(const hm_router *r) {
   if (!r) return HM_ERR_NULL;
   if (r->E < 1 || r->E > kMostExperts || r->K < 1 || r->K > kMostSlots) return HM_ERR_SHAPE;
   if (r->score != HM_SCORE_SOFTMAX && r->score != HM_SCORE_SIGMOID) return HM_ERR_SHAPE;
-  if (r->groups < 1 || r->groups > r->E || r->E % r->groups || r->top_groups < 1 || r->top_groups > r->groups) return HM_ERR_SHAPE;
+  if (r->groups < 1 || r->groups > r->E || r->E % r->groups) return HM_ERR_SHAPE;
+  if (r->top_groups < 1 || r->top_groups > r->groups) return HM_ERR_SHAPE;
   if (r->group_best < 1 || r->group_best > 2 || r->group_best > r->E / r->groups) return HM_ERR_SHAPE;
   if (r->K > r->E / r->groups * r->top_groups) return HM_ERR_SHAPE;
   return HM_OK;
 }
-// Lanes of a token for the choice by lists, 0 where it is not made: groups share the lanes, and a softmax with a bias needs its
-// sum before the choice.
+// Lanes of a token for the choice by lists, 0 where it is not made: groups share the lanes, and a softmax with a bias
+// needs its sum before the choice.
 static int list_lanes(const hm_router &r, bool biased, int64_t T) {
   if (r.K > 16 || (r.groups & (r.groups - 1)) || r.groups > 16 || (biased && r.score == HM_SCORE_SOFTMAX)) return 0;
   if (T >= 16384 && r.groups <= 8 && r.E <= 64 * 8) return 8;
@@ -588,13 +603,15 @@ static int list_lanes(const hm_router &r, bool biased, int64_t T) {
 }
 template <typename IN, int L>
 static void launch_lists(const RouteParams &p, hipStream_t stream) {
-  const int K = p.r.K, lanes_per_group = L / p.r.groups, run = (p.r.E / p.r.groups + lanes_per_group - 1) / lanes_per_group;
+  const int K = p.r.K, lanes_per_group = L / p.r.groups;
+  const int run = (p.r.E / p.r.groups + lanes_per_group - 1) / lanes_per_group;
   const auto kernel = K <= 2   ? route_lists_kernel<IN, L, 2>
                       : K <= 4 ? route_lists_kernel<IN, L, 4>
                       : K <= 8 ? route_lists_kernel<IN, L, 8>
                                : route_lists_kernel<IN, L, 16>;
   const int64_t per_block = kRouteThreads / L;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.T + per_block - 1) / per_block)), dim3(kRouteThreads), 0, stream, p, lanes_per_group, run);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.T + per_block - 1) / per_block)), dim3(kRouteThreads), 0, stream, p,
+                     lanes_per_group, run);
 }
 // Whether a launch has threads for T tokens of so many: it has less than 2^32, in whole workgroups.
 static bool threads_suffice(int64_t T, int each) { return T * each <= (1LL << 32) - kRouteThreads; }
@@ -607,8 +624,8 @@ static int tokens_per_group(int floats) {
 
 }  // namespace hm
 
-extern "C" hm_status hm_route(const void *logits, hm_dtype dtype, int64_t ld, const float *bias, int32_t T, const hm_router *router,
-                              int32_t *topk_ids, float *topk_weights, void *hip_stream) {
+extern "C" hm_status hm_route(const void *logits, hm_dtype dtype, int64_t ld, const float *bias, int32_t T,
+                              const hm_router *router, int32_t *topk_ids, float *topk_weights, void *hip_stream) {
   HM_ENTRY_SCOPE;
   using namespace hm;
   const hm_status bad = check_router(router);
@@ -629,30 +646,35 @@ extern "C" hm_status hm_route(const void *logits, hm_dtype dtype, int64_t ld, co
   }
   const int floats = router->E + (router->groups > 1 ? router->groups : 0), n = tokens_per_group(floats);
   const auto kernel = dtype == HM_BF16 ? route_kernel<uint16_t> : route_kernel<float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((T + (int64_t)n - 1) / n)), dim3((unsigned)(n * kWave)), (size_t)n * floats * 4, (hipStream_t)hip_stream, p);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((T + (int64_t)n - 1) / n)), dim3((unsigned)(n * kWave)),
+                     (size_t)n * floats * 4, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
 
-extern "C" hm_status hm_route_backward(const void *logits, hm_dtype dtype, int64_t ld, const int32_t *topk_ids, const float *grad_weights,
-                                       int32_t T, const hm_router *router, void *grad_logits, int64_t grad_ld, void *hip_stream) {
+extern "C" hm_status hm_route_backward(const void *logits, hm_dtype dtype, int64_t ld, const int32_t *topk_ids,
+                                       const float *grad_weights, int32_t T, const hm_router *router,
+                                       void *grad_logits, int64_t grad_ld, void *hip_stream) {
   HM_ENTRY_SCOPE;
   using namespace hm;
   const hm_status bad = check_router(router);
   if (bad != HM_OK) return bad;
   const hm_status shape = hm_check_tk(T, router->K);
   if (shape != HM_OK) return shape;
-  if (!dtype_known(dtype) || ((ld < router->E || grad_ld < router->E) && T > 1) || !threads_suffice(T, kWave)) return HM_ERR_SHAPE;
+  if (!dtype_known(dtype) || ((ld < router->E || grad_ld < router->E) && T > 1)) return HM_ERR_SHAPE;
+  if (!threads_suffice(T, kWave)) return HM_ERR_SHAPE;
   if (T == 0) return HM_OK;
   if (!logits || !topk_ids || !grad_weights || !grad_logits) return HM_ERR_NULL;
   const RouteBackParams p = {logits, ld, grad_ld, topk_ids, grad_weights, T, *router, grad_logits};
   const int n = tokens_per_group(router->E);
   const auto kernel = dtype == HM_BF16 ? route_backward_kernel<uint16_t> : route_backward_kernel<float>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((T + (int64_t)n - 1) / n)), dim3((unsigned)(n * kWave)), (size_t)n * router->E * 4, (hipStream_t)hip_stream, p);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((T + (int64_t)n - 1) / n)), dim3((unsigned)(n * kWave)),
+                     (size_t)n * router->E * 4, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
 
-extern "C" hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype, int64_t y_rows, int32_t T, int32_t K, int32_t H,
-                                            const hm_plan_out *plan, float *grad_weights, void *hip_stream) {
+extern "C" hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_dtype dtype, int64_t y_rows, int32_t T,
+                                            int32_t K, int32_t H, const hm_plan_out *plan, float *grad_weights,
+                                            void *hip_stream) {
   HM_ENTRY_SCOPE;
   using namespace hm;
   if (!plan || !plan->slot_row || !plan->status) return HM_ERR_NULL;
@@ -662,14 +684,16 @@ extern "C" hm_status hm_combine_weight_grad(const void *gout, const void *y, hm_
   if (T == 0) return HM_OK;
   if (!gout || !grad_weights || (!y && y_rows > 0)) return HM_ERR_NULL;
   const WeightGradParams p = {gout, y, y_rows, plan->slot_row, T, K, H, grad_weights, plan->status};
-  // A token's row in four parts where there are few tokens.  Eight slots at a time read the gradient's row once for most K; fp32
-  // rows take the registers of four waves a SIMD for that, so they go four at a time (8,192 x 2,048, K = 8: 125 us and 137) but where
-  // rows are long (8,192 x 7,168: 395 and 356).
+  // A token's row in four parts where there are few tokens.  Eight slots at a time read the gradient's row once for
+  // most K; fp32 rows take the registers of four waves a SIMD for that, so they go four at a time (8,192 x 2,048, K =
+  // 8: 125 us and 137) but where rows are long (8,192 x 7,168: 395 and 356).
   const int parts = T <= 4096 && H > 512 ? kRouteWaves : 1, tokens = kRouteWaves / parts;
   const auto whole = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, 1, 8>
                      : H >= 4096      ? combine_weight_grad_kernel<float, 1, 8>
                                       : combine_weight_grad_kernel<float, 1, 4>;
-  const auto split = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, kRouteWaves, 8> : combine_weight_grad_kernel<float, kRouteWaves, 4>;
-  hipLaunchKernelGGL((parts == 1 ? whole : split), dim3((unsigned)((T + tokens - 1) / tokens)), dim3(kRouteThreads), 0, (hipStream_t)hip_stream, p);
+  const auto split = dtype == HM_BF16 ? combine_weight_grad_kernel<uint16_t, kRouteWaves, 8>
+                                      : combine_weight_grad_kernel<float, kRouteWaves, 4>;
+  hipLaunchKernelGGL((parts == 1 ? whole : split), dim3((unsigned)((T + tokens - 1) / tokens)), dim3(kRouteThreads), 0,
+                     (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
