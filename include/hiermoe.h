@@ -544,6 +544,7 @@ hm_status hm_quantize_weights(const void *w, hm_dtype dtype, int32_t experts, in
  * hm_expert_matmul_dw -- the gradient of the weights:
  *     dw[e,n,h] = sum over the rows r of segment e of gy[r,n] x[r,h],
  * gy (C = N) and x (C = H) in the layout `columns`; dw [experts,N,H] of dw_dtype, zeros for an expert without rows.
+ * Its sums are those above, HM_BF16 always by the unit's products.
  * Limits: experts <= 1024, N and H up to 2^20, rows <= 2^31-1 - 128 * experts; hm_expert_matmul: rows * experts < 2^35
  * and (rows / 128 + experts) * ceil(N / 128) <= 2^23 - 8; hm_expert_matmul_dw: rows / 128 + experts < 2^17; beyond
  * HM_ERR_SHAPE.

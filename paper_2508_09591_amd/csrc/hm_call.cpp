@@ -471,7 +471,9 @@ T *shaped(PyObject *o, at::ScalarType type, std::initializer_list<int64_t> sizes
   if (t.sizes() != at::IntArrayRef(sizes)) throw NotOrdinary();
   return static_cast<T *>(t.data_ptr());
 }
-uint8_t *values8(PyObject *o, std::initializer_list<int64_t> sizes) { return shaped<uint8_t>(o, at::kFloat8_e4m3fn, sizes); }
+uint8_t *values8(PyObject *o, std::initializer_list<int64_t> sizes) {
+  return shaped<uint8_t>(o, at::kFloat8_e4m3fn, sizes);
+}
 uint8_t *scales8(PyObject *o, std::initializer_list<int64_t> sizes) { return shaped<uint8_t>(o, at::kByte, sizes); }
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
@@ -485,11 +487,14 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {   // logits, rou
     auto *ids = shaped<int32_t>(a[2], at::kInt, {T, K});
     auto *weights = shaped<float>(a[3], at::kFloat, {T, K});
     const auto *bias = a[4] == Py_None ? nullptr : shaped<const float>(a[4], at::kFloat, {E});
-    return launched([&](void *s) { return layer.route(logits.data_ptr(), floats(logits), E, bias, T, r.c(), ids, weights, s); });
+    return launched([&](void *s) {
+      return layer.route(logits.data_ptr(), floats(logits), E, bias, T, r.c(), ids, weights, s);
+    });
   });
 }
 
-PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {   // logits, router, ids, grad_weights, grad_logits
+// logits, router, ids, grad_weights, grad_logits
+PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return layer_answer(n, 5, [&] {
     int32_t T, E;
     const at::Tensor &logits = matrix(a[0], T, E);
@@ -499,7 +504,9 @@ PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {   // lo
     const auto *ids = shaped<const int32_t>(a[2], at::kInt, {T, K});
     const auto *grad = shaped<const float>(a[3], at::kFloat, {T, K});
     auto *to = shaped<void>(a[4], logits.scalar_type(), {T, E});
-    return launched([&](void *s) { return layer.route_backward(logits.data_ptr(), floats(logits), E, ids, grad, T, r.c(), to, E, s); });
+    return launched([&](void *s) {
+      return layer.route_backward(logits.data_ptr(), floats(logits), E, ids, grad, T, r.c(), to, E, s);
+    });
   });
 }
 
@@ -511,7 +518,9 @@ PyObject *combine_weight_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {   
     const Plan p(a[2]);
     p.expect(T, a[3]);
     auto *grad = pointer<float>(a[3], at::kFloat);
-    return launched([&](void *s) { return layer.combine_weight_grad(gout.data_ptr(), y.data_ptr(), floats(gout), rows, T, p.K, H, p.c(), grad, s); });
+    return launched([&](void *s) {
+      return layer.combine_weight_grad(gout.data_ptr(), y.data_ptr(), floats(gout), rows, T, p.K, H, p.c(), grad, s);
+    });
   });
 }
 
@@ -532,7 +541,9 @@ PyObject *quantize_columns(PyObject *, PyObject *const *a, Py_ssize_t n) {   // 
     const int32_t segments = size32(tensor(a[1]).numel() - 1);
     const int64_t blocks = rows / 128 + static_cast<int64_t>(segments);
     auto *q = values8(a[2], {C, 128 * blocks}), *scale = scales8(a[3], {blocks, C});
-    return launched([&](void *s) { return layer.quantize_columns(x.data_ptr(), floats(x), C, offsets, segments, rows, C, q, scale, s); });
+    return launched([&](void *s) {
+      return layer.quantize_columns(x.data_ptr(), floats(x), C, offsets, segments, rows, C, q, scale, s);
+    });
   });
 }
 
@@ -547,11 +558,14 @@ PyObject *quantize_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {   // 
     if (both == (a[4] == Py_None)) throw NotOrdinary();
     auto *qt = both ? values8(a[3], {E, C, up(N, 128)}) : nullptr;
     auto *scale_t = both ? scales8(a[4], {E, up(C, 128) / 128, up(N, 512) / 128}) : nullptr;
-    return launched([&](void *s) { return layer.quantize_weights(w.data_ptr(), dtype, E, N, C, q, scale, qt, scale_t, s); });
+    return launched([&](void *s) {
+      return layer.quantize_weights(w.data_ptr(), dtype, E, N, C, q, scale, qt, scale_t, s);
+    });
   });
 }
 
-PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, x_scale, w, w_scale, offsets, out, full_sums
+// x, x_scale, w, w_scale, offsets, out, full_sums
+PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return layer_answer(n, 7, [&] {
     const at::Tensor &w = checked(a[2], at::kFloat8_e4m3fn);
     if (w.dim() != 3) throw NotOrdinary();
@@ -565,11 +579,14 @@ PyObject *expert_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {   // x, 
     const auto *offsets = shaped<const int32_t>(a[4], at::kInt, {static_cast<int64_t>(E) + 1});
     const auto *wq = static_cast<const uint8_t *>(w.data_ptr());
     const hm_dtype dtype = sums(out, a[6]);
-    return launched([&](void *s) { return layer.expert_matmul(x, xs, wq, ws, offsets, E, rows, N, H, out.data_ptr(), dtype, s); });
+    return launched([&](void *s) {
+      return layer.expert_matmul(x, xs, wq, ws, offsets, E, rows, N, H, out.data_ptr(), dtype, s);
+    });
   });
 }
 
-PyObject *expert_matmul_dw(PyObject *, PyObject *const *a, Py_ssize_t n) {   // gy, gy_scale, x, x_scale, offsets, rows, dw, full_sums
+// gy, gy_scale, x, x_scale, offsets, rows, dw, full_sums
+PyObject *expert_matmul_dw(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return layer_answer(n, 8, [&] {
     const at::Tensor &dw = tensor(a[6]);
     if (!dw.is_cuda() || !dw.is_contiguous() || dw.dim() != 3) throw NotOrdinary();
@@ -580,7 +597,9 @@ PyObject *expert_matmul_dw(PyObject *, PyObject *const *a, Py_ssize_t n) {   // 
     const auto *gy = values8(a[0], {N, 128 * blocks}), *gs = scales8(a[1], {blocks, N});
     const auto *x = values8(a[2], {H, 128 * blocks}), *xs = scales8(a[3], {blocks, H});
     const auto *offsets = shaped<const int32_t>(a[4], at::kInt, {static_cast<int64_t>(E) + 1});
-    return launched([&](void *s) { return layer.expert_matmul_dw(gy, gs, x, xs, offsets, E, rows, N, H, dw.data_ptr(), dtype, s); });
+    return launched([&](void *s) {
+      return layer.expert_matmul_dw(gy, gs, x, xs, offsets, E, rows, N, H, dw.data_ptr(), dtype, s);
+    });
   });
 }
 
