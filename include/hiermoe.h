@@ -556,6 +556,82 @@ hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_scale, const 
                               const int32_t *offsets, int32_t experts, int64_t rows, int32_t N, int32_t H, void *dw,
                               hm_dtype dw_dtype, void *hip_stream);
 
+/*
+ * ---- Around the experts' products --------------------------------------------------------------
+ * hm_rms_norm -- the norm in front of a layer, with the residual's addition:
+ *     s = x + residual,   y = s / sqrt(mean(s^2) + eps) * weight      per row of C values
+ * residual [rows,C] of total_dtype or NULL; with it the sum, rounded to that type, is kept in total (not NULL then), and
+ * what is normed is the sum as it is kept.  y [rows,C] of y_dtype, and q, scale: the same values in 8 bits in the layout
+ * `rows` above, rounded once from fp32; either may be NULL, not both.  Sums are fp32: a row whose squares add up to more
+ * than 3.4e38 gives zeros, one with a NaN gives NaN.  x, residual and total have rows ld, residual_ld, total_ld elements
+ * apart; total may be x or residual itself (the same elements in the same place), y may be x.
+ * Limits: C <= 32768, rows <= 2^31 - 1, eps >= 0.
+ */
+hm_status hm_rms_norm(const void *x, hm_dtype dtype, int64_t ld, const void *residual, hm_dtype total_dtype,
+                      int64_t residual_ld, const void *weight, hm_dtype weight_dtype, float eps, int64_t rows, int32_t C,
+                      void *total, int64_t total_ld, void *y, hm_dtype y_dtype, uint8_t *q, uint8_t *scale,
+                      void *hip_stream);
+
+/*
+ * hm_rms_norm_backward -- from the gradient gy [rows,C] of y and what was normed, s [rows,C] (total, or x without a
+ * residual), the gradient of s and of the weight:
+ *     u = gy weight,  m = mean(s^2) + eps,  gx = (u - s mean(u s) / m) / sqrt(m) + gtotal,
+ *     gweight = sum over the rows of gy s / sqrt(m)
+ * gx [rows,C] is the gradient of x and of the residual alike; gtotal, of the dtype of s and gx, is the gradient that came
+ * past the layer, or NULL; gx may be gtotal, s or gy itself (of its type).  gweight fp32 [C], always whole: it does not add
+ * to what was there, and zeros stand for no rows.  The order of its sums follows from the sizes alone.
+ * workspace: hm_rms_norm_backward_workspace_bytes(rows, C) bytes of device scratch, 16-byte aligned.  Limits as above.
+ */
+size_t hm_rms_norm_backward_workspace_bytes(int64_t rows, int32_t C);
+hm_status hm_rms_norm_backward(const void *gy, hm_dtype gy_dtype, int64_t gy_ld, const void *s, hm_dtype dtype,
+                               int64_t s_ld, const void *weight, hm_dtype weight_dtype, float eps, int64_t rows, int32_t C,
+                               const void *gtotal, int64_t gtotal_ld, void *gx, int64_t gx_ld, float *gweight,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * hm_gated -- the activation between an expert's two products: rows h = [gate | up] of 2 F values, ld elements apart,
+ *     a = silu(gate) * up = gate / (1 + exp(-gate)) * up
+ * as values a [rows,F] of a_dtype, or in 8 bits in the layout `rows` above (C = F), rounded once from fp32; either may be
+ * NULL, not both.  With offsets (device int32[segments + 1], a plan's dest_offset) only rows offsets[0] to
+ * offsets[segments] - 1 are written; with NULL, where segments is not looked at, all.
+ * hm_gated_backward -- from h and the gradient ga [rows,F] of a, both of dtype, the gradient of h,
+ *     s = 1 / (1 + exp(-gate)),   g_gate = ga up s (1 + gate (1 - s)),   g_up = ga gate s,
+ * in up to four forms, each NULL or not, one at least not: values gh [rows,2F] of gh_dtype; rows in 8 bits q, scale
+ * (C = 2 F), for the rows' gradient; columns in 8 bits q_columns, scale_columns (C = 2 F), and those of a itself, a_columns,
+ * a_scale (C = F), for the gradients of the two weights.  Columns need offsets; with offsets only rows of segments are
+ * written, and of columns the blocks that segments need.  Outputs lie apart from each other and from the inputs.
+ * Limits: F <= 2^20 (2^19 on the way back), segments <= 1024, rows <= 2^31 - 1 (with offsets - 128 * segments),
+ * rows * ceil(F / 512) <= 2^25 (F: 2 F on the way back), columns: (rows / 128 + segments) * ceil(F / 128) <= 2^22 - 8;
+ * beyond HM_ERR_SHAPE.  Offsets that descend or lie outside [0,rows] are data errors as above.
+ */
+hm_status hm_gated(const void *h, hm_dtype dtype, int64_t ld, const int32_t *offsets, int32_t segments, int64_t rows,
+                   int32_t F, void *a, hm_dtype a_dtype, uint8_t *q, uint8_t *scale, void *hip_stream);
+hm_status hm_gated_backward(const void *h, const void *ga, hm_dtype dtype, int64_t ld, int64_t ga_ld,
+                            const int32_t *offsets, int32_t segments, int64_t rows, int32_t F, void *gh,
+                            hm_dtype gh_dtype, uint8_t *q, uint8_t *scale, uint8_t *q_columns, uint8_t *scale_columns,
+                            uint8_t *a_columns, uint8_t *a_scale, void *hip_stream);
+
+/*
+ * hm_layer_few -- a whole layer for a few tokens on the experts that are here, experts first .. first + experts - 1 of the
+ * router's:
+ *     ids, w = hm_route(logits),   out[t] = sum over k with ids[t,k] here of w[t,k] w2_e (silu(gate) * up),
+ *     [gate; up] = w13_e x[t],   e = ids[t,k] - first
+ * x [T,H] bf16, row t from element t*ld on.  w13 [experts, 2 F, up(H,128)] (F rows of gate, then F of up) and
+ * w2 [experts, H, up(F,128)] with their scales in the layout `weights` above.  logits, bias, router, topk_ids and topk_weights
+ * as in hm_route, which is part of the call.  out [T,H] of out_dtype; a token without an expert here gets zeros.  Nothing is
+ * rounded to 8 bits on the way: sums are fp32 and activations keep 16 bits (24 for fp32 results).  A token's output depends
+ * on its own row, logits and experts alone.  With an exchange in between, the sum over the ranks is the layer's output.
+ * workspace: hm_layer_few_workspace_bytes(T, K, F) bytes of device scratch, 16-byte aligned, not shared by calls that may
+ * run at once.  Limits: T <= 64, T * K <= 1024, experts <= 1024, H <= 2^20, F <= 2^19,
+ * min(experts, T * K) * ceil(F / 128) <= 2^20; beyond HM_ERR_SHAPE.
+ */
+size_t hm_layer_few_workspace_bytes(int32_t T, int32_t K, int32_t F);
+hm_status hm_layer_few(const void *x, int64_t ld, const void *logits, hm_dtype logits_dtype, int64_t logits_ld,
+                       const float *bias, int32_t T, const hm_router *router /* host */, const uint8_t *w13,
+                       const uint8_t *w13_scale, const uint8_t *w2, const uint8_t *w2_scale, int32_t first,
+                       int32_t experts, int32_t H, int32_t F, int32_t *topk_ids, float *topk_weights, void *out,
+                       hm_dtype out_dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Static, human-readable name of a status code. */
 const char *hm_status_string(hm_status s);
 

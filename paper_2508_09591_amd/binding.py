@@ -55,7 +55,8 @@ EXPORTS = ("hm_plan_workspace_bytes", "hm_plan", "hm_plan_status", "hm_dispatch_
            "hm_swap_counts_multi", "hm_swap_multi_workspace_bytes", "hm_combine_transpose_bf16", "hm_plan_one_launch_limit", "hm_plan_one_launch_capacity",
            "hm_plan_static", "hm_plan_static_max_bytes", "hm_combine_launch_shape", "hm_route", "hm_route_backward",
            "hm_combine_weight_grad", "hm_quantize_rows", "hm_quantize_columns", "hm_quantize_weights", "hm_expert_matmul",
-           "hm_expert_matmul_dw")
+           "hm_expert_matmul_dw", "hm_rms_norm", "hm_rms_norm_backward_workspace_bytes", "hm_rms_norm_backward", "hm_gated",
+           "hm_gated_backward", "hm_layer_few_workspace_bytes", "hm_layer_few")
 
 # The entry points _hmcall is handed, in the order of its Library struct.
 _NATIVE = ("hm_plan", "hm_plan_mapped", "hm_dispatch_pack", "hm_combine", "hm_combine_f32", "hm_combine_mix", "hm_combine_transpose",
@@ -66,6 +67,8 @@ _NATIVE = ("hm_plan", "hm_plan_mapped", "hm_dispatch_pack", "hm_combine", "hm_co
 # The same for the router's and the experts' calls: its Layer struct.
 _NATIVE_LAYER = ("hm_route", "hm_route_backward", "hm_combine_weight_grad", "hm_quantize_rows", "hm_quantize_columns", "hm_quantize_weights",
                  "hm_expert_matmul", "hm_expert_matmul_dw")
+# And for what stands around them: its Around struct.
+_NATIVE_AROUND = ("hm_rms_norm", "hm_rms_norm_backward", "hm_gated", "hm_gated_backward", "hm_layer_few")
 
 
 class hm_topology(ctypes.Structure):
@@ -182,12 +185,26 @@ def lib():
                            ("hm_quantize_columns", [vp, ctypes.c_int, i64, vp, i32, i64, i32, vp, vp, vp]),
                            ("hm_quantize_weights", [vp, ctypes.c_int, i32, i32, i32, vp, vp, vp, vp, vp]),
                            ("hm_expert_matmul", [vp, vp, vp, vp, vp, i32, i64, i32, i32, vp, ctypes.c_int, vp]),
-                           ("hm_expert_matmul_dw", [vp, vp, vp, vp, vp, i32, i64, i32, i32, vp, ctypes.c_int, vp])):
+                           ("hm_expert_matmul_dw", [vp, vp, vp, vp, vp, i32, i64, i32, i32, vp, ctypes.c_int, vp]),
+                           ("hm_rms_norm", [vp, ctypes.c_int, i64, vp, ctypes.c_int, i64, vp, ctypes.c_int, ctypes.c_float, i64, i32, vp,
+                                            i64, vp, ctypes.c_int, vp, vp, vp]),
+                           ("hm_rms_norm_backward", [vp, ctypes.c_int, i64, vp, ctypes.c_int, i64, vp, ctypes.c_int, ctypes.c_float, i64,
+                                                     i32, vp, i64, vp, i64, vp, vp, ctypes.c_size_t, vp]),
+                           ("hm_gated", [vp, ctypes.c_int, i64, vp, i32, i64, i32, vp, ctypes.c_int, vp, vp, vp]),
+                           ("hm_gated_backward", [vp, vp, ctypes.c_int, i64, i64, vp, i32, i64, i32, vp, ctypes.c_int, vp, vp, vp, vp,
+                                                  vp, vp, vp]),
+                           ("hm_layer_few", [vp, i64, vp, ctypes.c_int, i64, vp, i32, router, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp,
+                                             vp, ctypes.c_int, vp, ctypes.c_size_t, vp])):
             getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_int, args
+        L.hm_rms_norm_backward_workspace_bytes.restype = ctypes.c_size_t
+        L.hm_rms_norm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.hm_layer_few_workspace_bytes.restype = ctypes.c_size_t
+        L.hm_layer_few_workspace_bytes.argtypes = [i32, i32, i32]
         L.hm_status_string.restype = ctypes.c_char_p
         L.hm_status_string.argtypes = [ctypes.c_int]
         _native.bind(*[ctypes.cast(getattr(L, name), vp).value for name in _NATIVE])
         _native.bind_layer(*[ctypes.cast(getattr(L, name), vp).value for name in _NATIVE_LAYER])
+        _native.bind_around(*[ctypes.cast(getattr(L, name), vp).value for name in _NATIVE_AROUND])
         _lib = L
     return _lib
 
@@ -842,3 +859,191 @@ def hm_expert_matmul_dw(gy: torch.Tensor, gy_scale: torch.Tensor, x: torch.Tenso
                                    _dev(dw, dw.dtype, "dw"), _sums(dw, "dw", full_sums), _stream(stream))
     _check("hm_expert_matmul_dw", rc)
     return dw
+
+
+# ---- around the experts' products -----------------------------------------------------------------------------------
+def _device_of(stream, *tensors):
+    """The current device, or the given stream's; refuses tensors of another, whose memory a launch there may not reach."""
+    here = torch._C._cuda_getDevice() if stream is None else stream.device_index
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != here:
+            raise ValueError("a tensor is on device %d, the call on device %d" % (t.get_device(), here))
+
+
+def _optional_rows(t: Optional[torch.Tensor], shape, name: str):
+    """(address, elements from row to row) of a matrix that may be left out."""
+    return (None, 0) if t is None else _rows_of(_shaped(t, shape, name), name)
+
+
+def _optional_floats(t: Optional[torch.Tensor], name: str) -> int:
+    return HM_BF16 if t is None else _floats(t, name)
+
+
+def _pair8(q, scale, shape, scale_shape, name: str):
+    """Addresses of values in 8 bits and their scales, both or neither."""
+    if (q is None) != (scale is None):
+        raise ValueError("%s and its scales go together" % name)
+    return (None, None) if q is None else (_codes(q, shape, name), _scales(scale, scale_shape, "the scales of " + name))
+
+
+def alloc_rms_norm_workspace(rows: int, C: int, device="cuda") -> torch.Tensor:
+    """Scratch for hm_rms_norm_backward."""
+    return torch.empty(int(lib().hm_rms_norm_backward_workspace_bytes(rows, C)), dtype=torch.uint8, device=device)
+
+
+def alloc_layer_few_workspace(T: int, router: Router, H: int, F: int, device="cuda") -> torch.Tensor:
+    """Scratch for hm_layer_few of up to T tokens."""
+    return torch.empty(int(lib().hm_layer_few_workspace_bytes(T, router.K, F)), dtype=torch.uint8, device=device)
+
+
+def hm_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, y: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                scale: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None,
+                stream=None):
+    """y, or (q, scale) = hm_quantize_rows of it, or both: the norm of x, or of total = x + residual.  Returns (y, q, scale, total)."""
+    rc = _native.rms_norm(x, weight, eps, y, q, scale, residual, total) if stream is None else None
+    if rc is not None:
+        _check("hm_rms_norm", rc)
+        return y, q, scale, total
+    at, ld = _rows_of(x, "x")
+    rows, C = x.shape
+    _device_of(stream, x, weight, y, q, scale, residual, total)
+    r, r_ld = _optional_rows(residual, (rows, C), "residual")
+    t, t_ld = _optional_rows(total, (rows, C), "total")
+    if residual is not None and total is not None and residual.dtype != total.dtype:
+        raise TypeError("total must be %s as the residual is, got %s" % (residual.dtype, total.dtype))
+    if (residual is None) != (total is None):
+        raise ValueError("residual and total go together")
+    if y is None and q is None:
+        raise ValueError("y, or q and its scales, must be given")
+    codes = _pair8(q, scale, (rows, row8_bytes(C)), (rows, scale8_bytes(C)), "q")
+    rc = lib().hm_rms_norm(at, _floats(x, "x"), ld, r, _optional_floats(residual, "residual"), r_ld,
+                           _dev(_shaped(weight, (C,), "weight"), weight.dtype, "weight"), _floats(weight, "weight"), float(eps), rows, C, t, t_ld,
+                           None if y is None else _dev(_shaped(y, (rows, C), "y"), y.dtype, "y"), _optional_floats(y, "y"), *codes,
+                           _stream(stream))
+    _check("hm_rms_norm", rc)
+    return y, q, scale, total
+
+
+def hm_rms_norm_backward(gy: torch.Tensor, s: torch.Tensor, weight: torch.Tensor, eps: float, gx: torch.Tensor, gweight: torch.Tensor,
+                         gtotal: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """s: what was normed, hm_rms_norm's total or, without a residual, its x.  Returns (gx, gweight)."""
+    rc = _native.rms_norm_backward(gy, s, weight, eps, gx, gweight, gtotal, workspace) if stream is None else None
+    if rc is not None:
+        _check("hm_rms_norm_backward", rc)
+        return gx, gweight
+    at, ld = _rows_of(s, "s")
+    rows, C = s.shape
+    _device_of(stream, gy, s, weight, gx, gweight, gtotal, workspace)
+    g, g_ld = _rows_of(_shaped(gy, (rows, C), "gy"), "gy")
+    to, to_ld = _rows_of(_shaped(gx, (rows, C), "gx"), "gx")
+    t, t_ld = _optional_rows(gtotal, (rows, C), "gtotal")
+    for name, other in (("gx", gx), ("gtotal", gtotal)):
+        if other is not None and other.dtype != s.dtype:
+            raise TypeError("%s must be %s as s is, got %s" % (name, s.dtype, other.dtype))
+    if workspace is None:
+        workspace = alloc_rms_norm_workspace(rows, C, device=s.device)
+    rc = lib().hm_rms_norm_backward(g, _floats(gy, "gy"), g_ld, at, _floats(s, "s"), ld,
+                                    _dev(_shaped(weight, (C,), "weight"), weight.dtype, "weight"), _floats(weight, "weight"), float(eps), rows, C,
+                                    t, t_ld, to, to_ld, _dev(_shaped(gweight, (C,), "gweight"), torch.float32, "gweight"),
+                                    *_scratch(workspace), _stream(stream))
+    _check("hm_rms_norm_backward", rc)
+    return gx, gweight
+
+
+def _scratch(workspace: torch.Tensor):
+    """(address, bytes) of a workspace of any type."""
+    return _dev(workspace, workspace.dtype, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def hm_gated(h: torch.Tensor, a: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+             offsets: Optional[torch.Tensor] = None, stream=None):
+    """a = silu(gate) * up of h [rows, 2 F] = [gate | up], as values or in 8 bits; with offsets (a plan's dest_offset) of the rows that
+    a segment has.  Returns (a, q, scale)."""
+    rc = _native.gated(h, a, q, scale, offsets) if stream is None else None
+    if rc is not None:
+        _check("hm_gated", rc)
+        return a, q, scale
+    at, ld = _rows_of(h, "h")
+    rows, F = h.shape[0], h.shape[1] // 2
+    _device_of(stream, h, a, q, scale, offsets)
+    if h.shape[1] != 2 * F:
+        raise ValueError("h must have as many columns of gate as of up, got %d in all" % h.shape[1])
+    if a is None and q is None:
+        raise ValueError("a, or q and its scales, must be given")
+    codes = _pair8(q, scale, (rows, row8_bytes(F)), (rows, scale8_bytes(F)), "q")
+    rc = lib().hm_gated(at, _floats(h, "h"), ld, _dev(offsets, torch.int32, "offsets"), 0 if offsets is None else offsets.numel() - 1, rows, F,
+                        None if a is None else _dev(_shaped(a, (rows, F), "a"), a.dtype, "a"), _optional_floats(a, "a"), *codes,
+                        _stream(stream))
+    _check("hm_gated", rc)
+    return a, q, scale
+
+
+def hm_gated_backward(h: torch.Tensor, ga: torch.Tensor, offsets: Optional[torch.Tensor] = None, gh: Optional[torch.Tensor] = None,
+                      q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, q_columns: Optional[torch.Tensor] = None,
+                      scale_columns: Optional[torch.Tensor] = None, a_columns: Optional[torch.Tensor] = None,
+                      a_scale: Optional[torch.Tensor] = None, stream=None):
+    """The gradient of h from that of a, as values gh, as rows in 8 bits (q, scale), as columns in 8 bits (q_columns, scale_columns), and a
+    itself as columns in 8 bits (a_columns, a_scale): what is given is written.  Returns them in that order."""
+    outputs = (gh, q, scale, q_columns, scale_columns, a_columns, a_scale)
+    rc = _native.gated_backward(h, ga, offsets, *outputs) if stream is None else None
+    if rc is not None:
+        _check("hm_gated_backward", rc)
+        return outputs
+    at, ld = _rows_of(h, "h")
+    rows, F = h.shape[0], h.shape[1] // 2
+    _device_of(stream, h, ga, offsets, *outputs)
+    if h.shape[1] != 2 * F:
+        raise ValueError("h must have as many columns of gate as of up, got %d in all" % h.shape[1])
+    g, g_ld = _rows_of(_shaped(ga, (rows, F), "ga"), "ga")
+    if ga.dtype != h.dtype:
+        raise TypeError("ga must be %s as h is, got %s" % (h.dtype, ga.dtype))
+    if gh is None and q is None and q_columns is None and a_columns is None:
+        raise ValueError("one of the outputs must be given")
+    if offsets is None and (q_columns is not None or a_columns is not None):
+        raise ValueError("columns need offsets")
+    segments = 0 if offsets is None else offsets.numel() - 1
+    blocks = rows // 128 + segments
+    rc = lib().hm_gated_backward(at, g, _floats(h, "h"), ld, g_ld, _dev(offsets, torch.int32, "offsets"), segments, rows, F,
+                                 None if gh is None else _dev(_shaped(gh, (rows, 2 * F), "gh"), gh.dtype, "gh"), _optional_floats(gh, "gh"),
+                                 *_pair8(q, scale, (rows, row8_bytes(2 * F)), (rows, scale8_bytes(2 * F)), "q"),
+                                 *_pair8(q_columns, scale_columns, (2 * F, 128 * blocks), (blocks, 2 * F), "q_columns"),
+                                 *_pair8(a_columns, a_scale, (F, 128 * blocks), (blocks, F), "a_columns"), _stream(stream))
+    _check("hm_gated_backward", rc)
+    return outputs
+
+
+def hm_layer_few(x: torch.Tensor, logits: torch.Tensor, router: Router, w13: torch.Tensor, w13_scale: torch.Tensor, w2: torch.Tensor,
+                 w2_scale: torch.Tensor, topk_ids: torch.Tensor, topk_weights: torch.Tensor, out: torch.Tensor,
+                 workspace: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, first: int = 0, stream=None) -> torch.Tensor:
+    """The output of a layer for up to 64 tokens: choice, both products of the chosen experts that are here (first and those behind it,
+    as many as the weights hold), activation and sum.  topk_ids and topk_weights are written as hm_route does."""
+    rc = _native.layer_few(x, logits, router, w13, w13_scale, w2, w2_scale, topk_ids, topk_weights, out, workspace, bias, first) \
+        if stream is None else None
+    if rc is not None:
+        _check("hm_layer_few", rc)
+        return out
+    at, ld = _rows_of(x, "x")
+    from_logits, logits_ld = _rows_of(logits, "logits")
+    (T, H), (experts, wide, _), K = x.shape, w13.shape, router.K
+    F = wide // 2
+    _device_of(stream, x, logits, w13, w13_scale, w2, w2_scale, topk_ids, topk_weights, out, workspace, bias)
+    if x.dtype != torch.bfloat16:
+        raise TypeError("x must be torch.bfloat16, got %s" % x.dtype)
+    if wide != 2 * F:
+        raise ValueError("w13 must have as many rows of gate as of up, got %d in all" % wide)
+    if logits.shape != (T, router.E):
+        raise ValueError("logits must be %s, got %s" % ((T, router.E), tuple(logits.shape)))
+    if bias is not None:
+        _shaped(bias, (router.E,), "bias")
+    if workspace is None:
+        workspace = alloc_layer_few_workspace(T, router, H, F, device=x.device)
+    rc = lib().hm_layer_few(at, ld, from_logits, _floats(logits, "logits"), logits_ld, _dev(bias, torch.float32, "bias"), T, router.ref(),
+                            _codes(w13, (experts, wide, row8_bytes(H)), "w13"),
+                            _scales(w13_scale, (experts, (wide + 127) // 128, scale8_bytes(H)), "w13_scale"),
+                            _codes(w2, (experts, H, row8_bytes(F)), "w2"),
+                            _scales(w2_scale, (experts, (H + 127) // 128, scale8_bytes(F)), "w2_scale"), first, experts, H, F,
+                            _dev(_shaped(topk_ids, (T, K), "topk_ids"), torch.int32, "topk_ids"),
+                            _dev(_shaped(topk_weights, (T, K), "topk_weights"), torch.float32, "topk_weights"),
+                            _dev(_shaped(out, (T, H), "out"), out.dtype, "out"), _floats(out, "out"), *_scratch(workspace), _stream(stream))
+    _check("hm_layer_few", rc)
+    return out

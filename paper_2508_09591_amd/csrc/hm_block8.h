@@ -28,6 +28,27 @@ __device__ __forceinline__ Segment8 segment8(const int32_t *__restrict__ offsets
   return {from, min(max(offsets[segment + 1], from), rows)};
 }
 
+// The segment that owns block b, the last whose first block is not behind it, and its rows; called by whole waves.
+// Both offsets of a lane's segment are loaded together: what follows waits for one trip to memory.
+struct BlockOwner8 {
+  int segment;   // -1: none
+  Segment8 rows;
+};
+__device__ __forceinline__ BlockOwner8 owner_of_block8(const int32_t *__restrict__ offsets, int segments, int rows,
+                                                       int b) {
+  const int lane = lane_id();
+  BlockOwner8 owner = {-1, {0, 0}};
+  for (int e0 = 0; e0 < segments; e0 += kWave) {
+    const int e = e0 + lane;
+    const Segment8 s = segment8(offsets, min(e, segments - 1), rows);
+    const uint64_t upto = __ballot(e < segments && first_block8(s.from, e) <= b);
+    if (upto == 0) break;
+    const int l = 63 - __builtin_clzll(upto);
+    owner = {e0 + l, {read_lane(s.from, l), read_lane(s.to, l)}};
+  }
+  return owner;
+}
+
 constexpr uint32_t kInfinityBits = 0x7F800000u;
 
 // Scale code of a block whose largest finite value has these bits: the least exponent e with amax <= 448 * 2^e, + 127.
@@ -62,6 +83,28 @@ __device__ __forceinline__ uint32_t largest_bits(float (&v)[N]) {
 __device__ __forceinline__ uint32_t pack8(float a, float b, float c, float d, float by) {
   const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a * by, b * by, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * by, d * by, low, true);
+}
+
+// Largest value of the sixteen lanes of a row, in all of them.
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xF, 0xF, true));
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xF, 0xF, true));
+}
+
+// Eight values a lane of the 512 columns from 512 `part` on of a row in 8 bits: the row's bytes, `width` of them, and its
+// scales; sixteen lanes have a block.  What lies behind the row's end is zero.  Called by whole waves.
+__device__ __forceinline__ void store_piece8(uint8_t *q, uint8_t *scale, int part, int width, float (&v)[8]) {
+  const int lane = lane_id(), c = part * 512 + lane * 8;
+  const int code = scale_code8(max16(largest_bits(v)));
+  const float by = inverse_scale8(code);
+  if (c < width)
+    *(uint64_t *)(q + c) = (uint64_t)pack8(v[4], v[5], v[6], v[7], by) << 32 | pack8(v[0], v[1], v[2], v[3], by);
+  const uint32_t mine = c < width ? (uint32_t)code : 0u;   // behind the last block zeros
+  const uint32_t codes = (uint32_t)read_lane((int)mine, 0) | (uint32_t)read_lane((int)mine, 16) << 8 |
+                         (uint32_t)read_lane((int)mine, 32) << 16 | (uint32_t)read_lane((int)mine, 48) << 24;
+  if (lane == 0) *(uint32_t *)(scale + part * 4) = codes;
 }
 
 typedef f32x4 f32x4_align4 __attribute__((aligned(4)));
@@ -115,8 +158,68 @@ __device__ __forceinline__ void load_row_end(const IN *__restrict__ row, int c, 
   for (int i = 0; i < N; ++i) v[i] = by < N ? v[i] : 0.0f;
 }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+// Eight values as bf16, times their block's power of two, of which the conversion takes the exponent (code 0 too is
+// 2^-127).  Exact down to the least subnormal, 2^-133: values are multiples of 2^-9, so that codes from 3 on lose
+// nothing.  2^128, to which what lies next to fp32's largest number is rounded (256 under code 247), is infinite.
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi, uint32_t code) {
+  const float power = __builtin_bit_cast(float, (code & 0xFFu) << 23);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true);
+  return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// N consecutive elements, to nearest even; any alignment of the elements.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {   // two an instruction
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
+}
+__device__ __forceinline__ void store_eight(uint16_t *p, const float (&v)[8]) {
+  *(u32x4_align2 *)p = u32x4{round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]),
+                             round_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void store_eight(float *p, const float (&v)[8]) {
+  *(f32x4_align4 *)p = f32x4{v[0], v[1], v[2], v[3]};
+  *(f32x4_align4 *)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store_float(uint16_t *p, float v) { *p = (uint16_t)round_bf16x2(v, v); }
+__device__ __forceinline__ void store_float(float *p, float v) { *p = v; }
+// Elements c to c + 7 of a row of C.
+template <typename OUT>
+__device__ __forceinline__ void store_row(OUT *row, int c, int C, const float (&v)[8]) {
+  if (c + 8 <= C) {
+    store_eight(row + c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < C) store_float(row + c + i, v[i]);
+  }
+}
+// The same loaded, zeros behind the row's end; `whole` (uniform): none of the wave's reach it.
+template <typename IN>
+__device__ __forceinline__ void load_row(const IN *__restrict__ row, int c, int C, bool whole, float (&v)[8]) {
+  if (whole) load_floats<8>(row + c, v);
+  else load_row_end<8>(row, c, C, v);
+}
+// Rounded to the type of OUT, as fp32.
+__device__ __forceinline__ void round_to(const uint16_t *, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const uint32_t w = round_bf16x2(v[i], v[i + 1]);
+    v[i] = bf16_lo(w);
+    v[i + 1] = bf16_hi(w);
+  }
+}
+__device__ __forceinline__ void round_to(const float *, float (&)[8]) {}
+
 static inline bool buffers8_aligned(const void *q, const void *scale) {
   return ((uintptr_t)q & 15) == 0 && ((uintptr_t)scale & 3) == 0;
+}
+static inline bool aligned_as(hm_dtype dtype, const void *at) {
+  return ((uintptr_t)at & (dtype == HM_F32 ? 3 : 1)) == 0;
 }
 static inline bool dtype_known(hm_dtype dtype) { return dtype == HM_BF16 || dtype == HM_F32; }
 constexpr int kMostSegments8 = 1024, kMostColumns8 = 1 << 20;

@@ -603,6 +603,172 @@ PyObject *expert_matmul_dw(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// ---- around the experts' products ----
+struct Around {
+  decltype(&hm_rms_norm) rms_norm;
+  decltype(&hm_rms_norm_backward) rms_norm_backward;
+  decltype(&hm_gated) gated;
+  decltype(&hm_gated_backward) gated_backward;
+  decltype(&hm_layer_few) layer_few;
+} around;
+bool around_bound = false;
+
+template <typename Body>
+PyObject *around_answer(Py_ssize_t given, Py_ssize_t wanted, Body body) {
+  if (around_bound && given == wanted) {
+    try {
+      return PyLong_FromLong(body());
+    } catch (...) {   // as in answer()
+      PyErr_Clear();
+    }
+  }
+  Py_RETURN_NONE;
+}
+
+// A tensor on the current device.
+const at::Tensor &here(PyObject *o) {
+  const at::Tensor &t = tensor(o);
+  if (!t.is_cuda() || t.get_device() != c10::hip::current_device() || !t.is_contiguous()) throw NotOrdinary();
+  return t;
+}
+struct Floats {   // a dense tensor of floats of a given shape, or none
+  void *at = nullptr;
+  hm_dtype dtype = HM_BF16;
+};
+Floats floats_or_none(PyObject *o, std::initializer_list<int64_t> sizes) {
+  if (o == Py_None) return {};
+  const at::Tensor &t = here(o);
+  if (t.sizes() != at::IntArrayRef(sizes)) throw NotOrdinary();
+  return {t.data_ptr(), floats(t)};
+}
+Floats floats_of(PyObject *o, std::initializer_list<int64_t> sizes) {
+  const Floats f = floats_or_none(o, sizes);
+  if (!f.at && o == Py_None) throw NotOrdinary();
+  return f;
+}
+Floats floats_of(PyObject *o, std::initializer_list<int64_t> sizes, hm_dtype dtype) {
+  const Floats f = floats_of(o, sizes);
+  if (f.dtype != dtype) throw NotOrdinary();
+  return f;
+}
+struct Pair8 {
+  uint8_t *q = nullptr, *scale = nullptr;
+};
+Pair8 pair8(PyObject *q, PyObject *scale, std::initializer_list<int64_t> sizes, std::initializer_list<int64_t> scale_sizes) {
+  const at::Tensor &a = here(q), &b = here(scale);
+  if (a.scalar_type() != at::kFloat8_e4m3fn || (b.scalar_type() != at::kByte && b.scalar_type() != at::kFloat8_e8m0fnu)) throw NotOrdinary();
+  if (a.sizes() != at::IntArrayRef(sizes) || b.sizes() != at::IntArrayRef(scale_sizes)) throw NotOrdinary();
+  return {static_cast<uint8_t *>(a.data_ptr()), static_cast<uint8_t *>(b.data_ptr())};
+}
+Pair8 pair8_or_none(PyObject *q, PyObject *scale, std::initializer_list<int64_t> sizes, std::initializer_list<int64_t> scale_sizes) {
+  if (q == Py_None && scale == Py_None) return {};
+  return pair8(q, scale, sizes, scale_sizes);
+}
+const int32_t *offsets_or_none(PyObject *o, int32_t &segments) {
+  segments = 0;
+  if (o == Py_None) return nullptr;
+  const at::Tensor &t = here(o);
+  if (t.scalar_type() != at::kInt) throw NotOrdinary();
+  segments = size32(t.numel() - 1);
+  return static_cast<const int32_t *>(t.data_ptr());
+}
+
+// x, weight, eps, y, q, scale, residual, total
+PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return around_answer(n, 8, [&] {
+    int32_t rows, C;
+    shape(here(a[0]), rows, C);
+    const Floats x = floats_of(a[0], {rows, C}), w = floats_of(a[1], {C}), y = floats_or_none(a[3], {rows, C});
+    const float eps = static_cast<float>(real(a[2]));
+    const Pair8 q = pair8_or_none(a[4], a[5], {rows, up(C, 128)}, {rows, up(C, 512) / 128});
+    const Floats r = floats_or_none(a[6], {rows, C}), total = floats_or_none(a[7], {rows, C});
+    if ((a[6] == Py_None) != (a[7] == Py_None) || r.dtype != total.dtype || (a[3] == Py_None && a[4] == Py_None)) throw NotOrdinary();
+    return launched([&](void *s) {
+      return around.rms_norm(x.at, x.dtype, C, r.at, r.dtype, C, w.at, w.dtype, eps, rows, C, total.at, C, y.at, y.dtype, q.q, q.scale, s);
+    });
+  });
+}
+
+// gy, s, weight, eps, gx, gweight, gtotal, workspace
+PyObject *rms_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return around_answer(n, 8, [&] {
+    int32_t rows, C;
+    shape(here(a[1]), rows, C);
+    const Floats gy = floats_of(a[0], {rows, C}), v = floats_of(a[1], {rows, C}), w = floats_of(a[2], {C});
+    const float eps = static_cast<float>(real(a[3]));
+    const Floats gx = floats_of(a[4], {rows, C}, v.dtype), gw = floats_of(a[5], {C}, HM_F32);
+    const Floats gt = a[6] == Py_None ? Floats() : floats_of(a[6], {rows, C}, v.dtype);
+    const at::Tensor &ws = here(a[7]);
+    return launched([&](void *s) {
+      return around.rms_norm_backward(gy.at, gy.dtype, C, v.at, v.dtype, C, w.at, w.dtype, eps, rows, C, gt.at, C, gx.at, C,
+                                      static_cast<float *>(gw.at), ws.data_ptr(), ws.nbytes(), s);
+    });
+  });
+}
+
+PyObject *gated(PyObject *, PyObject *const *a, Py_ssize_t n) {   // h, a, q, scale, offsets
+  return around_answer(n, 5, [&] {
+    int32_t rows, wide, segments;
+    shape(here(a[0]), rows, wide);
+    const int32_t F = wide / 2;
+    if (wide != 2 * F || (a[1] == Py_None && a[2] == Py_None)) throw NotOrdinary();
+    const Floats h = floats_of(a[0], {rows, wide}), out = floats_or_none(a[1], {rows, F});
+    const Pair8 q = pair8_or_none(a[2], a[3], {rows, up(F, 128)}, {rows, up(F, 512) / 128});
+    const int32_t *offsets = offsets_or_none(a[4], segments);
+    return launched([&](void *s) {
+      return around.gated(h.at, h.dtype, wide, offsets, segments, rows, F, out.at, out.dtype, q.q, q.scale, s);
+    });
+  });
+}
+
+// h, ga, offsets, gh, q, scale, q_columns, scale_columns, a_columns, a_scale
+PyObject *gated_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return around_answer(n, 10, [&] {
+    int32_t rows, wide, segments;
+    shape(here(a[0]), rows, wide);
+    const int32_t F = wide / 2;
+    if (wide != 2 * F) throw NotOrdinary();
+    const Floats h = floats_of(a[0], {rows, wide}), ga = floats_of(a[1], {rows, F}, h.dtype), gh = floats_or_none(a[3], {rows, wide});
+    const int32_t *offsets = offsets_or_none(a[2], segments);
+    const int64_t blocks = rows / 128 + static_cast<int64_t>(segments);
+    const Pair8 q = pair8_or_none(a[4], a[5], {rows, up(wide, 128)}, {rows, up(wide, 512) / 128});
+    const Pair8 qc = pair8_or_none(a[6], a[7], {wide, 128 * blocks}, {blocks, wide});
+    const Pair8 ac = pair8_or_none(a[8], a[9], {F, 128 * blocks}, {blocks, F});
+    const bool columns = a[6] != Py_None || a[8] != Py_None;
+    if ((columns && !offsets) || (a[3] == Py_None && a[4] == Py_None && !columns)) throw NotOrdinary();
+    return launched([&](void *s) {
+      return around.gated_backward(h.at, ga.at, h.dtype, wide, F, offsets, segments, rows, F, gh.at, gh.dtype, q.q, q.scale, qc.q, qc.scale,
+                                   ac.q, ac.scale, s);
+    });
+  });
+}
+
+// x, logits, router, w13, w13_scale, w2, w2_scale, ids, weights, out, workspace, bias, first
+PyObject *layer_few(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return around_answer(n, 13, [&] {
+    int32_t T, H;
+    shape(here(a[0]), T, H);
+    const Router r(a[2]);
+    const int64_t E = r.c()->E, K = r.c()->K;
+    const Floats x = floats_of(a[0], {T, H}, HM_BF16), logits = floats_of(a[1], {T, E}), out = floats_of(a[9], {T, H});
+    const at::Tensor &w = here(a[3]);
+    if (w.dim() != 3) throw NotOrdinary();
+    const int32_t experts = size32(w.size(0)), wide = size32(w.size(1)), F = wide / 2;
+    if (wide != 2 * F) throw NotOrdinary();
+    const Pair8 w13 = pair8(a[3], a[4], {experts, wide, up(H, 128)}, {experts, up(wide, 128) / 128, up(H, 512) / 128});
+    const Pair8 w2 = pair8(a[5], a[6], {experts, H, up(F, 128)}, {experts, up(H, 128) / 128, up(F, 512) / 128});
+    const at::Tensor &ids = here(a[7]), &ws = here(a[10]);
+    if (ids.scalar_type() != at::kInt || ids.sizes() != at::IntArrayRef({static_cast<int64_t>(T), K})) throw NotOrdinary();
+    const Floats weights = floats_of(a[8], {T, K}, HM_F32), bias = a[11] == Py_None ? Floats() : floats_of(a[11], {E}, HM_F32);
+    const int32_t first = integer32(a[12]);
+    return launched([&](void *s) {
+      return around.layer_few(x.at, H, logits.at, logits.dtype, E, static_cast<const float *>(bias.at), T, r.c(), w13.q, w13.scale, w2.q,
+                              w2.scale, first, experts, H, F, static_cast<int32_t *>(ids.data_ptr()), static_cast<float *>(weights.at),
+                              out.at, out.dtype, ws.data_ptr(), ws.nbytes(), s);
+    });
+  });
+}
+
 // Takes the addresses of a struct's entry points, in its order.
 template <typename Entries>
 PyObject *take(Entries &entries, bool &done, PyObject *const *a, Py_ssize_t n) {
@@ -625,6 +791,7 @@ PyObject *take(Entries &entries, bool &done, PyObject *const *a, Py_ssize_t n) {
 }
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) { return take(lib, bound, a, n); }
 PyObject *bind_layer(PyObject *, PyObject *const *a, Py_ssize_t n) { return take(layer, layer_bound, a, n); }
+PyObject *bind_around(PyObject *, PyObject *const *a, Py_ssize_t n) { return take(around, around_bound, a, n); }
 
 #define HM_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HM_METHOD(plan), HM_METHOD(plan_mapped), HM_METHOD(dispatch_pack), HM_METHOD(combine), HM_METHOD(combine_f32),
@@ -633,6 +800,8 @@ PyMethodDef methods[] = {HM_METHOD(plan), HM_METHOD(plan_mapped), HM_METHOD(disp
                          HM_METHOD(swap_select), HM_METHOD(swap_apply), HM_METHOD(bind), HM_METHOD(route), HM_METHOD(route_backward),
                          HM_METHOD(combine_weight_grad), HM_METHOD(quantize_rows), HM_METHOD(quantize_columns),
                          HM_METHOD(quantize_weights), HM_METHOD(expert_matmul), HM_METHOD(expert_matmul_dw), HM_METHOD(bind_layer),
+                         HM_METHOD(rms_norm), HM_METHOD(rms_norm_backward), HM_METHOD(gated), HM_METHOD(gated_backward),
+                         HM_METHOD(layer_few), HM_METHOD(bind_around),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hmcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

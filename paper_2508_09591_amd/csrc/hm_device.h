@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "hiermoe.h"
 
 namespace hm {
@@ -215,6 +217,22 @@ __device__ __forceinline__ int read_lane(int v, int src) { return __builtin_amdg
 __device__ __forceinline__ float read_lane(float v, int src) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), src));
 }
+
+// Over all lanes, the result in each: within rows of sixteen by rotations, then the four rows.
+template <typename OP>
+__device__ __forceinline__ float wave_all(float v, OP op) {
+  auto turned = [](float x, auto control) {
+    const int from = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), control(), 0xF, 0xF, true);
+    return __builtin_bit_cast(float, from);
+  };
+  v = op(v, turned(v, std::integral_constant<int, 0x128>()));
+  v = op(v, turned(v, std::integral_constant<int, 0x124>()));
+  v = op(v, turned(v, std::integral_constant<int, 0x122>()));
+  v = op(v, turned(v, std::integral_constant<int, 0x121>()));
+  return op(op(read_lane(v, 0), read_lane(v, 16)), op(read_lane(v, 32), read_lane(v, 48)));
+}
+__device__ __forceinline__ float wave_max(float v) { return wave_all(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_sum(float v) { return wave_all(v, [](float a, float b) { return a + b; }); }
 
 // bf16 pair packed in one 32-bit word -> two floats (low half first).
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }

@@ -23,8 +23,6 @@ namespace hm {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 struct ProductParams {
   const uint8_t *q, *q_scale, *p, *p_scale;
@@ -101,21 +99,10 @@ struct Slice<true> {   // 16 values: two instructions, a quarter of a step
   __device__ __forceinline__ void read(const uint8_t *lds, const uint32_t (&at)[4], int fragment, int part) {
     v = *(const i32x4 *)(lds + at[part] + fragment);
   }
-  // Eight values as bf16, times their block's power of two, of which the conversion takes the exponent (code 0 too is
-  // 2^-127).  Exact down to the least subnormal, 2^-133: values are multiples of 2^-9, so that codes from 3 on lose
-  // nothing.  2^128, to which what lies next to fp32's largest number is rounded (256 under code 247), is infinite.
-  static __device__ __forceinline__ bf16x8 widen(int lo, int hi, uint32_t code) {
-    const float power = __builtin_bit_cast(float, (code & 0xFFu) << 23);
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, false);
-    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, power, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, false);
-    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, power, true);
-    return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-  }
   static constexpr int kProducts = 2;
   __device__ __forceinline__ void times(const Slice &q, uint32_t code_p, uint32_t code_q, f32x16 &acc, int h) const {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(v[2 * h], v[2 * h + 1], code_p),
-                                                  widen(q.v[2 * h], q.v[2 * h + 1], code_q), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(v[2 * h], v[2 * h + 1], code_p),
+                                                  widen8(q.v[2 * h], q.v[2 * h + 1], code_q), acc, 0, 0, 0);
   }
 };
 
@@ -451,8 +438,8 @@ __global__ __launch_bounds__(kThinWaves * kWave) void thin_product_kernel(Produc
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            Slice<true>::widen(g.w[s][2 * i], g.w[s][2 * i + 1], g.sp >> 8 * s),
-            Slice<true>::widen(g.q[s][2 * i], g.q[s][2 * i + 1], g.sq >> 8 * s), acc, 0, 0, 0);
+            widen8(g.w[s][2 * i], g.w[s][2 * i + 1], g.sp >> 8 * s),
+            widen8(g.q[s][2 * i], g.q[s][2 * i + 1], g.sq >> 8 * s), acc, 0, 0, 0);
     }
   };
   Group a, b;   // one on its way while the other is multiplied

@@ -1,0 +1,312 @@
+// The norm in front of a layer: s = x + residual, y = s m^-1/2 w with m = mean(s^2) + eps, as values and in 8 bits, and the
+// way back:
+//     u = gy w,   gs = m^-1/2 (u - s mean(u s) / m) + gtotal,   gw = sum over the rows of gy s m^-1/2.
+// Both need a row's sums before they can write the row, so a row stays in registers between: THREADS threads have VEC
+// vectors of eight values of it, the k-th of thread i being vector k THREADS + i.  A wave's vectors are 512 neighbouring
+// columns, four blocks of 8 bits.
+#include "hm_block8.h"
+
+namespace hm {
+
+constexpr int kMostNormColumns = 32768;   // 1,024 threads of four vectors
+
+struct NormParams {
+  const void *x, *residual, *weight;
+  void *total, *y;
+  uint8_t *q, *scale;
+  int64_t ld, residual_ld, total_ld, rows;
+  int32_t C;
+  float eps;
+  bool weight_bf16, y_bf16;
+};
+
+// The sum over a row's threads, in all of them; `sums` has a place for every wave, another one from call to call, so that one
+// barrier is enough.
+template <int THREADS, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (&sums)[2][N][THREADS / kWave > 0 ? THREADS / kWave : 1], int turn) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
+  if constexpr (THREADS > kWave) {
+    const int wave = threadIdx.x / kWave;
+    if (lane_id() == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) sums[turn][n][wave] = v[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      v[n] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < THREADS / kWave; ++w) v[n] += sums[turn][n][w];
+    }
+  }
+}
+
+// A vector of the weight of either type.
+__device__ __forceinline__ void load_weight(const void *weight, bool bf16, int c, int C, float (&v)[8]) {
+  if (bf16) load_row_end<8>((const uint16_t *)weight, c, C, v);
+  else load_row_end<8>((const float *)weight, c, C, v);
+}
+
+// Threads of a workgroup: a row's, or four rows of a wave each.
+template <int THREADS>
+constexpr int norm_block() { return THREADS < 256 ? 256 : THREADS; }
+
+template <typename IN, typename SUM, int VEC, int THREADS>
+__global__ __launch_bounds__(norm_block<THREADS>()) void rms_norm_kernel(NormParams p) {
+  constexpr int kRows = norm_block<THREADS>() / THREADS;   // of a workgroup
+  __shared__ float sums[2][1][THREADS / kWave];
+  const int tid = threadIdx.x % THREADS, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int first_part = THREADS < 256 ? 0 : wave;   // the wave's pieces of 512 columns: this one, and every kStep-th behind it
+  constexpr int kStep = THREADS / kWave;
+  const int width = (int)row8_bytes(p.C);
+  float w[VEC][8];
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) load_weight(p.weight, p.weight_bf16, (k * THREADS + tid) * 8, p.C, w[k]);
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + (THREADS < 256 ? wave : 0); row < p.rows; row += (int64_t)gridDim.x * kRows) {
+    float v[VEC][8], sum[1] = {0.0f};
+    const IN *x = (const IN *)p.x + row * p.ld;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) load_row(x, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C, v[k]);
+    if (p.residual) {
+      const SUM *r = (const SUM *)p.residual + row * p.residual_ld;
+      float add[VEC][8];
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) load_row(r, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C, add[k]);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[k][i] += add[k][i];
+        round_to((const SUM *)nullptr, v[k]);   // what is normed is the sum as it is kept, so that the way back sees the same
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[0] = fmaf(v[k][i], v[k][i], sum[0]);
+    row_sums<THREADS>(sum, sums, turn);
+    turn ^= 1;
+    const float by = 1.0f / sqrtf(sum[0] / (float)p.C + p.eps);
+    // Stores come behind the barrier: outputs may take the place of the row's inputs, of which a thread at a row's end reads more
+    // than it has.
+    if (p.residual) {
+      SUM *total = (SUM *)p.total + row * p.total_ld;
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) store_row(total, (k * THREADS + tid) * 8, p.C, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const int c = (k * THREADS + tid) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * by * w[k][i];
+      if (p.y) {
+        if (p.y_bf16) store_row((uint16_t *)p.y + row * p.C, c, p.C, v[k]);
+        else store_row((float *)p.y + row * p.C, c, p.C, v[k]);
+      }
+      const int part = first_part + k * kStep;
+      if (p.q && part * 512 < p.C) store_piece8(p.q + row * width, p.scale + row * scale8_bytes(p.C), part, width, v[k]);
+    }
+  }
+}
+
+struct NormBackParams {
+  const void *gy, *s, *weight, *gtotal;
+  void *gx;
+  float *gweight;   // of the weight, or parts [groups, C] of it
+  int64_t gy_ld, s_ld, gtotal_ld, gx_ld, rows;
+  int32_t C, groups;
+  float eps;
+  bool weight_bf16;
+};
+
+// THREADS threads are a group, which takes every groups-th row and adds up its part of the weight's gradient in registers.
+template <typename GY, typename IN, int VEC, int THREADS>
+__global__ __launch_bounds__(norm_block<THREADS>()) void rms_norm_backward_kernel(NormBackParams p) {
+  constexpr int kGroups = norm_block<THREADS>() / THREADS;   // of a workgroup
+  __shared__ float sums[2][2][THREADS / kWave];
+  const int tid = threadIdx.x % THREADS, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int group = (int)blockIdx.x * kGroups + (THREADS < 256 ? wave : 0);
+  if (group >= p.groups) return;   // whole waves; workgroups of one group have none too many
+  const int first_part = THREADS < 256 ? 0 : wave;
+  constexpr int kStep = THREADS / kWave;
+  float w[VEC][8], gw[VEC][8];
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) {
+    load_weight(p.weight, p.weight_bf16, (k * THREADS + tid) * 8, p.C, w[k]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gw[k][i] = 0.0f;
+  }
+  int turn = 0;
+  for (int64_t row = group; row < p.rows; row += p.groups) {
+    float s[VEC][8], g[VEC][8], t[VEC][8], sum[2] = {0.0f, 0.0f};
+    const IN *from_s = (const IN *)p.s + row * p.s_ld;
+    const GY *from_g = (const GY *)p.gy + row * p.gy_ld;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      const bool whole = (first_part + k * kStep) * 512 + 512 <= p.C;
+      load_row(from_s, (k * THREADS + tid) * 8, p.C, whole, s[k]);
+      load_row(from_g, (k * THREADS + tid) * 8, p.C, whole, g[k]);
+    }
+    if (p.gtotal) {
+      const IN *from_t = (const IN *)p.gtotal + row * p.gtotal_ld;
+#pragma unroll
+      for (int k = 0; k < VEC; ++k)
+        load_row(from_t, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C, t[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sum[0] = fmaf(s[k][i], s[k][i], sum[0]);
+        sum[1] = fmaf(g[k][i] * w[k][i], s[k][i], sum[1]);
+      }
+    row_sums<THREADS>(sum, sums, turn);
+    turn ^= 1;
+    const float by = 1.0f / sqrtf(sum[0] / (float)p.C + p.eps), mean = by * by * (sum[1] / (float)p.C);
+    IN *gx = (IN *)p.gx + row * p.gx_ld;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      float out[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        gw[k][i] = fmaf(g[k][i], s[k][i] * by, gw[k][i]);
+        out[i] = by * (g[k][i] * w[k][i] - s[k][i] * mean);
+      }
+      if (p.gtotal) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] += t[k][i];
+      }
+      store_row(gx, (k * THREADS + tid) * 8, p.C, out);
+    }
+  }
+  if (p.gweight) {
+    float *to = p.gweight + (int64_t)group * p.C;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) store_row(to, (k * THREADS + tid) * 8, p.C, gw[k]);
+  }
+}
+
+// The parts of the weight's gradient added up: a workgroup takes 64 columns, a wave every 16th part.
+constexpr int kPartWaves = 16;
+__global__ __launch_bounds__(kPartWaves * kWave) void rms_norm_weight_grad_kernel(const float *__restrict__ parts, int groups, int C,
+                                                                                  float *__restrict__ gweight) {
+  __shared__ float sums[kPartWaves][kWave];
+  const int lane = lane_id(), wave = threadIdx.x / kWave, c = (int)blockIdx.x * kWave + lane;
+  float sum = 0.0f;
+  if (c < C) {
+#pragma unroll 8
+    for (int g = wave; g < groups; g += kPartWaves) sum += parts[(int64_t)g * C + c];
+  }
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && c < C) {
+    float all = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kPartWaves; ++w) all += sums[w][lane];
+    gweight[c] = all;
+  }
+}
+
+// Groups of rows that have a part of the weight's gradient each.
+static int norm_groups(int64_t rows, int32_t C) {
+  const int64_t most = C <= 1024 ? 1024 : 512;
+  return (int)(rows < most ? rows : most);
+}
+
+// Calls launch(vectors, threads) with the threads of a row and the vectors that each has of it.
+template <typename LAUNCH>
+static void norm_shape(int64_t rows, int32_t C, LAUNCH launch) {
+#define HM_NORM_SHAPE(v, t) launch(std::integral_constant<int, v>(), std::integral_constant<int, t>())
+  if (C <= 512) HM_NORM_SHAPE(1, 64);
+  else if (C <= 1024) HM_NORM_SHAPE(2, 64);
+  else if (C <= 2048) HM_NORM_SHAPE(1, 256);
+  else if (C <= 4096) HM_NORM_SHAPE(2, 256);
+  else if (C <= 8192) HM_NORM_SHAPE(2, 512);
+  else if (C <= 16384) HM_NORM_SHAPE(4, 512);
+  else HM_NORM_SHAPE(4, 1024);
+#undef HM_NORM_SHAPE
+}
+
+template <typename IN, typename SUM>
+static void launch_norm(const NormParams &p, hipStream_t stream) {
+  norm_shape(p.rows, p.C, [&](auto vec, auto threads) {
+    constexpr int kRows = norm_block<threads()>() / threads();
+    const int64_t blocks = (p.rows + kRows - 1) / kRows;
+    hipLaunchKernelGGL((rms_norm_kernel<IN, SUM, vec(), threads()>), dim3((unsigned)(blocks < 2048 ? blocks : 2048)),
+                       dim3(norm_block<threads()>()), 0, stream, p);
+  });
+}
+template <typename GY, typename IN>
+static void launch_norm_backward(const NormBackParams &p, hipStream_t stream) {
+  norm_shape(p.rows, p.C, [&](auto vec, auto threads) {
+    constexpr int kGroups = norm_block<threads()>() / threads();
+    hipLaunchKernelGGL((rms_norm_backward_kernel<GY, IN, vec(), threads()>), dim3((unsigned)((p.groups + kGroups - 1) / kGroups)),
+                       dim3(norm_block<threads()>()), 0, stream, p);
+  });
+}
+
+}  // namespace hm
+
+extern "C" hm_status hm_rms_norm(const void *x, hm_dtype dtype, int64_t ld, const void *residual, hm_dtype total_dtype,
+                                 int64_t residual_ld, const void *weight, hm_dtype weight_dtype, float eps, int64_t rows, int32_t C,
+                                 void *total, int64_t total_ld, void *y, hm_dtype y_dtype, uint8_t *q, uint8_t *scale,
+                                 void *hip_stream) {
+  HM_ENTRY_SCOPE;
+  using namespace hm;
+  if (!dtype_known(dtype) || !dtype_known(total_dtype) || !dtype_known(weight_dtype) || !dtype_known(y_dtype)) return HM_ERR_SHAPE;
+  if (rows < 0 || rows > 2147483647LL || C < 1 || C > kMostNormColumns || !(eps >= 0.0f)) return HM_ERR_SHAPE;
+  if (rows > 1 && (ld < C || (residual && (residual_ld < C || total_ld < C)))) return HM_ERR_SHAPE;
+  if (!aligned_as(dtype, x) || !aligned_as(total_dtype, residual) || !aligned_as(total_dtype, total)) return HM_ERR_SHAPE;
+  if (!aligned_as(weight_dtype, weight) || !aligned_as(y_dtype, y) || !buffers8_aligned(q, scale)) return HM_ERR_SHAPE;
+  if (rows == 0) return HM_OK;
+  if (!residual != !total || !q != !scale || (!y && !q)) return HM_ERR_NULL;
+  if (!x || !weight) return HM_ERR_NULL;
+  const NormParams p = {x, residual, weight, total, y, q, scale, ld, residual_ld, total_ld, rows, C, eps, weight_dtype == HM_BF16,
+                        y_dtype == HM_BF16};
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const bool same = !residual || total_dtype == dtype;   // without a residual its type is not looked at
+  if (dtype == HM_BF16) same ? launch_norm<uint16_t, uint16_t>(p, stream) : launch_norm<uint16_t, float>(p, stream);
+  else same ? launch_norm<float, float>(p, stream) : launch_norm<float, uint16_t>(p, stream);
+  return hm_launch_status();
+}
+
+extern "C" size_t hm_rms_norm_backward_workspace_bytes(int64_t rows, int32_t C) {
+  if (rows < 0 || C < 1 || C > hm::kMostNormColumns) return 0;
+  const int groups = hm::norm_groups(rows, C);
+  return groups > 1 ? (size_t)groups * C * 4 : 0;
+}
+
+extern "C" hm_status hm_rms_norm_backward(const void *gy, hm_dtype gy_dtype, int64_t gy_ld, const void *s, hm_dtype dtype,
+                                          int64_t s_ld, const void *weight, hm_dtype weight_dtype, float eps, int64_t rows,
+                                          int32_t C, const void *gtotal, int64_t gtotal_ld, void *gx, int64_t gx_ld,
+                                          float *gweight, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  HM_ENTRY_SCOPE;
+  using namespace hm;
+  if (!dtype_known(gy_dtype) || !dtype_known(dtype) || !dtype_known(weight_dtype)) return HM_ERR_SHAPE;
+  if (rows < 0 || rows > 2147483647LL || C < 1 || C > kMostNormColumns || !(eps >= 0.0f)) return HM_ERR_SHAPE;
+  if (rows > 1 && (gy_ld < C || s_ld < C || gx_ld < C || (gtotal && gtotal_ld < C))) return HM_ERR_SHAPE;
+  if (!aligned_as(gy_dtype, gy) || !aligned_as(dtype, s) || !aligned_as(weight_dtype, weight)) return HM_ERR_SHAPE;
+  if (!aligned_as(dtype, gtotal) || !aligned_as(dtype, gx) || ((uintptr_t)gweight & 3)) return HM_ERR_SHAPE;
+  if (!gweight) return HM_ERR_NULL;
+  NormBackParams p = {gy, s, weight, gtotal, gx, gweight, gy_ld, s_ld, gtotal_ld, gx_ld, rows, C, norm_groups(rows, C), eps,
+                      weight_dtype == HM_BF16};
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const bool parts = p.groups != 1;   // no rows: the sum of no parts
+  if (rows > 0) {
+    if (!gy || !s || !weight || !gx) return HM_ERR_NULL;
+    if (parts) {
+      if (!workspace || workspace_bytes < hm_rms_norm_backward_workspace_bytes(rows, C) || ((uintptr_t)workspace & 15))
+        return HM_ERR_WORKSPACE;
+      p.gweight = (float *)workspace;
+    }
+    if (gy_dtype == HM_BF16) dtype == HM_BF16 ? launch_norm_backward<uint16_t, uint16_t>(p, stream)
+                                              : launch_norm_backward<uint16_t, float>(p, stream);
+    else dtype == HM_BF16 ? launch_norm_backward<float, uint16_t>(p, stream) : launch_norm_backward<float, float>(p, stream);
+    const hm_status launched = hm_launch_status();
+    if (launched != HM_OK || !parts) return launched;
+  }
+  hipLaunchKernelGGL(rms_norm_weight_grad_kernel, dim3((unsigned)((C + kWave - 1) / kWave)), dim3(kPartWaves * kWave), 0, stream,
+                     (const float *)workspace, p.groups, C, gweight);
+  return hm_launch_status();
+}

@@ -5,14 +5,6 @@ namespace hm {
 
 constexpr int kQuantThreads = 256;
 
-// Largest value of the sixteen lanes of a row, in all of them.
-__device__ __forceinline__ uint32_t max16(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, true));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xF, 0xF, true));
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xF, 0xF, true));
-}
-
 struct RowParams {
   const void *x;
   int64_t ld, pieces;   // pieces of 512 columns of all rows
@@ -34,17 +26,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(RowParams 
   const IN *row = (const IN *)p.x + r * p.ld;
   if (part * 512 + 512 <= p.C) load_floats<8>(row + c, v);   // the whole wave
   else load_row_end<8>(row, c, p.C, v);
-  const uint32_t most = max16(largest_bits(v));
-  const int code = scale_code8(most);
-  const float by = inverse_scale8(code);
-  if (c < width) {
-    const uint64_t out = (uint64_t)pack8(v[4], v[5], v[6], v[7], by) << 32 | pack8(v[0], v[1], v[2], v[3], by);
-    *(uint64_t *)(p.q + r * width + c) = out;
-  }
-  const uint32_t mine = c < width ? (uint32_t)code : 0u;   // behind the last block zeros
-  const uint32_t codes = (uint32_t)read_lane((int)mine, 0) | (uint32_t)read_lane((int)mine, 16) << 8 |
-                         (uint32_t)read_lane((int)mine, 32) << 16 | (uint32_t)read_lane((int)mine, 48) << 24;
-  if (lane == 0) *(uint32_t *)(p.scale + r * scale8_bytes(p.C) + part * 4) = codes;
+  store_piece8(p.q + r * width, p.scale + r * scale8_bytes(p.C), part, (int)width, v);
 }
 
 struct ColumnParams {
@@ -54,27 +36,6 @@ struct ColumnParams {
   int32_t segments, rows, C, blocks, tiles;   // blocks of rows; tiles of columns
   uint8_t *q, *scale;
 };
-
-// The segment that owns block b, the last whose first block is not behind it, and its rows; called by whole waves.
-// Both offsets of a lane's segment are loaded together: what follows waits for one trip to memory.
-struct BlockOwner8 {
-  int segment;   // -1: none
-  Segment8 rows;
-};
-__device__ __forceinline__ BlockOwner8 owner_of_block8(const int32_t *__restrict__ offsets, int segments, int rows,
-                                                       int b) {
-  const int lane = lane_id();
-  BlockOwner8 owner = {-1, {0, 0}};
-  for (int e0 = 0; e0 < segments; e0 += kWave) {
-    const int e = e0 + lane;
-    const Segment8 s = segment8(offsets, min(e, segments - 1), rows);
-    const uint64_t upto = __ballot(e < segments && first_block8(s.from, e) <= b);
-    if (upto == 0) break;
-    const int l = 63 - __builtin_clzll(upto);
-    owner = {e0 + l, {read_lane(s.from, l), read_lane(s.to, l)}};
-  }
-  return owner;
-}
 
 // A workgroup takes a block of 128 rows and 64 columns: a thread eight rows of four columns, whose bytes it turns in
 // registers; LDS puts a column's 128 bytes together.  6,001 rows of 2,056 bf16 in 16 segments 11 us, 3.3 TB/s: one

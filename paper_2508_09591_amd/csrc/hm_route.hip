@@ -1,6 +1,4 @@
 // The router in front of the dispatch: logits -> expert ids and weights, and the way back.
-#include <type_traits>
-
 #include "hm_block8.h"
 
 namespace hm {
@@ -32,22 +30,6 @@ __device__ __forceinline__ float reciprocal(float y) {   // of y >= 1
   return y < 8.50705917e37f ? better : 0.0f;
 }
 __device__ __forceinline__ float logistic(float x) { return reciprocal(1.0f + expf(-x)); }
-
-// Over all lanes, the result in each: within rows of sixteen by rotations, then the four rows.
-template <typename OP>
-__device__ __forceinline__ float wave_all(float v, OP op) {
-  auto turned = [](float x, auto control) {
-    const int from = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), control(), 0xF, 0xF, true);
-    return __builtin_bit_cast(float, from);
-  };
-  v = op(v, turned(v, std::integral_constant<int, 0x128>()));
-  v = op(v, turned(v, std::integral_constant<int, 0x124>()));
-  v = op(v, turned(v, std::integral_constant<int, 0x122>()));
-  v = op(v, turned(v, std::integral_constant<int, 0x121>()));
-  return op(op(read_lane(v, 0), read_lane(v, 16)), op(read_lane(v, 32), read_lane(v, 48)));
-}
-__device__ __forceinline__ float wave_max(float v) { return wave_all(v, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ float wave_sum(float v) { return wave_all(v, [](float a, float b) { return a + b; }); }
 
 // The largest of the wave's values and the lowest index that has it.
 __device__ __forceinline__ void wave_first(float &v, int &i) {
