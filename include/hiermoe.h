@@ -621,11 +621,11 @@ hm_status hm_gated_backward(const void *h, const void *ga, hm_dtype dtype, int64
  * as in hm_route, which is part of the call.  out [T,H] of out_dtype; a token without an expert here gets zeros.  Nothing is
  * rounded to 8 bits on the way: sums are fp32 and activations keep 16 bits (24 for fp32 results).  A token's output depends
  * on its own row, logits and experts alone.  With an exchange in between, the sum over the ranks is the layer's output.
- * workspace: hm_layer_few_workspace_bytes(T, K, F) bytes of device scratch, 16-byte aligned, not shared by calls that may
+ * workspace: hm_layer_few_workspace_bytes(T, K, H, F) bytes of device scratch, 16-byte aligned, not shared by calls that may
  * run at once.  Limits: T <= 64, T * K <= 1024, experts <= 1024, H <= 2^20, F <= 2^19,
  * min(experts, T * K) * ceil(F / 128) <= 2^20; beyond HM_ERR_SHAPE.
  */
-size_t hm_layer_few_workspace_bytes(int32_t T, int32_t K, int32_t F);
+size_t hm_layer_few_workspace_bytes(int32_t T, int32_t K, int32_t H, int32_t F);
 hm_status hm_layer_few(const void *x, int64_t ld, const void *logits, hm_dtype logits_dtype, int64_t logits_ld,
                        const float *bias, int32_t T, const hm_router *router /* host */, const uint8_t *w13,
                        const uint8_t *w13_scale, const uint8_t *w2, const uint8_t *w2_scale, int32_t first,

@@ -199,7 +199,7 @@ def lib():
         L.hm_rms_norm_backward_workspace_bytes.restype = ctypes.c_size_t
         L.hm_rms_norm_backward_workspace_bytes.argtypes = [i64, i32]
         L.hm_layer_few_workspace_bytes.restype = ctypes.c_size_t
-        L.hm_layer_few_workspace_bytes.argtypes = [i32, i32, i32]
+        L.hm_layer_few_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.hm_status_string.restype = ctypes.c_char_p
         L.hm_status_string.argtypes = [ctypes.c_int]
         _native.bind(*[ctypes.cast(getattr(L, name), vp).value for name in _NATIVE])
@@ -893,7 +893,7 @@ def alloc_rms_norm_workspace(rows: int, C: int, device="cuda") -> torch.Tensor:
 
 def alloc_layer_few_workspace(T: int, router: Router, H: int, F: int, device="cuda") -> torch.Tensor:
     """Scratch for hm_layer_few of up to T tokens."""
-    return torch.empty(int(lib().hm_layer_few_workspace_bytes(T, router.K, F)), dtype=torch.uint8, device=device)
+    return torch.empty(int(lib().hm_layer_few_workspace_bytes(T, router.K, H, F)), dtype=torch.uint8, device=device)
 
 
 def hm_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, y: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,

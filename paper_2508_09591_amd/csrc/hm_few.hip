@@ -19,54 +19,50 @@ struct FewParams {
   const int32_t *ids;      // [T,K]
   const float *weights;
   int32_t T, K, first, experts, H, F;
+  uint32_t per_K;          // ceil(2^20 / K)
   const uint8_t *w13, *s13, *w2, *s2;
   uint16_t *a;             // [planes, T K, up(F,128)]
+  float *y;                // [T K, H]
   void *out;
 };
 
-// The experts that are here and that a slot has chosen, as bits in LDS; called by all threads, before a barrier of theirs is
-// left.
-constexpr int kHitWords = kMostSegments8 / 32;
-__device__ __forceinline__ int local_expert(const FewParams &p, int slot) {   // -1: not here
-  const int e = slot < p.T * p.K ? p.ids[slot] - p.first : -1;
+// A workgroup's expert and the slots that chose it.  There are as many workgroups' shares as experts here, or, if those are fewer,
+// as slots: a slot's are taken where no slot before it has chosen the same expert.
+__device__ __forceinline__ int expert_here(const FewParams &p, int slot) {   // -1: none or elsewhere
+  const int e = p.ids[slot] - p.first;
   return (unsigned)e < (unsigned)p.experts ? e : -1;
 }
-__device__ __forceinline__ void find_hits(const FewParams &p, uint32_t *hits, int16_t *expert_of) {
-  for (int i = threadIdx.x; i < kHitWords; i += blockDim.x) hits[i] = 0;
-  __syncthreads();
-  for (int s = threadIdx.x; s < p.T * p.K; s += blockDim.x) {
-    const int e = local_expert(p, s);
-    expert_of[s] = (int16_t)e;
-    if (e >= 0) atomicOr(&hits[e >> 5], 1u << (e & 31));
-  }
-  __syncthreads();
-}
-// The n-th of them in ascending order, -1 if there are fewer; and how many there are.  By whole waves.
-__device__ __forceinline__ int nth_hit(const uint32_t *hits, int n, int &count) {
-  const int lane = lane_id();
-  const uint32_t mine = lane < kHitWords ? hits[lane] : 0u;
-  const int upto = lane_scan(__popc(mine));
-  count = read_lane(upto, kWave - 1);
-  if (n >= count) return -1;
-  const int word = __builtin_ctzll(__ballot(upto > n));
-  uint32_t bits = (uint32_t)read_lane((int)mine, word);
-  for (int skip = n - (read_lane(upto, word) - __popc(bits)); skip > 0; --skip) bits &= bits - 1;
-  return word * 32 + __builtin_ctz(bits);
-}
-// The slots of an expert, ascending, into `list`; at most one of a token's, so at most kMostFewTokens.  By one wave.
-__device__ __forceinline__ int slots_of(const int16_t *expert_of, int slots, int e, int *list) {
-  const int lane = lane_id();
+// Writes the slots, ascending, to `list`, one of the wave's own: at most one of a token's.  0: nothing to do.  By whole waves.
+__device__ __forceinline__ int slots_of_share(const FewParams &p, int share, int &e, int *list) {
+  const int lane = lane_id(), slots = p.T * p.K;
+  const bool by_slot = slots < p.experts;
+  e = by_slot ? expert_here(p, share) : share;
   int n = 0;
-  for (int s0 = 0; s0 < slots; s0 += kWave) {
-    const bool mine = s0 + lane < slots && expert_of[s0 + lane] == e;
-    const uint64_t all = __ballot(mine);
-    const int at = n + __popcll(all & ((1ull << lane) - 1));
-    if (mine && at < kMostFewTokens) list[at] = s0 + lane;
+  auto take = [&](int s, int expert) {
+    const uint64_t all = __ballot(s < slots && expert == e);
+    const int at = n + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));   // before this lane
+    if (s < slots && expert == e && at < kMostFewTokens) list[at] = s;
     n += __popcll(all);
+  };
+  if (slots <= kWave) {
+    take(lane, expert_here(p, min(lane, slots - 1)));
+  } else {
+    constexpr int kTogether = 4;   // loads on their way
+    for (int s0 = 0; s0 < slots; s0 += kTogether * kWave) {
+      int expert[kTogether];
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i) expert[i] = expert_here(p, min(s0 + i * kWave + lane, slots - 1));
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i) take(s0 + i * kWave + lane, expert[i]);
+    }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (e < 0 || n == 0 || (by_slot && __builtin_amdgcn_readfirstlane(list[0]) != share)) return 0;
   return min(n, kMostFewTokens);
 }
+
+// slot / K: slots are below 2^10, so that what per_K is too large by does not reach the next multiple.
+__device__ __forceinline__ int token_of(const FewParams &p, int slot) { return (int)((uint32_t)slot * p.per_K >> 20); }
 
 // 32 bytes of a weight's row, 32 bf16 numbers.
 __device__ __forceinline__ i32x8 load32(const uint8_t *p) {
@@ -83,6 +79,27 @@ __device__ __forceinline__ Wide load_wide(const uint16_t *p) {   // at any align
   for (int i = 0; i < 4; ++i) w.v[i] = __builtin_bit_cast(bf16x8, (u32x4)*(const u32x4_align2 *)(p + 8 * i));
   return w;
 }
+// The same of a row of H from column c on, zeros behind its end: vectors that would pass it are loaded from before it and moved down.
+__device__ __forceinline__ Wide load_wide_end(const uint16_t *row, int c, int H) {
+  Wide w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i, c += 8) {
+    u32x4 v = {0, 0, 0, 0};
+    if (H < 8) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j / 2] |= c + j < H ? (uint32_t)row[c + j] << 16 * (j & 1) : 0u;
+    } else {
+      const int at = min(c, H - 8), by = c - at;
+      v = *(const u32x4_align2 *)(row + at);
+      v = by & 4 ? u32x4{v[2], v[3], 0, 0} : v;
+      v = by & 2 ? u32x4{v[1], v[2], v[3], 0} : v;
+      v = by & 1 ? u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16} : v;
+      v = by < 8 ? v : u32x4{0, 0, 0, 0};
+    }
+    w.v[i] = __builtin_bit_cast(bf16x8, v);
+  }
+  return w;
+}
 __device__ __forceinline__ Wide zero_wide() {
   Wide w;
 #pragma unroll
@@ -92,103 +109,99 @@ __device__ __forceinline__ Wide zero_wide() {
 
 // ---- the first product and the activation --------------------------------------------------------------
 // A workgroup takes an expert and 16 columns of its activation: as many rows of the gate's weights and of the up's.  Its four
-// waves take every fourth step of 128 columns of x and add up in LDS.  A lane has row l % 16 of the weights and of the slots,
-// bytes 32 (l / 16) to 32 (l / 16) + 31 of a step.
+// waves share the steps of 128 columns of x and add up in LDS.  A lane has row l % 16 of the weights and of the slots, bytes
+// 32 (l / 16) to 32 (l / 16) + 31 of a step.
 constexpr int kUpWaves = 4;
+
 template <int GROUPS, int PLANES>
 __global__ __launch_bounds__(kUpWaves * kWave) void few_up_kernel(FewParams p) {
-  __shared__ uint32_t hits[kHitWords];
-  __shared__ int16_t expert_of[kMostFewSlots];
   __shared__ int lists[kUpWaves][kMostFewTokens];
   __shared__ f32x4 sums[kUpWaves][2][kWave];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-  const int width_a = (int)row8_bytes(p.F), strips = width_a / 16, slots = p.T * p.K;
-  find_hits(p, hits, expert_of);
-  int count;
-  const int e = nth_hit(hits, (int)(blockIdx.x / (uint32_t)strips), count);
-  if (e < 0) return;
-  const int n = slots_of(expert_of, slots, e, lists[wave]);
+  const int width_a = (int)row8_bytes(p.F), slots = p.T * p.K;
   const int *list = lists[wave];
-  const int f0 = (int)(blockIdx.x % (uint32_t)strips) * 16, row = lane & 15, part = (lane >> 4) * 32;
-  const int steps = (int)blocks8(p.H);
+  const int share = (int)blockIdx.y, f0 = (int)blockIdx.x * 16;
+  int e;
+  const int all = slots_of_share(p, share, e, lists[wave]);
+  if (all == 0) return;   // the same for the workgroup
+  const int row = lane & 15, part = (lane >> 4) * 32, steps = (int)blocks8(p.H);
   const int64_t pitch = row8_bytes(p.H), scale_pitch = scale8_bytes(p.H);
-  const int gate = min(f0 + row, p.F - 1), up = p.F + gate;
   const uint8_t *w = p.w13 + (int64_t)e * 2 * p.F * pitch + part, *s = p.s13 + (int64_t)e * blocks8(2 * (int64_t)p.F) * scale_pitch;
-  const uint8_t *from_gate = w + gate * pitch, *from_up = w + up * pitch;
-  const uint8_t *scale_gate = s + (gate / 128) * scale_pitch, *scale_up = s + (up / 128) * scale_pitch;
-  const uint16_t *x[GROUPS];
-  bool there[GROUPS];
+  const uint8_t *from[2], *scale[2];   // of gate and up
 #pragma unroll
-  for (int g = 0; g < GROUPS; ++g) {
-    there[g] = g * 16 + row < n;
-    x[g] = p.x + (int64_t)(list[min(g * 16 + row, n - 1)] / p.K) * p.ld + part;
+  for (int h = 0; h < 2; ++h) {
+    const int n = min(f0 + row, p.F - 1) + h * p.F;
+    from[h] = w + n * pitch;
+    scale[h] = s + (n / 128) * scale_pitch;
   }
-  f32x4 acc[GROUPS][2];
+  for (int first = 0; first < all; first += 16 * GROUPS) {   // more slots than that read the weights again
+    const int n = all - first;
+    const uint16_t *x[GROUPS];
 #pragma unroll
-  for (int g = 0; g < GROUPS; ++g) acc[g][0] = acc[g][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  struct Step {
-    i32x8 gate, up;
-    uint32_t scale_gate, scale_up;
-    Wide x[GROUPS];
-  };
-  auto load = [&](Step &t, int k) {
-    t.gate = load32(from_gate + (int64_t)k * 128);
-    t.up = load32(from_up + (int64_t)k * 128);
-    t.scale_gate = scale_gate[k];
-    t.scale_up = scale_up[k];
+    for (int g = 0; g < GROUPS; ++g) x[g] = p.x + (int64_t)token_of(p, list[first + min(g * 16 + row, n - 1)]) * p.ld;
+    f32x4 acc[GROUPS][2];
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      t.x[g] = zero_wide();
-      if (g * 16 >= n) continue;
-      if (k * 128 + 128 <= p.H) {
-        if (there[g]) t.x[g] = load_wide(x[g] + k * 128);
-      } else if (there[g]) {   // the row's end: zeros behind it
+    for (int g = 0; g < GROUPS; ++g) acc[g][0] = acc[g][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Step {
+      i32x8 w[2];
+      uint32_t scale[2];
+      Wide x[GROUPS];
+    };
+    auto load = [&](Step &t, int k) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          t.x[g].v[i / 8][i % 8] = k * 128 + part + i < p.H ? __builtin_bit_cast(__bf16, x[g][k * 128 + i]) : (__bf16)0.0f;
+      for (int h = 0; h < 2; ++h) {
+        t.w[h] = load32(from[h] + (int64_t)k * 128);
+        t.scale[h] = scale[h][k];
       }
-    }
-  };
-  auto multiply = [&](const Step &t) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bf16x8 wg = widen8(t.gate[2 * i], t.gate[2 * i + 1], t.scale_gate), wu = widen8(t.up[2 * i], t.up[2 * i + 1], t.scale_up);
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g) {
+        t.x[g] = zero_wide();
         if (g * 16 >= n) continue;
-        acc[g][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wg, t.x[g].v[i], acc[g][0], 0, 0, 0);
-        acc[g][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wu, t.x[g].v[i], acc[g][1], 0, 0, 0);
+        if (g * 16 + row >= n) continue;
+        if (k * 128 + 128 <= p.H) t.x[g] = load_wide(x[g] + k * 128 + part);
+        else t.x[g] = load_wide_end(x[g], k * 128 + part, p.H);
+      }
+    };
+    auto multiply = [&](const Step &t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8 u = widen8(t.w[h][2 * i], t.w[h][2 * i + 1], t.scale[h]);
+#pragma unroll
+          for (int g = 0; g < GROUPS; ++g)
+            if (g * 16 < n) acc[g][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, t.x[g].v[i], acc[g][h], 0, 0, 0);
+        }
+    };
+    Step a, b;   // one on its way while the other is multiplied
+    int k = wave;
+    if (k < steps) load(a, k);
+    for (; k < steps; k += 2 * kUpWaves) {
+      if (k + kUpWaves < steps) load(b, k + kUpWaves);
+      multiply(a);
+      if (k + kUpWaves < steps) {
+        if (k + 2 * kUpWaves < steps) load(a, k + 2 * kUpWaves);
+        multiply(b);
       }
     }
-  };
-  Step a, b;   // one on its way while the other is multiplied
-  int k = wave;
-  if (k < steps) load(a, k);
-  for (; k < steps; k += 2 * kUpWaves) {
-    if (k + kUpWaves < steps) load(b, k + kUpWaves);
-    multiply(a);
-    if (k + kUpWaves < steps) {
-      if (k + 2 * kUpWaves < steps) load(a, k + 2 * kUpWaves);
-      multiply(b);
-    }
-  }
-  // thread: slot / 16, column % 16 of a group; lane l had slot l % 16 and columns 4 (l / 16) to 4 (l / 16) + 3
-  const int r = threadIdx.x >> 4, c = threadIdx.x & 15, f = f0 + c;
+    // thread: slot / 16, column % 16 of a group; lane l had slot l % 16 and columns 4 (l / 16) to 4 (l / 16) + 3
+    const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
 #pragma unroll
-  for (int g = 0; g < GROUPS; ++g) {
-    if (g * 16 >= n) break;   // the same for the workgroup
-    if (g > 0) __syncthreads();
-    sums[wave][0][lane] = acc[g][0];
-    sums[wave][1][lane] = acc[g][1];
-    __syncthreads();
-    float v[2] = {0.0f, 0.0f};
+    for (int g = 0; g < GROUPS; ++g) {
+      if (g * 16 >= n) break;   // the same for the workgroup
+      if (first + g > 0) __syncthreads();
+      sums[wave][0][lane] = acc[g][0];
+      sums[wave][1][lane] = acc[g][1];
+      __syncthreads();
+      if (g * 16 + r >= n) continue;
+      float v[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int u = 0; u < kUpWaves; ++u)
+      for (int u = 0; u < kUpWaves; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) v[h] += ((const float *)&sums[u][h][(c >> 2) * 16 + r])[c & 3];
-    if (g * 16 + r < n) {
-      float rest = f < p.F ? v[0] / (1.0f + expf(-v[0])) * v[1] : 0.0f;   // zeros up to a whole block
-      const int64_t at = (int64_t)list[g * 16 + r] * width_a + f;
+        for (int h = 0; h < 2; ++h) v[h] += ((const float *)&sums[u][h][(c >> 2) * 16 + r])[c & 3];
+      const int column = f0 + c;
+      float rest = column < p.F ? v[0] / (1.0f + expf(-v[0])) * v[1] : 0.0f;   // zeros up to a whole block
+      const int64_t at = (int64_t)list[first + g * 16 + r] * width_a + column;
 #pragma unroll
       for (int plane = 0; plane < PLANES; ++plane) {
         const uint32_t bits = round_bf16x2(rest, rest);
@@ -201,127 +214,248 @@ __global__ __launch_bounds__(kUpWaves * kWave) void few_up_kernel(FewParams p) {
 }
 
 // ---- the second product and the sum over a token's experts ---------------------------------------------
-// A workgroup takes 16 columns of the output.  Its waves share the steps of all experts hit evenly; behind an expert's steps a
-// wave adds what its slots get, times their weights, to its own sums of the tokens in LDS, which are added up in the end.
-template <int GROUPS, int PLANES, typename OUT>
-__global__ __launch_bounds__(512) void few_down_kernel(FewParams p, int columns) {
-  extern __shared__ float sums[];   // [waves][T][16]
-  __shared__ uint32_t hits[kHitWords];
-  __shared__ int16_t expert_of[kMostFewSlots];
-  __shared__ int lists[8][kMostFewTokens];
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), waves = blockDim.x / kWave;
+// Few slots: a workgroup takes up to 16 columns of the output, all activations stand in its LDS, and its waves share the weights'
+// rows of all experts hit evenly, in pieces of four steps; behind an expert's pieces a wave adds what its slots get, times their
+// weights, to its own sums of the tokens, which are added up in the end.
+constexpr int kDownWaves = 8, kPieceSteps = 4;
+template <int PLANES, typename OUT>
+__global__ __launch_bounds__(kDownWaves * kWave, PLANES == 2 ? 4 : 2) void few_down_kernel(FewParams p, int columns) {
+  extern __shared__ __attribute__((aligned(16))) float sums[];   // [waves][T][16], and the activations behind them
+  __shared__ int lists[kDownWaves][kWave];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int width_a = (int)row8_bytes(p.F), slots = p.T * p.K, row = lane & 15, part = (lane >> 4) * 32, h0 = (int)blockIdx.x * columns;
-  for (int i = threadIdx.x; i < waves * p.T * 16; i += blockDim.x) sums[i] = 0.0f;
-  find_hits(p, hits, expert_of);
-  int count;
-  nth_hit(hits, 0, count);
-  const int steps = (int)blocks8(p.F), h = min(h0 + min(row, columns - 1), p.H - 1);
-  const int64_t pitch = row8_bytes(p.F), scale_pitch = scale8_bytes(p.F), all = (int64_t)count * steps;
-  int64_t at = all * wave / waves;
-  const int64_t end = all * (wave + 1) / waves;
+  const int mine_is = lane < slots ? expert_here(p, lane) : -1;   // at most 64 slots
+  const int pitch_a = width_a + 8;   // of a row in LDS: rows read together lie in different banks
+  uint16_t *staged = (uint16_t *)(sums + kDownWaves * p.T * 16);
+  uint64_t hit = 0;   // slots that are their expert's first
+  for (int s = 0; s < slots; ++s) {
+    const int e = read_lane(mine_is, s);
+    hit |= (uint64_t)(e >= 0 && __builtin_ctzll(__ballot(mine_is == e)) == s) << s;
+  }
+  const int steps = (int)blocks8(p.F), pieces = (steps + kPieceSteps - 1) / kPieceSteps, h = min(h0 + min(row, columns - 1), p.H - 1);
+  const int64_t pitch = row8_bytes(p.F), scale_pitch = scale8_bytes(p.F);
+  const int all = __popcll(hit) * pieces, end = (int)((int64_t)all * (wave + 1) / kDownWaves);
+  int at = (int)((int64_t)all * wave / kDownWaves);
+  for (int skip = at / pieces; skip > 0; --skip) hit &= hit - 1;
+  struct Piece {
+    i32x8 w[kPieceSteps];
+    uint32_t scales;
+  };
+  auto load = [&](Piece &t, int e, int piece) {   // steps behind the last are the last: their products are left out
+    const uint8_t *w = p.w2 + ((int64_t)e * p.H + h) * pitch + part;
+#pragma unroll
+    for (int s = 0; s < kPieceSteps; ++s) {
+      t.w[s] = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (row < columns) t.w[s] = load32(w + (int64_t)min(piece * kPieceSteps + s, steps - 1) * 128);
+    }
+    t.scales = *(const uint32_t *)(p.s2 + ((int64_t)e * blocks8(p.H) + h / 128) * scale_pitch + piece * kPieceSteps);
+  };
+  Piece x, y;   // one on its way while the other is multiplied
+  if (at < end) load(x, read_lane(mine_is, __builtin_ctzll(hit)), at % pieces);
+  const int vectors = width_a / 8;
+  for (int i = threadIdx.x; i < PLANES * slots * vectors; i += kDownWaves * kWave) {   // those of slots elsewhere nobody reads
+    const int r = i / vectors, c = i - r * vectors;
+    *(u32x4 *)(staged + r * pitch_a + c * 8) = *(const u32x4 *)(p.a + (int64_t)i * 8);
+  }
+  for (int i = threadIdx.x; i < kDownWaves * p.T * 16; i += kDownWaves * kWave) sums[i] = 0.0f;
+  __syncthreads();
   int *list = lists[wave];
   float *mine = sums + wave * p.T * 16;
-  struct Step {
-    i32x8 w;
-    uint32_t scale;
-    Wide a[GROUPS][PLANES];
-  };
   while (at < end) {
-    const int j = (int)(at / steps), from = (int)(at - (int64_t)j * steps), to = (int)min((int64_t)steps, from + end - at);
-    int unused;
-    const int e = nth_hit(hits, j, unused);
-    const int n = slots_of(expert_of, slots, e, list);
-    const uint8_t *w = p.w2 + ((int64_t)e * p.H + h) * pitch + part;
-    const uint8_t *scale = p.s2 + ((int64_t)e * blocks8(p.H) + h / 128) * scale_pitch;
-    int slot[GROUPS];
-    f32x4 acc[GROUPS];
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      slot[g] = g * 16 + row < n ? list[g * 16 + row] : -1;
-      acc[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    auto load = [&](Step &t, int k) {
-      t.w = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
-      if (row < columns) t.w = load32(w + (int64_t)k * 128);
-      t.scale = scale[k];
-#pragma unroll
-      for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-        for (int plane = 0; plane < PLANES; ++plane) {
-          t.a[g][plane] = zero_wide();
-          if (slot[g] >= 0) t.a[g][plane] = load_wide(p.a + ((int64_t)plane * slots + slot[g]) * width_a + k * 128 + part);
-        }
-    };
-    auto multiply = [&](const Step &t) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bf16x8 v = widen8(t.w[2 * i], t.w[2 * i + 1], t.scale);
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-          if (g * 16 >= n) continue;
-#pragma unroll
-          for (int plane = 0; plane < PLANES; ++plane)
-            acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, t.a[g][plane].v[i], acc[g], 0, 0, 0);
-        }
-      }
-    };
-    Step a, b;
-    int k = from;
-    load(a, k);
-    for (; k < to; k += 2) {
-      if (k + 1 < to) load(b, k + 1);
-      multiply(a);
-      if (k + 1 < to) {
-        if (k + 2 < to) load(a, k + 2);
-        multiply(b);
-      }
-    }
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g)
-      if (slot[g] >= 0) {   // lane: slot l % 16, columns 4 (l / 16) to 4 (l / 16) + 3; a token has one slot of an expert
-        const float by = p.weights[slot[g]];
-        float *to_token = mine + (slot[g] / p.K) * 16 + (lane >> 4) * 4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to_token[i] = fmaf(by, acc[g][i], to_token[i]);
-      }
+    const int from = at % pieces, to = min(pieces, from + end - at);
+    const int e = read_lane(mine_is, __builtin_ctzll(hit));
+    const uint64_t chosen = __ballot(mine_is == e);
+    const int n = __popcll(chosen);
+    if (chosen >> lane & 1) list[__popcll(chosen & ((1ull << lane) - 1))] = lane;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     at += to - from;
+    hit &= hit - 1;
+    for (int first = 0; first < n; first += 16) {   // more than 16 slots of an expert: its weights again
+      if (first > 0) load(x, e, from);
+      const int slot = first + row < n ? list[first + row] : -1;
+      const float by = slot >= 0 ? p.weights[slot] : 0.0f;
+      const uint16_t *a = staged + max(slot, 0) * pitch_a + part;
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      auto multiply = [&](const Piece &t, int piece) {
+#pragma unroll
+        for (int s = 0; s < kPieceSteps; ++s) {
+          const int step = piece * kPieceSteps + s;
+          if (step >= steps) break;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bf16x8 u = widen8(t.w[s][2 * i], t.w[s][2 * i + 1], t.scales >> 8 * s);
+#pragma unroll
+            for (int plane = 0; plane < PLANES; ++plane) {
+              const bf16x8 v = *(const bf16x8 *)(a + plane * slots * pitch_a + step * 128 + i * 8);
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, v, acc, 0, 0, 0);
+            }
+          }
+        }
+      };
+      for (int piece = from; piece < to; piece += 2) {
+        if (piece + 1 < to) load(y, e, piece + 1);
+        multiply(x, piece);
+        if (piece + 1 < to) {
+          if (piece + 2 < to) load(x, e, piece + 2);
+          multiply(y, piece + 1);
+        }
+      }
+      if (first + 16 >= n && at < end) load(x, read_lane(mine_is, __builtin_ctzll(hit)), 0);   // the next expert's
+      if (slot >= 0) {   // lane: slot l % 16, columns 4 (l / 16) to 4 (l / 16) + 3; a token has one slot of an expert
+        float *to_token = mine + token_of(p, slot) * 16 + (lane >> 4) * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to_token[i] = fmaf(by, acc[i], to_token[i]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < p.T * 16; i += blockDim.x) {
+  for (int i = threadIdx.x; i < p.T * 16; i += kDownWaves * kWave) {
     const int t = i >> 4, c = i & 15;
     if (c >= columns || h0 + c >= p.H) continue;
     float sum = 0.0f;
-    for (int u = 0; u < waves; ++u) sum += sums[(u * p.T + t) * 16 + c];
+#pragma unroll
+    for (int u = 0; u < kDownWaves; ++u) sum += sums[(u * p.T + t) * 16 + c];
     store_float((OUT *)p.out + (int64_t)t * p.H + h0 + c, sum);
   }
 }
 
+// The same by experts: a workgroup takes one and FRAGS times 16 columns of the output, and leaves what its slots get; its four waves
+// take every fourth step.
+template <int PLANES, int FRAGS>
+__global__ __launch_bounds__(kUpWaves * kWave) void few_down_slots_kernel(FewParams p) {
+  __shared__ int lists[kUpWaves][kMostFewTokens];
+  __shared__ f32x4 sums[kUpWaves][FRAGS][kWave];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int slots = p.T * p.K, width_a = (int)row8_bytes(p.F);
+  const int *list = lists[wave];
+  const int share = (int)blockIdx.y, h0 = (int)blockIdx.x * 16 * FRAGS;
+  int e;
+  const int n = slots_of_share(p, share, e, lists[wave]);
+  if (n == 0) return;   // the same for the workgroup
+  const int row = lane & 15, part = (lane >> 4) * 32, steps = (int)blocks8(p.F);
+  const int64_t pitch = row8_bytes(p.F), scale_pitch = scale8_bytes(p.F);
+  const uint8_t *w[FRAGS], *scale[FRAGS];
+#pragma unroll
+  for (int f = 0; f < FRAGS; ++f) {
+    const int h = min(h0 + f * 16 + row, p.H - 1);
+    w[f] = p.w2 + ((int64_t)e * p.H + h) * pitch + part;
+    scale[f] = p.s2 + ((int64_t)e * blocks8(p.H) + h / 128) * scale_pitch;
+  }
+  for (int first = 0; first < n; first += 16) {
+    const int slot = first + row < n ? list[first + row] : -1;
+    const uint16_t *a = p.a + (int64_t)max(slot, 0) * width_a + part;
+    struct Step {
+      i32x8 w[FRAGS];
+      uint32_t scale[FRAGS];
+      Wide a[PLANES];
+    };
+    f32x4 acc[FRAGS];
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) acc[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto load = [&](Step &t, int k) {
+#pragma unroll
+      for (int f = 0; f < FRAGS; ++f) {
+        t.w[f] = load32(w[f] + (int64_t)k * 128);
+        t.scale[f] = scale[f][k];
+      }
+#pragma unroll
+      for (int plane = 0; plane < PLANES; ++plane) {
+        t.a[plane] = zero_wide();
+        if (slot >= 0) t.a[plane] = load_wide(a + (int64_t)plane * slots * width_a + k * 128);
+      }
+    };
+    auto multiply = [&](const Step &t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) {
+          const bf16x8 u = widen8(t.w[f][2 * i], t.w[f][2 * i + 1], t.scale[f]);
+#pragma unroll
+          for (int plane = 0; plane < PLANES; ++plane)
+            acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, t.a[plane].v[i], acc[f], 0, 0, 0);
+        }
+    };
+    Step x, y;   // one on its way while the other is multiplied
+    int k = wave;
+    if (k < steps) load(x, k);
+    for (; k < steps; k += 2 * kUpWaves) {
+      if (k + kUpWaves < steps) load(y, k + kUpWaves);
+      multiply(x);
+      if (k + kUpWaves < steps) {
+        if (k + 2 * kUpWaves < steps) load(x, k + 2 * kUpWaves);
+        multiply(y);
+      }
+    }
+    if (first > 0) __syncthreads();
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) sums[wave][f][lane] = acc[f];
+    __syncthreads();
+    const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int u = 0; u < kUpWaves; ++u) sum += ((const float *)&sums[u][f][(c >> 2) * 16 + r])[c & 3];
+      const int h = h0 + f * 16 + c;
+      if (first + r < n && h < p.H) p.y[(int64_t)list[first + r] * p.H + h] = sum;
+    }
+  }
+}
+// out[t] = sum over k of w[t,k] y[t,k], k ascending.
+template <typename OUT>
+__global__ __launch_bounds__(256) void few_sum_kernel(FewParams p) {
+  const int h = (int)blockIdx.x * 256 + (int)threadIdx.x, t = (int)blockIdx.y;
+  if (h >= p.H) return;
+  float sum = 0.0f;
+#pragma unroll 8
+  for (int k = 0; k < p.K; ++k) {
+    const int slot = t * p.K + k;
+    if ((unsigned)(p.ids[slot] - p.first) < (unsigned)p.experts) sum = fmaf(p.weights[slot], p.y[(int64_t)slot * p.H + h], sum);
+  }
+  store_float((OUT *)p.out + (int64_t)t * p.H + h, sum);
+}
+
 static int few_planes(hm_dtype out) { return out == HM_F32 ? 3 : 2; }
 
-template <int GROUPS, int PLANES, typename OUT>
-static hm_status launch_few(const FewParams &p, int64_t experts, hipStream_t stream) {
-  const int64_t strips = row8_bytes(p.F) / 16;
-  hipLaunchKernelGGL((few_up_kernel<GROUPS, PLANES>), dim3((unsigned)(experts * strips)), dim3(kUpWaves * kWave), 0, stream, p);
-  const hm_status up = hm_launch_status();
-  if (up != HM_OK) return up;
-  const int columns = 16, waves = 8;
-  hipLaunchKernelGGL((few_down_kernel<GROUPS, PLANES, OUT>), dim3((unsigned)((p.H + columns - 1) / columns)), dim3(waves * kWave),
-                     (size_t)waves * p.T * 16 * 4, stream, p, columns);
-  return hm_launch_status();
+template <int GROUPS, int PLANES>
+static void launch_few_up(const FewParams &p, int64_t shares, hipStream_t stream) {
+  hipLaunchKernelGGL((few_up_kernel<GROUPS, PLANES>), dim3((unsigned)(row8_bytes(p.F) / 16), (unsigned)shares),
+                     dim3(kUpWaves * kWave), 0, stream, p);
 }
 template <int PLANES, typename OUT>
-static hm_status launch_few_groups(const FewParams &p, int64_t experts, hipStream_t stream) {
-  if (p.T <= 16) return launch_few<1, PLANES, OUT>(p, experts, stream);
-  if (p.T <= 32) return launch_few<2, PLANES, OUT>(p, experts, stream);
-  return launch_few<4, PLANES, OUT>(p, experts, stream);
+static hm_status launch_few(const FewParams &p, int64_t shares, int E, hipStream_t stream) {
+  if (p.T <= 16 || p.T * p.K <= 6 * E) {
+    launch_few_up<1, PLANES>(p, shares, stream);
+  } else if (p.T <= 32) {
+    launch_few_up<2, PLANES>(p, shares, stream);
+  } else {
+    launch_few_up<4, PLANES>(p, shares, stream);
+  }
+  const hm_status up = hm_launch_status();
+  if (up != HM_OK) return up;
+  const int64_t slots = (int64_t)p.T * p.K, staged = PLANES * slots * (row8_bytes(p.F) + 8) * 2, sums = (int64_t)kDownWaves * p.T * 16 * 4;
+  if (slots <= kWave && staged + sums <= 66 * 1024) {
+    const int columns = p.H < 4096 ? 8 : 16;
+    hipLaunchKernelGGL((few_down_kernel<PLANES, OUT>), dim3((unsigned)((p.H + columns - 1) / columns)), dim3(kDownWaves * kWave),
+                       (size_t)(sums + staged), stream, p, columns);
+    return hm_launch_status();
+  }
+  const bool wide = shares * ((p.H + 63) / 64) >= 2048;
+  const int64_t strip = wide ? 64 : 32;
+  hipLaunchKernelGGL((wide ? few_down_slots_kernel<PLANES, 4> : few_down_slots_kernel<PLANES, 2>),
+                     dim3((unsigned)((p.H + strip - 1) / strip), (unsigned)shares), dim3(kUpWaves * kWave), 0, stream, p);
+  const hm_status down = hm_launch_status();
+  if (down != HM_OK) return down;
+  hipLaunchKernelGGL((few_sum_kernel<OUT>), dim3((unsigned)((p.H + 255) / 256), (unsigned)p.T), dim3(256), 0, stream, p);
+  return hm_launch_status();
 }
-
 }  // namespace hm
 
-extern "C" size_t hm_layer_few_workspace_bytes(int32_t T, int32_t K, int32_t F) {
-  if (T < 0 || T > hm::kMostFewTokens || K < 1 || (int64_t)T * K > hm::kMostFewSlots || F < 1 || F > hm::kMostColumns8 / 2) return 0;
-  return (size_t)3 * T * K * hm::row8_bytes(F) * 2;
+extern "C" size_t hm_layer_few_workspace_bytes(int32_t T, int32_t K, int32_t H, int32_t F) {
+  if (T < 0 || T > hm::kMostFewTokens || K < 1 || (int64_t)T * K > hm::kMostFewSlots) return 0;
+  if (H < 1 || H > hm::kMostColumns8 || F < 1 || F > hm::kMostColumns8 / 2) return 0;
+  return (size_t)T * K * (3 * 2 * hm::row8_bytes(F) + 4 * (size_t)H);
 }
 
 extern "C" hm_status hm_layer_few(const void *x, int64_t ld, const void *logits, hm_dtype logits_dtype, int64_t logits_ld,
@@ -340,13 +474,14 @@ extern "C" hm_status hm_layer_few(const void *x, int64_t ld, const void *logits,
   const int64_t hit = experts < (int64_t)T * router->K ? experts : (int64_t)T * router->K;
   if (hit * (row8_bytes(F) / 16) > (1 << 23)) return HM_ERR_SHAPE;
   if (T > 0 && (!x || !w13 || !w13_scale || !w2 || !w2_scale || !out)) return HM_ERR_NULL;
-  if (T > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < hm_layer_few_workspace_bytes(T, router->K, F)))
+  if (T > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < hm_layer_few_workspace_bytes(T, router->K, H, F)))
     return HM_ERR_WORKSPACE;
   const hm_status routed = hm_route(logits, logits_dtype, logits_ld, bias, T, router, topk_ids, topk_weights, hip_stream);
   if (routed != HM_OK || T == 0) return routed;
-  const FewParams p = {(const uint16_t *)x, ld, topk_ids, topk_weights, T, router->K, first, experts, H, F, w13, w13_scale, w2, w2_scale,
-                       (uint16_t *)workspace, out};
+  const FewParams p = {(const uint16_t *)x, ld, topk_ids, topk_weights, T, router->K, first, experts, H, F,
+                       ((1u << 20) + router->K - 1) / router->K, w13, w13_scale, w2, w2_scale,
+                       (uint16_t *)workspace, (float *)((char *)workspace + (int64_t)T * router->K * 6 * row8_bytes(F)), out};
   const hipStream_t stream = (hipStream_t)hip_stream;
-  if (out_dtype == HM_F32) return launch_few_groups<3, float>(p, hit, stream);
-  return launch_few_groups<2, uint16_t>(p, hit, stream);
+  if (out_dtype == HM_F32) return launch_few<3, float>(p, hit, router->E, stream);
+  return launch_few<2, uint16_t>(p, hit, router->E, stream);
 }

@@ -94,12 +94,13 @@ def test_the_layer_of_a_few_tokens_checks_its_arguments():
             dict(F=0), dict(F=(1 << 19) + 1), dict(ld=63), dict(lld=63), dict(ldtype=2), dict(odtype=2), dict(x=P(0x1001)), dict(out=P(0x1001)),
             dict(out=P(0x1002), odtype=F32), dict(w13=P(0x1008)), dict(w2=P(0x1004)), dict(s13=P(0x1001)), dict(s2=P(0x1002)),
             dict(T=64, K=16, experts=1024, E=1024, lld=1024, F=1 << 19))
-    need = L.hm_layer_few_workspace_bytes(4, 4, 32)
+    need = L.hm_layer_few_workspace_bytes(4, 4, 64, 32)
     refused(call, B.HM_ERR_WORKSPACE, dict(ws=None), dict(bytes=need - 1), dict(ws=P(0x1004)))
     assert call(T=0, x=None, w13=None, ws=None, out=None) == B.HM_OK
     size = L.hm_layer_few_workspace_bytes
-    assert size(65, 1, 8) == size(-1, 1, 8) == size(1, 0, 8) == size(64, 17, 8) == size(1, 1, 0) == size(1, 1, (1 << 19) + 1) == 0
-    assert need > 0 and size(64, 16, 1 << 19) == 3 * 1024 * (1 << 19) * 2
+    assert size(65, 1, 8, 8) == size(-1, 1, 8, 8) == size(1, 0, 8, 8) == size(64, 17, 8, 8) == 0
+    assert size(1, 1, 8, 0) == size(1, 1, 8, (1 << 19) + 1) == size(1, 1, 0, 8) == size(1, 1, (1 << 20) + 1, 8) == 0
+    assert need > 0 and size(64, 16, 1 << 20, 1 << 19) == 1024 * (6 * (1 << 19) + 4 * (1 << 20))
 
 
 def test_the_binding_says_what_does_not_fit():
