@@ -177,24 +177,28 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {   // two an instruction
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
 }
-__device__ __forceinline__ void store_eight(uint16_t *p, const float (&v)[8]) {
+__device__ __forceinline__ void store_floats(uint16_t *p, const float (&v)[8]) {
   *(u32x4_align2 *)p = u32x4{round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]),
                              round_bf16x2(v[6], v[7])};
 }
-__device__ __forceinline__ void store_eight(float *p, const float (&v)[8]) {
-  *(f32x4_align4 *)p = f32x4{v[0], v[1], v[2], v[3]};
-  *(f32x4_align4 *)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+__device__ __forceinline__ void store_floats(uint16_t *p, const float (&v)[4]) {
+  *(u32x2_align2 *)p = u32x2_align2{round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3])};
+}
+template <int N>
+__device__ __forceinline__ void store_floats(float *p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) *(f32x4_align4 *)(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 __device__ __forceinline__ void store_float(uint16_t *p, float v) { *p = (uint16_t)round_bf16x2(v, v); }
 __device__ __forceinline__ void store_float(float *p, float v) { *p = v; }
-// Elements c to c + 7 of a row of C.
-template <typename OUT>
-__device__ __forceinline__ void store_row(OUT *row, int c, int C, const float (&v)[8]) {
-  if (c + 8 <= C) {
-    store_eight(row + c, v);
+// Elements c to c + N - 1 of a row of C.
+template <int N, typename OUT>
+__device__ __forceinline__ void store_row(OUT *row, int c, int C, const float (&v)[N]) {
+  if (c + N <= C) {
+    store_floats(row + c, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < N; ++i)
       if (c + i < C) store_float(row + c + i, v[i]);
   }
 }

@@ -19,11 +19,23 @@ struct GatedParams {
   bool a_bf16;
 };
 
-// The kernels round alike, whichever writes a value: no products and sums are joined but where it says so.
-__device__ __forceinline__ float gated_value(float gate, float up) {
+// s = 1 / (1 + exp(-gate)) and gate s.  exp(-x) = 2^(-x log2 e), of whose exponent the part that is lost to its rounding is
+// multiplied back in: three instructions more than the bare power, and right to two units in the last place for every x.  The
+// reciprocal has one Newton step.  Beyond 88 in size s is 1 or at most e^-88.  All kernels round alike, whichever writes a value: no product and
+// sum are joined but where it says so.
+struct Gate {
+  float s, times;
+};
+__device__ __forceinline__ Gate gate_of(float gate) {
 #pragma clang fp contract(off)
-  return gate / (1.0f + expf(-gate)) * up;
+  constexpr float kLog2E = 1.44269502f, kRest = 1.92596299e-8f, kLn2 = 0.693147181f;   // log2 e = the first and the second
+  const float x = __builtin_amdgcn_fmed3f(gate, -88.0f, 88.0f), t = -x * kLog2E;
+  const float lost = fmaf(-x, kRest, fmaf(-x, kLog2E, -t)), power = __builtin_amdgcn_exp2f(t);
+  const float y = 1.0f + fmaf(power, lost * kLn2, power), r = __builtin_amdgcn_rcpf(y);   // y is finite: r may be 0, not NaN
+  const float s = fmaf(fmaf(-y, r, 1.0f), r, r);
+  return {s, gate * s};
 }
+__device__ __forceinline__ float gated_value(float gate, float up) { return gate_of(gate).times * up; }
 
 // First and last row of all segments.
 __device__ __forceinline__ void rows_of_segments(const int32_t *__restrict__ offsets, int segments, int64_t rows, int64_t &from, int64_t &to) {
@@ -35,36 +47,27 @@ __device__ __forceinline__ void rows_of_segments(const int32_t *__restrict__ off
   }
 }
 
-// A wave takes 512 columns of a of ROWS rows.
-template <typename IN, int ROWS>
+// A wave takes 512 columns of a row of a; neighbouring waves take neighbouring pieces.
+template <typename IN>
 __global__ __launch_bounds__(kGatedThreads) void gated_kernel(GatedParams p) {
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-  const uint32_t block = blockIdx.x / (uint32_t)p.parts;
-  const int part = (int)(blockIdx.x - block * (uint32_t)p.parts), c = part * 512 + lane * 8;
-  const int64_t first = ((int64_t)block * kGatedWaves + wave) * ROWS;
-  const bool whole = part * 512 + 512 <= p.F;
-  const int width = (int)row8_bytes(p.F);
+  const uint32_t piece = blockIdx.x * (uint32_t)kGatedWaves + (uint32_t)wave, r = piece / (uint32_t)p.parts;
+  const int part = (int)(piece - r * (uint32_t)p.parts), c = part * 512 + lane * 8;
   int64_t from, to;
   rows_of_segments(p.offsets, p.segments, p.rows, from, to);
-  float gate[ROWS][8], up[ROWS][8];
+  if (r < from || r >= to) return;
+  const bool whole = part * 512 + 512 <= p.F;
+  const IN *row = (const IN *)p.h + r * p.ld;
+  float a[8], up[8];
+  load_row(row, c, p.F, whole, a);
+  load_row(row + p.F, c, p.F, whole, up);
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {   // rows behind the last are read from it
-    const IN *row = (const IN *)p.h + min(first + i, p.rows - 1) * p.ld;
-    load_row(row, c, p.F, whole, gate[i]);
-    load_row(row + p.F, c, p.F, whole, up[i]);
+  for (int j = 0; j < 8; ++j) a[j] = gated_value(a[j], up[j]);
+  if (p.a) {
+    if (p.a_bf16) store_row((uint16_t *)p.a + (int64_t)r * p.F, c, p.F, a);
+    else store_row((float *)p.a + (int64_t)r * p.F, c, p.F, a);
   }
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const int64_t r = first + i;
-    if (r < from || r >= to) continue;   // the same for the wave
-#pragma unroll
-    for (int j = 0; j < 8; ++j) gate[i][j] = gated_value(gate[i][j], up[i][j]);
-    if (p.a) {
-      if (p.a_bf16) store_row((uint16_t *)p.a + r * p.F, c, p.F, gate[i]);
-      else store_row((float *)p.a + r * p.F, c, p.F, gate[i]);
-    }
-    if (p.q) store_piece8(p.q + r * width, p.scale + r * scale8_bytes(p.F), part, width, gate[i]);
-  }
+  if (p.q) store_piece8(p.q + r * row8_bytes(p.F), p.scale + r * scale8_bytes(p.F), part, (int)row8_bytes(p.F), a);
 }
 
 struct GatedBackParams {
@@ -80,171 +83,275 @@ struct GatedBackParams {
   int32_t blocks, tiles;   // of 128 rows of a segment; of 128 columns
 };
 
-struct GatedGradient {
-  float gate, up;
-};
-__device__ __forceinline__ GatedGradient gated_gradient(float gate, float up, float ga) {
+// The gradient's two halves: ga up s (1 + gate (1 - s)) and ga gate s.
+__device__ __forceinline__ float gradient_of_gate(const Gate &g, float up, float ga) {
 #pragma clang fp contract(off)
-  const float s = 1.0f / (1.0f + expf(-gate));
-  return {ga * up * s * fmaf(gate, 1.0f - s, 1.0f), ga * gate * s};
+  return ga * up * fmaf(g.times, 1.0f - g.s, g.s);
 }
+__device__ __forceinline__ float gradient_of_up(const Gate &g, float ga) { return ga * g.times; }
 
-// Rows of [g_gate | g_up]: a wave takes 512 columns of ROWS rows, of either half or of both.
-template <typename IN, int ROWS>
+// Rows of [g_gate | g_up]: a wave takes 512 columns of a row, of either half or of both.
+template <typename IN>
 __global__ __launch_bounds__(kGatedThreads) void gated_backward_rows_kernel(GatedBackParams p) {
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-  const uint32_t block = blockIdx.x / (uint32_t)p.parts;
-  const int part = (int)(blockIdx.x - block * (uint32_t)p.parts), c = part * 512 + lane * 8, F = p.F;
-  const int64_t first = ((int64_t)block * kGatedWaves + wave) * ROWS;
-  const int width = (int)row8_bytes(2 * (int64_t)F);
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), F = p.F;
+  const uint32_t piece = blockIdx.x * (uint32_t)kGatedWaves + (uint32_t)wave, r = piece / (uint32_t)p.parts;
+  const int part = (int)(piece - r * (uint32_t)p.parts), c = part * 512 + lane * 8;
   int64_t from, to;
   rows_of_segments(p.offsets, p.segments, p.rows, from, to);
+  if (r < from || r >= to) return;
   // columns c to c + 7 of the gradient are those from `at` on of one half, or the first `mine` of them are g_gate's last
   const bool upper = c >= F;
   const int at = upper ? c - F : c, mine = upper ? 0 : min(F - c, 8);
-  const bool whole = (part * 512 + 512 <= F) || (part * 512 >= F && part * 512 + 512 <= 2 * (int64_t)F);
-  float v[ROWS][8];
+  const bool whole = part * 512 + 512 <= F || (part * 512 >= F && part * 512 + 512 <= 2 * F);
+  const IN *h = (const IN *)p.h + r * p.ld, *from_ga = (const IN *)p.ga + r * p.ga_ld;
+  float v[8], up[8], ga[8];
+  load_row(h, at, F, whole, v);
+  load_row(h + F, at, F, whole, up);
+  load_row(from_ga, at, F, whole, ga);
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const int64_t r = min(first + i, p.rows - 1);
-    const IN *h = (const IN *)p.h + r * p.ld, *from_ga = (const IN *)p.ga + r * p.ga_ld;
-    float gate[8], up[8], ga[8];
-    load_row(h, at, F, whole, gate);
-    load_row(h + F, at, F, whole, up);
-    load_row(from_ga, at, F, whole, ga);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const GatedGradient g = gated_gradient(gate[j], up[j], ga[j]);
-      v[i][j] = upper ? g.up : g.gate;
-    }
-    if (!whole && mine < 8 && mine > 0) {   // g_up's first behind g_gate's last
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j >= mine && j - mine < F) {
-          const int n = j - mine;
-          v[i][j] = gated_gradient(load_float(h + n), load_float(h + F + n), load_float(from_ga + n)).up;
-        }
-    }
+  for (int j = 0; j < 8; ++j) {
+    const Gate g = gate_of(v[j]);
+    v[j] = upper ? gradient_of_up(g, ga[j]) : gradient_of_gate(g, up[j], ga[j]);
   }
+  if (!whole && mine < 8 && mine > 0) {   // g_up's first behind g_gate's last
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const int64_t r = first + i;
-    if (r < from || r >= to) continue;
-    if (p.gh) {
-      if (p.gh_bf16) store_row((uint16_t *)p.gh + r * 2 * F, c, 2 * F, v[i]);
-      else store_row((float *)p.gh + r * 2 * F, c, 2 * F, v[i]);
-    }
-    if (p.q) store_piece8(p.q + r * width, p.scale + r * scale8_bytes(2 * (int64_t)F), part, width, v[i]);
+    for (int j = 0; j < 8; ++j)
+      if (j >= mine && j - mine < F) v[j] = gradient_of_up(gate_of(load_float(h + j - mine)), load_float(from_ga + j - mine));
   }
+  if (p.gh) {
+    if (p.gh_bf16) store_row((uint16_t *)p.gh + (int64_t)r * 2 * F, c, 2 * F, v);
+    else store_row((float *)p.gh + (int64_t)r * 2 * F, c, 2 * F, v);
+  }
+  if (p.q) store_piece8(p.q + r * row8_bytes(2 * (int64_t)F), p.scale + r * scale8_bytes(2 * (int64_t)F), part, (int)row8_bytes(2 * (int64_t)F), v);
 }
 
-// A workgroup takes a block of 128 rows of a segment and 128 columns of each half; a thread four rows of eight columns.
-// g_gate, g_up and a one after the other: rows leave from registers, columns are turned in LDS.
-constexpr int kTurnThreads = 512, kTurnPitch = 128 + 8;
+// Four values as they were loaded, zeros behind a row's end.
 template <typename IN>
-__global__ __launch_bounds__(kTurnThreads) void gated_backward_kernel(GatedBackParams p) {
-  constexpr int kWaves = kTurnThreads / kWave;
-  __shared__ __attribute__((aligned(16))) uint8_t turned[128 * kTurnPitch];
-  __shared__ uint32_t most_of[kWaves][128];
-  const int64_t all = (int64_t)p.blocks * p.tiles, per_die = (all + 7) / 8;
-  const int64_t at = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);   // a die gets neighbouring tiles
-  if ((int64_t)(blockIdx.x >> 3) >= per_die || at >= all) return;
-  const int b = (int)(at / p.tiles), tile = (int)(at - (int64_t)b * p.tiles);
-  const BlockOwner8 owner = owner_of_block8(p.offsets, p.segments, (int)p.rows, b);
-  if (owner.segment < 0) return;
-  const int first = owner.rows.from + (b - first_block8(owner.rows.from, owner.segment)) * 128, end = owner.rows.to;
-  if (first >= end) return;
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave, F = p.F;
-  const int c0 = tile * 128, cl = (tid & 15) * 8, c = c0 + cl, rl = (tid >> 4) * 4;
-  const bool whole = c0 + 128 <= F;
-  float gate[4][8], up[4][8], ga[4][8];
+struct Four;
+template <>
+struct Four<uint16_t> {
+  uint32_t w[2];
+  // columns c to c + 3 of the row of C that begins `at` elements, less than 2^30, behind `rows`
+  __device__ __forceinline__ void load(const uint16_t *rows, uint32_t at, int c, int C, bool whole) {
+    if (whole) {
+      const u32x2_align2 t = *(const u32x2_align2 *)((const char *)rows + (at + (uint32_t)c) * 2u);
+      w[0] = t[0];
+      w[1] = t[1];
+    } else {
+      float v[4];
+      load_row_end<4>(rows + at, c, C, v);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {   // rows behind the segment are read from its last and count as zeros
-    const int64_t r = min(first + rl + i, end - 1);
-    const IN *h = (const IN *)p.h + r * p.ld;
-    load_row(h, c, F, whole, gate[i]);
-    load_row(h + F, c, F, whole, up[i]);
-    load_row((const IN *)p.ga + r * p.ga_ld, c, F, whole, ga[i]);
+      for (int i = 0; i < 2; ++i) w[i] = __builtin_bit_cast(uint32_t, v[2 * i]) >> 16 | __builtin_bit_cast(uint32_t, v[2 * i + 1]);
+    }
   }
-  const int64_t width = row8_bytes(2 * (int64_t)F), scales = scale8_bytes(2 * (int64_t)F);
+  __device__ __forceinline__ float at(int i) const { return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
+  __device__ __forceinline__ void keep(bool there) {   // or zeros
 #pragma unroll
-  for (int plane = 0; plane < 3; ++plane) {
-    const int half = plane == 1 ? F : 0;   // first column of this half
-    float v[4][8];
+    for (int i = 0; i < 2; ++i) w[i] = there ? w[i] : 0u;
+  }
+};
+template <>
+struct Four<float> {
+  float v[4];
+  __device__ __forceinline__ void load(const float *rows, uint32_t at, int c, int C, bool whole) {
+    if (whole) load_floats<4>((const float *)((const char *)rows + (at + (uint32_t)c) * 4u), v);
+    else load_row_end<4>(rows + at, c, C, v);
+  }
+  __device__ __forceinline__ float at(int i) const { return v[i]; }
+  __device__ __forceinline__ void keep(bool there) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const GatedGradient g = gated_gradient(gate[i][j], up[i][j], ga[i][j]);
-        const float x = plane == 0 ? g.gate : plane == 1 ? g.up : gated_value(gate[i][j], up[i][j]);
-        v[i][j] = first + rl + i < end ? x : 0.0f;
+    for (int i = 0; i < 4; ++i) v[i] = there ? v[i] : 0.0f;
+  }
+};
+// The larger of each pair of lanes 16, or 32, apart, in both.
+__device__ __forceinline__ uint32_t max_16_apart(uint32_t v) {
+  const auto t = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max((uint32_t)t[0], (uint32_t)t[1]);
+}
+__device__ __forceinline__ uint32_t max_32_apart(uint32_t v) {
+  const auto t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max((uint32_t)t[0], (uint32_t)t[1]);
+}
+
+// The values of one element: g_gate, g_up and a.
+struct Three {
+  float v[3];
+};
+__device__ __forceinline__ Three three_of(float gate, float up, float ga) {
+  const Gate g = gate_of(gate);
+  return {{gradient_of_gate(g, up, ga), gradient_of_up(g, ga), g.times * up}};
+}
+__device__ __forceinline__ float finite_size(float v) { return fabsf(v) < __builtin_inff() ? fabsf(v) : 0.0f; }   // 0 of others
+
+// A tile is a block of 128 rows of a segment and 128 columns of each half; a thread has four rows of four columns.  Rows leave from
+// registers and the columns' largest values meet in LDS, and behind a barrier the values are turned in LDS and stored as columns.
+// What a thread loads for the next tile is on its way meanwhile, so a workgroup goes through several; one fills a CU.
+constexpr int kTurnThreads = 1024, kTurnPitch = 128 + 4, kTurnRows = 4, kTurnGroups = 256;
+// Everybody's accesses of LDS are done; loads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+  __asm__ volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  __asm__ volatile("" ::: "memory");
+}
+template <typename IN, bool VALUES>   // whether gh is wanted: stores of any alignment are much code, which runs cold
+__global__ __launch_bounds__(kTurnThreads, 4) void gated_backward_kernel(GatedBackParams p) {
+  __shared__ __attribute__((aligned(16))) uint8_t turned[3][128 * kTurnPitch];
+  __shared__ uint32_t most_of[2][3][4][32];   // of every other tile: column 4 i + j at [j][i]
+  __shared__ int32_t offsets[kMostSegments8 + 1];
+  const int tid = threadIdx.x, lane = lane_id(), F = p.F;
+  const int i32 = tid & 31, cl = i32 * 4, rl = (tid >> 5) * kTurnRows;
+  for (int i = tid; i <= p.segments; i += kTurnThreads) offsets[i] = p.offsets[i];
+  if (tid < 3 * 128) (&most_of[0][0][0][0])[tid] = 0;
+  lds_barrier();
+  const int64_t all = (int64_t)p.blocks * p.tiles, per_die = (all + 7) / 8;   // a die gets neighbouring tiles
+  const int64_t last = min((int64_t)((blockIdx.x & 7) + 1) * per_die, all);
+  int64_t at = (int64_t)(blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
+  struct Place {
+    int b, c0, first, end;
+  };
+  auto next_place = [&](Place &t) {   // the next tile with rows; false: none is left
+    for (; at < last; at += gridDim.x >> 3) {
+      t.b = (int)(at / p.tiles);
+      t.c0 = (int)(at - (int64_t)t.b * p.tiles) * 128;
+      const BlockOwner8 owner = owner_of_block8(offsets, p.segments, (int)p.rows, t.b);
+      t.end = owner.rows.to;
+      t.first = owner.segment < 0 ? t.end : owner.rows.from + (t.b - first_block8(owner.rows.from, owner.segment)) * 128;
+      if (t.first < t.end) {
+        at += gridDim.x >> 3;
+        t.b = __builtin_amdgcn_readfirstlane(t.b);
+        t.c0 = __builtin_amdgcn_readfirstlane(t.c0);
+        t.first = __builtin_amdgcn_readfirstlane(t.first);
+        t.end = __builtin_amdgcn_readfirstlane(t.end);
+        return true;
       }
-    if (plane < 2) {
+    }
+    return false;
+  };
+  Four<IN> gate[kTurnRows], up[kTurnRows], ga[kTurnRows];
+  auto load = [&](const Place &t) {
+    // uniform bases and offsets of 32 bits: addresses of 64 bits would take as many registers again as what they load
+    const IN *from_h = (const IN *)p.h + (int64_t)t.first * p.ld, *from_ga = (const IN *)p.ga + (int64_t)t.first * p.ga_ld;
+    const bool whole = t.c0 + 128 <= F;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t r = first + rl + i;
-        if (p.gh && r < end) {
-          if (p.gh_bf16) store_row((uint16_t *)p.gh + r * 2 * F + half, c, F, v[i]);
-          else store_row((float *)p.gh + r * 2 * F + half, c, F, v[i]);
+    for (int i = 0; i < kTurnRows; ++i) {   // rows behind the segment are read from its last and count as zeros
+      const uint32_t r = (uint32_t)min(rl + i, t.end - 1 - t.first);
+      const uint32_t at_h = r * (uint32_t)p.ld, at_ga = r * (uint32_t)p.ga_ld;
+      gate[i].load(from_h, at_h, t.c0 + cl, F, whole);
+      up[i].load(from_h + F, at_h, t.c0 + cl, F, whole);
+      ga[i].load(from_ga, at_ga, t.c0 + cl, F, whole);
+    }
+  };
+  const int64_t width = row8_bytes(2 * (int64_t)F), scales = scale8_bytes(2 * (int64_t)F);
+  const int64_t row_bytes = column8_blocks(p.rows, p.segments) * 128;
+  Place place;
+  if (!next_place(place)) return;
+  load(place);
+  for (int turn = 0;; turn ^= 1) {
+    const int c = place.c0 + cl;
+    float v[3][kTurnRows][4], column[3][4];
+#pragma unroll
+    for (int n = 0; n < 3; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) column[n][j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTurnRows; ++i) {
+      const int64_t r = place.first + rl + i;
+      const bool there = r < place.end;
+      gate[i].keep(there);
+      up[i].keep(there);
+      ga[i].keep(there);
+      float most[2] = {0.0f, 0.0f};   // a NaN does not count
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const Three t = three_of(gate[i].at(j), up[i].at(j), ga[i].at(j));
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+          v[n][i][j] = t.v[n];
+          column[n][j] = fmaxf(column[n][j], fabsf(t.v[n]));
+          __asm__("" : "+v"(column[n][j]), "+v"(v[n][i][j]));   // now: put off, what they are computed from would take more registers
         }
-        if (p.q) {   // whole blocks of both halves: F is a multiple of 128
-          float u[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) u[j] = v[i][j];
-          const int code = scale_code8(max16(largest_bits(u)));
-          const float by = inverse_scale8(code);
-          if (r < end) {
-            *(uint64_t *)(p.q + r * width + half + c) =
-                (uint64_t)pack8(u[4], u[5], u[6], u[7], by) << 32 | pack8(u[0], u[1], u[2], u[3], by);
-            const int k = (half + c0) / 128;
-            if ((lane & 15) == 0) p.scale[r * scales + k] = (uint8_t)code;
-            if ((lane & 15) < 3 && k == 2 * F / 128 - 1 && k + 1 + (lane & 15) < scales)
-              p.scale[r * scales + k + 1 + (lane & 15)] = 0;   // zeros behind the last
+        for (int n = 0; n < 2; ++n) most[n] = fmaxf(most[n], fabsf(t.v[n]));
+      }
+      if (VALUES && there) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          if (p.gh_bf16) store_row((uint16_t *)p.gh + r * 2 * F + n * F, c, F, v[n][i]);
+          else store_row((float *)p.gh + r * 2 * F + n * F, c, F, v[n][i]);
+        }
+      }
+      if (p.q) {   // whole blocks of both halves: F is a multiple of 128
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          if (most[n] == __builtin_inff()) {   // nor does an infinity; both become NaN in 8 bits
+            most[n] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) most[n] = fmaxf(most[n], finite_size(v[n][i][j]));
+          }
+          const int code = scale_code8(max_16_apart(max16(__builtin_bit_cast(uint32_t, most[n]))));
+          if (there) {
+            const int k = (n * F + place.c0) / 128;
+            *(uint32_t *)(p.q + r * width + n * F + c) = pack8(v[n][i][0], v[n][i][1], v[n][i][2], v[n][i][3], inverse_scale8(code));
+            if (i32 == 0) p.scale[r * scales + k] = (uint8_t)code;
+            if (i32 < 3 && k == 2 * F / 128 - 1 && k + 1 + i32 < scales) p.scale[r * scales + k + 1 + i32] = 0;   // zeros behind the last
           }
         }
       }
     }
-    uint8_t *to = plane < 2 ? p.q_columns : p.a_columns, *to_scale = plane < 2 ? p.scale_columns : p.a_scale;
-    if (!to) continue;
-    const int64_t C = plane < 2 ? 2 * (int64_t)F : F;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float u[4] = {v[0][j], v[1][j], v[2][j], v[3][j]};
-      uint32_t most = largest_bits(u);
+    for (int n = 0; n < 3; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i][j] = u[i];
-      most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
-      most = max(most, (uint32_t)__shfl_xor((int)most, 32, kWave));
-      if (lane < 16) most_of[wave][cl + j] = most;
+      for (int j = 0; j < 4; ++j) {
+        if (column[n][j] == __builtin_inff()) {
+          column[n][j] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kTurnRows; ++i) column[n][j] = fmaxf(column[n][j], finite_size(v[n][i][j]));
+        }
+        const uint32_t most = max_32_apart(__builtin_bit_cast(uint32_t, column[n][j]));
+        if (lane < 32) atomicMax(&most_of[turn][n][j][i32], most);
+      }
+    const Place here = place;
+    const bool more = next_place(place);
+    if (more) load(place);
+    lds_barrier();
+#pragma unroll
+    for (int n = 0; n < 3; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int code = scale_code8(most_of[turn][n][j][i32]);
+        *(uint32_t *)(turned[n] + (cl + j) * kTurnPitch + rl) = pack8(v[n][0][j], v[n][1][j], v[n][2][j], v[n][3][j], inverse_scale8(code));
+      }
+    if (tid < 128 && here.c0 + tid < F) {
+#pragma unroll
+      for (int n = 0; n < 3; ++n) {
+        uint8_t *to = n < 2 ? p.scale_columns : p.a_scale;
+        const int64_t C = n < 2 ? 2 * (int64_t)F : F;
+        if (to) to[(int64_t)here.b * C + (n == 1 ? F : 0) + here.c0 + tid] = (uint8_t)scale_code8(most_of[turn][n][tid & 3][tid >> 2]);
+      }
     }
-    __syncthreads();
+    if (tid < 3 * 128) (&most_of[turn ^ 1][0][0][0])[tid] = 0;   // nobody has read it since the last tile's second barrier
+    lds_barrier();
+    const int col = tid >> 3, piece = (tid & 7) * 16;
+    if (here.c0 + col < F) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) m = max(m, most_of[w][cl + j]);
-      const int code = scale_code8(m);
-      if (tid < 16 && c + j < F) to_scale[(int64_t)b * C + half + c + j] = (uint8_t)code;
-      *(uint32_t *)(turned + (cl + j) * kTurnPitch + rl) = pack8(v[0][j], v[1][j], v[2][j], v[3][j], inverse_scale8(code));
+      for (int n = 0; n < 3; ++n) {
+        uint8_t *to = n < 2 ? p.q_columns : p.a_columns;
+        if (!to) continue;
+        const uint32_t *in = (const uint32_t *)(turned[n] + col * kTurnPitch + piece);
+        *(u32x4 *)(to + (int64_t)((n == 1 ? F : 0) + here.c0 + col) * row_bytes + (int64_t)here.b * 128 + piece) =
+            u32x4{in[0], in[1], in[2], in[3]};
+      }
     }
-    __syncthreads();
-    const int col = tid >> 2, piece = (tid & 3) * 32;
-    if (c0 + col < F) {
-      const int64_t row_bytes = column8_blocks(p.rows, p.segments) * 128;
-      uint64_t *out = (uint64_t *)(to + (int64_t)(half + c0 + col) * row_bytes + (int64_t)b * 128 + piece);
-      const uint64_t *in = (const uint64_t *)(turned + col * kTurnPitch + piece);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) out[i] = in[i];
-    }
-    // the next plane writes `turned` behind its first barrier and `most_of`, which is read before this one's second
+    if (!more) return;   // the same for the workgroup
   }
 }
 
 static bool segments_given_ok(const int32_t *offsets, int32_t segments, int64_t rows) {
   return !offsets || segments8_ok(segments, rows);
 }
-// Rows of a wave: one where few rows would not fill the chip otherwise.
-static int rows_of_wave(int64_t rows, int32_t parts) { return rows * parts >= 32768 ? 4 : 1; }
+static unsigned gated_blocks(int64_t rows, int32_t parts) { return (unsigned)((rows * parts + kGatedWaves - 1) / kGatedWaves); }
+constexpr int64_t kMostTurnPitch = 1 << 22;   // 128 rows of it within offsets of 32 bits
 constexpr int64_t kMostGatedPieces = 1 << 25;   // of 512 columns, of all rows
 
 }  // namespace hm
@@ -262,12 +369,9 @@ extern "C" hm_status hm_gated(const void *h, hm_dtype dtype, int64_t ld, const i
   if (!h) return HM_ERR_NULL;
   const int32_t parts = (F + 511) / 512;
   const GatedParams p = {h, ld, offsets, segments, rows, F, parts, a, q, scale, a_dtype == HM_BF16};
-  const int each = rows_of_wave(rows, parts);
-  const int64_t blocks = (rows + kGatedWaves * each - 1) / (kGatedWaves * each) * parts;
   if (rows * parts > kMostGatedPieces) return HM_ERR_SHAPE;
-  const auto kernel = dtype == HM_BF16 ? each == 4 ? gated_kernel<uint16_t, 4> : gated_kernel<uint16_t, 1>
-                                       : each == 4 ? gated_kernel<float, 4> : gated_kernel<float, 1>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kGatedThreads), 0, (hipStream_t)hip_stream, p);
+  const auto kernel = dtype == HM_BF16 ? gated_kernel<uint16_t> : gated_kernel<float>;
+  hipLaunchKernelGGL(kernel, dim3(gated_blocks(rows, parts)), dim3(kGatedThreads), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }
 
@@ -292,23 +396,21 @@ extern "C" hm_status hm_gated_backward(const void *h, const void *ga, hm_dtype d
                        q_columns, scale_columns, a_columns, a_scale, 0, (F + 127) / 128};
   // blocks of 8 bits of a row that lie in both halves are not the tiles'
   const bool by_rows = !columns || (q && F % 128 != 0);
-  const int each = rows_of_wave(rows, p.parts);
-  const int64_t row_blocks = (rows + kGatedWaves * each - 1) / (kGatedWaves * each) * p.parts;
   if (rows * p.parts > kMostGatedPieces) return HM_ERR_SHAPE;
   if (columns) {
     p.blocks = (int32_t)column8_blocks(rows, segments);
     const int64_t workgroups = ((int64_t)p.blocks * p.tiles + 7) / 8 * 8;
-    if (workgroups > (1 << 22)) return HM_ERR_SHAPE;
+    if (workgroups > (1 << 22) || ld > kMostTurnPitch || ga_ld > kMostTurnPitch) return HM_ERR_SHAPE;
     GatedBackParams tiles = p;
     if (by_rows) tiles.q = nullptr;
-    const auto kernel = dtype == HM_BF16 ? gated_backward_kernel<uint16_t> : gated_backward_kernel<float>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)workgroups), dim3(kTurnThreads), 0, (hipStream_t)hip_stream, tiles);
+    const auto kernel = dtype == HM_BF16 ? gh ? gated_backward_kernel<uint16_t, true> : gated_backward_kernel<uint16_t, false>
+                                         : gh ? gated_backward_kernel<float, true> : gated_backward_kernel<float, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(workgroups < kTurnGroups ? workgroups : kTurnGroups)), dim3(kTurnThreads), 0, (hipStream_t)hip_stream, tiles);
     const hm_status launched = hm_launch_status();
     if (launched != HM_OK || !by_rows) return launched;
     p.gh = nullptr;   // written
   }
-  const auto kernel = dtype == HM_BF16 ? each == 4 ? gated_backward_rows_kernel<uint16_t, 4> : gated_backward_rows_kernel<uint16_t, 1>
-                                       : each == 4 ? gated_backward_rows_kernel<float, 4> : gated_backward_rows_kernel<float, 1>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)row_blocks), dim3(kGatedThreads), 0, (hipStream_t)hip_stream, p);
+  const auto kernel = dtype == HM_BF16 ? gated_backward_rows_kernel<uint16_t> : gated_backward_rows_kernel<float>;
+  hipLaunchKernelGGL(kernel, dim3(gated_blocks(rows, p.parts)), dim3(kGatedThreads), 0, (hipStream_t)hip_stream, p);
   return hm_launch_status();
 }

@@ -146,6 +146,39 @@ def test_each_output_alone_is_the_same(F):
         assert torch.equal(free[i][:280].view(torch.uint8), whole[i][:280].view(torch.uint8)) and not is_poison(free[i][280:])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("F", [128, 130])
+def test_what_is_no_number_becomes_nan_and_does_not_count(dtype, F):
+    """Infinities and NaN in a block: those values are NaN in 8 bits, the others keep the scale that they have without them."""
+    rows = 140
+    h, ga = drawn(1, rows, 2 * F, dtype, 2.0), drawn(2, rows, F, dtype, 0.03)
+    odd = torch.zeros((rows, F), dtype=torch.bool)
+    for r, c, which, v in ((0, 0, "ga", float("inf")), (5, 77, "ga", float("-inf")), (9, 3, "ga", float("nan")), (127, 127, "gate", float("nan")),
+                           (128, 2, "up", float("inf")), (130, 9, "up", float("nan")), (139, 100, "ga", float("inf"))):
+        odd[r, c] = True
+        if which == "ga":
+            ga[r, c] = v
+        else:
+            h[r, c + (F if which == "up" else 0)] = v
+    offsets = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    full, a = torch.empty((rows, 2 * F), device="cuda"), torch.empty((rows, F), device="cuda")
+    rows8, a_rows8 = B.alloc_rows8(rows, 2 * F), B.alloc_rows8(rows, F)
+    columns8, a8 = poisoned(B.alloc_columns8(rows, 1, 2 * F)), poisoned(B.alloc_columns8(rows, 1, F))
+    B.hm_gated_backward(h.cuda(), ga.cuda(), offsets, full, *rows8, *columns8, *a8)
+    B.hm_gated(h.cuda(), a, *a_rows8)
+    finite = torch.isfinite(full).cpu()
+    assert not finite[:, :F][odd].all() and finite[:, :F][~odd].all() and finite[:, F:][~odd].all()
+    for pair, values in ((rows8, full), (a_rows8, a)):
+        want, want_codes = R.rows8(f64(values))
+        q, codes = numbers8(pair)
+        assert np.array_equal(codes, want_codes) and np.array_equal(q, want, equal_nan=True)
+    for pair, values in ((columns8, full), (a8, a)):
+        want, want_codes, there = R.columns8(f64(values), offsets.cpu().numpy())
+        q, codes = numbers8(pair)
+        assert np.array_equal(codes[there], want_codes[there])
+        assert np.array_equal(q[:, np.repeat(there, 128)], want[:, np.repeat(there, 128)], equal_nan=True)
+
+
 def test_rows_of_segments_only():
     h = drawn(1, 40, 64, F32).cuda()
     offsets = torch.tensor([3, 3, 20, 31], dtype=torch.int32, device="cuda")
