@@ -158,6 +158,58 @@ __device__ __forceinline__ void load_row_end(const IN *__restrict__ row, int c, 
   for (int i = 0; i < N; ++i) v[i] = by < N ? v[i] : 0.0f;
 }
 
+// Eight elements as they were loaded.
+template <typename IN>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+  u32x4 w;
+  Eight() = default;
+  __device__ __forceinline__ explicit Eight(const uint16_t *p) : w(*(const u32x4_align2 *)p) {}
+  __device__ __forceinline__ float at(int i) const { return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
+  // What has been computed from them is forgotten, not kept in registers.
+  __device__ __forceinline__ void forget() { __asm__("" : "+v"(w)); }
+  __device__ __forceinline__ float times(const Eight &v, float sum) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = fmaf(bf16_hi(w[i]), bf16_hi(v.w[i]), fmaf(bf16_lo(w[i]), bf16_lo(v.w[i]), sum));
+    return sum;
+  }
+};
+template <>
+struct Eight<float> {
+  f32x4 a, b;
+  Eight() = default;
+  __device__ __forceinline__ explicit Eight(const float *p)
+      : a(*(const f32x4_align4 *)p), b(*(const f32x4_align4 *)(p + 4)) {}
+  __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
+  __device__ __forceinline__ void forget() { __asm__("" : "+v"(a), "+v"(b)); }
+  __device__ __forceinline__ float times(const Eight &v, float sum) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = fmaf(b[i], v.b[i], fmaf(a[i], v.a[i], sum));
+    return sum;
+  }
+};
+// Those of a row of C from column c on, zeros behind its end; `whole` (uniform): none of the wave's reach it.
+__device__ __forceinline__ Eight<uint16_t> eight_of_row(const uint16_t *__restrict__ row, int c, int C, bool whole) {
+  if (whole) return Eight<uint16_t>(row + c);
+  float v[8];
+  load_row_end<8>(row, c, C, v);
+  Eight<uint16_t> e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    e.w[i] = __builtin_bit_cast(uint32_t, v[2 * i]) >> 16 | (__builtin_bit_cast(uint32_t, v[2 * i + 1]) & 0xFFFF0000u);
+  return e;
+}
+__device__ __forceinline__ Eight<float> eight_of_row(const float *__restrict__ row, int c, int C, bool whole) {
+  if (whole) return Eight<float>(row + c);
+  float v[8];
+  load_row_end<8>(row, c, C, v);
+  Eight<float> e;
+  e.a = f32x4{v[0], v[1], v[2], v[3]};
+  e.b = f32x4{v[4], v[5], v[6], v[7]};
+  return e;
+}
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // Eight values as bf16, times their block's power of two, of which the conversion takes the exponent (code 0 too is

@@ -20,26 +20,37 @@ struct NormParams {
   bool weight_bf16, y_bf16;
 };
 
-// The sum over a row's threads, in all of them; `sums` has a place for every wave, another one from call to call, so that one
+// The sums over a row's threads, in all of them; `sums` has a place for every wave, another one from call to call, so that one
 // barrier is enough.
 template <int THREADS, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float (&sums)[2][N][THREADS / kWave > 0 ? THREADS / kWave : 1], int turn) {
+__device__ __forceinline__ void row_sums(const float (&v)[N], float (&sums)[2][N][THREADS / kWave], int turn, double (&sum)[N]) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
-  if constexpr (THREADS > kWave) {
-    const int wave = threadIdx.x / kWave;
-    if (lane_id() == 0) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) sums[turn][n][wave] = v[n];
+  for (int n = 0; n < N; ++n) {
+    const float s = wave_sum(v[n]);
+    if constexpr (THREADS > kWave) {
+      if (lane_id() == 0) sums[turn][n][threadIdx.x / kWave] = s;
+    } else {
+      sum[n] = (double)s;
     }
+  }
+  if constexpr (THREADS > kWave) {
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      v[n] = 0.0f;
+      sum[n] = 0.0;
 #pragma unroll
-      for (int w = 0; w < THREADS / kWave; ++w) v[n] += sums[turn][n][w];
+      for (int w = 0; w < THREADS / kWave; ++w) sum[n] += (double)sums[turn][n][w];
     }
   }
+}
+// m^-1/2 and what it is short of the exact value, from one step of Newton's in 64 bits: every value of a row would share its error.
+struct Inverse {
+  float root, rest;
+};
+__device__ __forceinline__ Inverse inverse_root(double m) {
+  const float r = 1.0f / sqrtf((float)m);
+  const float rest = r * (float)(0.5 * (1.0 - m * (double)r * (double)r));
+  return {r, fabsf(rest) < __builtin_inff() ? rest : 0.0f};   // none of 0 and of what is no number
 }
 
 // A vector of the weight of either type.
@@ -53,7 +64,7 @@ template <int THREADS>
 constexpr int norm_block() { return THREADS < 256 ? 256 : THREADS; }
 
 template <typename IN, typename SUM, int VEC, int THREADS>
-__global__ __launch_bounds__(norm_block<THREADS>()) void rms_norm_kernel(NormParams p) {
+__global__ __launch_bounds__(norm_block<THREADS>(), THREADS == 512 && VEC == 2 ? 6 : 1) void rms_norm_kernel(NormParams p) {
   constexpr int kRows = norm_block<THREADS>() / THREADS;   // of a workgroup
   __shared__ float sums[2][1][THREADS / kWave];
   const int tid = threadIdx.x % THREADS, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -63,31 +74,34 @@ __global__ __launch_bounds__(norm_block<THREADS>()) void rms_norm_kernel(NormPar
   float w[VEC][8];
 #pragma unroll
   for (int k = 0; k < VEC; ++k) load_weight(p.weight, p.weight_bf16, (k * THREADS + tid) * 8, p.C, w[k]);
+  const double per_C = 1.0 / (double)p.C;
   int turn = 0;
   for (int64_t row = (int64_t)blockIdx.x * kRows + (THREADS < 256 ? wave : 0); row < p.rows; row += (int64_t)gridDim.x * kRows) {
-    float v[VEC][8], sum[1] = {0.0f};
+    float v[VEC][8], squares[1] = {0.0f};
     const IN *x = (const IN *)p.x + row * p.ld;
+    Eight<IN> own[VEC];   // as they were loaded: half the registers of fp32
+    Eight<SUM> add[VEC];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) load_row(x, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C, v[k]);
+    for (int k = 0; k < VEC; ++k) own[k] = eight_of_row(x, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C);
     if (p.residual) {
       const SUM *r = (const SUM *)p.residual + row * p.residual_ld;
-      float add[VEC][8];
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) load_row(r, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C, add[k]);
+      for (int k = 0; k < VEC; ++k) add[k] = eight_of_row(r, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C);
+    }
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) {
+    for (int k = 0; k < VEC; ++k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] += add[k][i];
-        round_to((const SUM *)nullptr, v[k]);   // what is normed is the sum as it is kept, so that the way back sees the same
-      }
+      for (int i = 0; i < 8; ++i) v[k][i] = p.residual ? own[k].at(i) + add[k].at(i) : own[k].at(i);
+      if (p.residual) round_to((const SUM *)nullptr, v[k]);   // what is normed is the sum as it is kept, so that the way back sees the same
     }
 #pragma unroll
     for (int k = 0; k < VEC; ++k)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[0] = fmaf(v[k][i], v[k][i], sum[0]);
-    row_sums<THREADS>(sum, sums, turn);
+      for (int i = 0; i < 8; ++i) squares[0] = fmaf(v[k][i], v[k][i], squares[0]);
+    double sum[1];
+    row_sums<THREADS>(squares, sums, turn, sum);
     turn ^= 1;
-    const float by = 1.0f / sqrtf(sum[0] / (float)p.C + p.eps);
+    const Inverse by = inverse_root(sum[0] * per_C + (double)p.eps);
     // Stores come behind the barrier: outputs may take the place of the row's inputs, of which a thread at a row's end reads more
     // than it has.
     if (p.residual) {
@@ -99,7 +113,10 @@ __global__ __launch_bounds__(norm_block<THREADS>()) void rms_norm_kernel(NormPar
     for (int k = 0; k < VEC; ++k) {
       const int c = (k * THREADS + tid) * 8;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * by * w[k][i];
+      for (int i = 0; i < 8; ++i) {   // one rounding in the end, for three instructions more
+        const float normed = v[k][i] * by.root, rest = fmaf(v[k][i], by.rest, fmaf(v[k][i], by.root, -normed));
+        v[k][i] = fmaf(normed, w[k][i], rest * w[k][i]);
+      }
       if (p.y) {
         if (p.y_bf16) store_row((uint16_t *)p.y + row * p.C, c, p.C, v[k]);
         else store_row((float *)p.y + row * p.C, c, p.C, v[k]);
@@ -137,45 +154,44 @@ __global__ __launch_bounds__(norm_block<THREADS>()) void rms_norm_backward_kerne
 #pragma unroll
     for (int i = 0; i < 8; ++i) gw[k][i] = 0.0f;
   }
+  const double per_C = 1.0 / (double)p.C;
   int turn = 0;
   for (int64_t row = group; row < p.rows; row += p.groups) {
-    float s[VEC][8], g[VEC][8], t[VEC][8], sum[2] = {0.0f, 0.0f};
-    const IN *from_s = (const IN *)p.s + row * p.s_ld;
+    Eight<IN> s[VEC], t[VEC];   // as they were loaded: half the registers of fp32, for twice the waves
+    Eight<GY> g[VEC];
+    float parts[2] = {0.0f, 0.0f};
+    const IN *from_s = (const IN *)p.s + row * p.s_ld, *from_t = (const IN *)p.gtotal + row * p.gtotal_ld;
     const GY *from_g = (const GY *)p.gy + row * p.gy_ld;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
       const bool whole = (first_part + k * kStep) * 512 + 512 <= p.C;
-      load_row(from_s, (k * THREADS + tid) * 8, p.C, whole, s[k]);
-      load_row(from_g, (k * THREADS + tid) * 8, p.C, whole, g[k]);
-    }
-    if (p.gtotal) {
-      const IN *from_t = (const IN *)p.gtotal + row * p.gtotal_ld;
-#pragma unroll
-      for (int k = 0; k < VEC; ++k)
-        load_row(from_t, (k * THREADS + tid) * 8, p.C, (first_part + k * kStep) * 512 + 512 <= p.C, t[k]);
+      s[k] = eight_of_row(from_s, (k * THREADS + tid) * 8, p.C, whole);
+      g[k] = eight_of_row(from_g, (k * THREADS + tid) * 8, p.C, whole);
+      if (p.gtotal) t[k] = eight_of_row(from_t, (k * THREADS + tid) * 8, p.C, whole);
     }
 #pragma unroll
     for (int k = 0; k < VEC; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        sum[0] = fmaf(s[k][i], s[k][i], sum[0]);
-        sum[1] = fmaf(g[k][i] * w[k][i], s[k][i], sum[1]);
+        parts[0] = fmaf(s[k].at(i), s[k].at(i), parts[0]);
+        parts[1] = fmaf(g[k].at(i) * w[k][i], s[k].at(i), parts[1]);
       }
-    row_sums<THREADS>(sum, sums, turn);
+    double sum[2];
+    row_sums<THREADS>(parts, sums, turn, sum);
     turn ^= 1;
-    const float by = 1.0f / sqrtf(sum[0] / (float)p.C + p.eps), mean = by * by * (sum[1] / (float)p.C);
+    const float by = 1.0f / sqrtf((float)(sum[0] * per_C + (double)p.eps)), mean = by * by * (float)(sum[1] * per_C);
     IN *gx = (IN *)p.gx + row * p.gx_ld;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
+      s[k].forget();
+      g[k].forget();
       float out[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        gw[k][i] = fmaf(g[k][i], s[k][i] * by, gw[k][i]);
-        out[i] = by * (g[k][i] * w[k][i] - s[k][i] * mean);
-      }
-      if (p.gtotal) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] += t[k][i];
+        const float v = s[k].at(i), u = g[k].at(i);
+        gw[k][i] = fmaf(u, v * by, gw[k][i]);
+        out[i] = by * (u * w[k][i] - v * mean);
+        if (p.gtotal) out[i] += t[k].at(i);
       }
       store_row(gx, (k * THREADS + tid) * 8, p.C, out);
     }
@@ -218,10 +234,13 @@ static int norm_groups(int64_t rows, int32_t C) {
 template <typename LAUNCH>
 static void norm_shape(int64_t rows, int32_t C, LAUNCH launch) {
 #define HM_NORM_SHAPE(v, t) launch(std::integral_constant<int, v>(), std::integral_constant<int, t>())
+  const bool few = rows <= 256;
   if (C <= 512) HM_NORM_SHAPE(1, 64);
   else if (C <= 1024) HM_NORM_SHAPE(2, 64);
   else if (C <= 2048) HM_NORM_SHAPE(1, 256);
+  else if (C <= 4096 && few) HM_NORM_SHAPE(1, 512);
   else if (C <= 4096) HM_NORM_SHAPE(2, 256);
+  else if (C <= 8192 && few) HM_NORM_SHAPE(1, 1024);
   else if (C <= 8192) HM_NORM_SHAPE(2, 512);
   else if (C <= 16384) HM_NORM_SHAPE(4, 512);
   else HM_NORM_SHAPE(4, 1024);

@@ -453,35 +453,6 @@ struct WeightGradParams {
   int32_t *status;
 };
 
-// Eight elements as they were loaded.
-template <typename IN>
-struct Eight;
-template <>
-struct Eight<uint16_t> {
-  u32x4 w;
-  Eight() = default;
-  __device__ __forceinline__ explicit Eight(const uint16_t *p) : w(*(const u32x4_align2 *)p) {}
-  __device__ __forceinline__ float at(int i) const { return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
-  __device__ __forceinline__ float times(const Eight &v, float sum) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum = fmaf(bf16_hi(w[i]), bf16_hi(v.w[i]), fmaf(bf16_lo(w[i]), bf16_lo(v.w[i]), sum));
-    return sum;
-  }
-};
-template <>
-struct Eight<float> {
-  f32x4 a, b;
-  Eight() = default;
-  __device__ __forceinline__ explicit Eight(const float *p)
-      : a(*(const f32x4_align4 *)p), b(*(const f32x4_align4 *)(p + 4)) {}
-  __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i] : b[i - 4]; }
-  __device__ __forceinline__ float times(const Eight &v, float sum) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum = fmaf(b[i], v.b[i], fmaf(a[i], v.a[i], sum));
-    return sum;
-  }
-};
-
 // A wave takes a part of a token's row and SLOTS of its slots at a time: its gradient's row once, the slots' rows
 // beside it, all loads of 512 elements on their way together.  Where a row is split, the parts' sums meet in LDS.  What
 // bounds it is memory, (K + 1) rows a token: 8,192 tokens, K = 8, 7,168 bf16 180 us, 5.9 TB/s; few tokens wait for one
