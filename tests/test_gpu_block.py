@@ -1,0 +1,144 @@
+"""The example layer with a norm in front, the activation's calls inside and the way for a few tokens, against 64 bits without
+quantising, as they are used together."""
+import pytest
+import torch
+
+from paper_2508_09591_amd import binding as B
+from paper_2508_09591_amd import layer as L
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+
+
+def inputs(T, H, seed, kept=None):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    r = lambda: torch.randn((T, H), generator=g, device="cuda")
+    return r().to(BF16), r().to(BF16), None if kept is None else (2 * r()).to(kept), None if kept is None else r().to(kept)
+
+
+def reference(layer, x, residual, gout, gtotal, ids):
+    """Output, the sum that is kept, and the gradients by torch in 64 bits, with the choice that was made."""
+    leaf = lambda t: t.detach().double().cpu().requires_grad_()
+    x, gate, w13, w2, norm = (leaf(t) for t in (x, layer.gate, layer.w13, layer.w2, layer.norm))
+    total = x if residual is None else x + residual.double().cpu()
+    y = total * torch.rsqrt(total.square().mean(dim=1, keepdim=True) + layer.eps) * norm
+    ids = ids.long().cpu()
+    score = torch.softmax(y @ gate.t(), dim=1)
+    w = torch.where(ids >= 0, score.gather(1, ids.clamp(min=0)), 0.0)
+    w = w / w.sum(dim=1, keepdim=True)
+    out = torch.zeros_like(x)
+    for e in range(layer.E):
+        t, k = (ids == e).nonzero(as_tuple=True)
+        if len(t):
+            h = y[t] @ w13[e].t()
+            a = torch.nn.functional.silu(h[:, :layer.F]) * h[:, layer.F:]
+            out = out.index_add(0, t, w[t, k][:, None] * (a @ w2[e].t()))
+    loss = (out * gout.double().cpu()).sum()
+    if gtotal is not None:
+        loss = loss + (total * gtotal.double().cpu()).sum()
+    loss.backward()
+    return out.detach(), total.detach(), (x.grad, gate.grad, w13.grad, w2.grad, norm.grad)
+
+
+def far(a, b):
+    return float((a.double().cpu() - b).norm() / b.norm())
+
+
+@pytest.mark.parametrize("T,E,K,H,F,kept", [(1, 8, 2, 512, 128, BF16), (200, 8, 2, 512, 320, torch.float32), (157, 16, 4, 1024, 200, BF16),
+                                            (64, 12, 3, 512, 136, None)])
+def test_norm_layer_and_gradients(T, E, K, H, F, kept):
+    layer = L.make_layer(E, K, H, F, seed=T, norm=True)
+    x, gout, residual, gtotal = inputs(T, H, T + 1, kept)
+    out = layer.forward(x, residual)
+    grads = layer.backward(gout, gtotal)
+    want, total, want_grads = reference(layer, x, residual, gout, gtotal, layer.ids)
+    if kept is not None:
+        assert layer.total.dtype == kept and far(layer.total, total) <= 2 ** -8
+    # e4m3 values are off by 2^-5.5 of themselves on average; two a product, up to three products in a row, with room (as the layer's
+    # own test has it); the router's gradient is a small difference of large terms, so it and what it adds to the others has more
+    assert far(out, want) <= 0.12
+    for name, a, b in zip(("x", "w13", "w2", "norm"), (grads[0], *grads[2:]), (want_grads[0], *want_grads[2:])):
+        assert torch.isfinite(a).all(), name
+        assert far(a, b) <= 0.12, (name, far(a, b))
+    assert torch.isfinite(grads[1]).all()
+
+
+@pytest.mark.parametrize("T,E,K,H,F,kept", [(1, 16, 4, 512, 256, BF16), (16, 8, 2, 1024, 320, torch.float32), (50, 32, 4, 512, 200, None)])
+def test_few_tokens(T, E, K, H, F, kept):
+    layer = L.make_layer(E, K, H, F, seed=T, norm=True)
+    x, gout, residual, _ = inputs(T, H, T + 1, kept)
+    whole = layer.forward(x, residual)
+    ids = layer.ids
+    few = layer.few(x, residual)
+    want = reference(layer, x, residual, gout, None, ids)[0]
+    # the weights alone are in 8 bits: 2^-5.5 a product on average, two of them, silu amplifying less than twofold
+    assert far(few, want) <= 3 * 2 ** -5.5
+    assert far(whole, want) <= 0.12
+    assert far(few, want) < far(whole, want) or T == 1
+
+
+def test_few_tokens_where_experts_are_gone():
+    layer = L.make_layer(8, 4, 512, 64, norm=True)
+    layer.gone = torch.arange(8, device="cuda") >= 3
+    x, gout, residual, _ = inputs(20, 512, 3, BF16)
+    layer.forward(x, residual)
+    ids = layer.ids
+    assert (ids >= 0).sum() == 60
+    assert far(layer.few(x, residual), reference(layer, x, residual, gout, None, ids)[0]) <= 3 * 2 ** -5.5
+
+
+def test_a_decoding_step_in_a_graph():
+    """Norm, router's product, the layer: captured once, replayed for other tokens, with eager steps between."""
+    layer = L.make_layer(16, 4, 512, 256, seed=9, norm=True)
+    x, _, residual, _ = inputs(4, 512, 1, BF16)
+    layer.few(x, residual)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = layer.few(x, residual)
+        kept = layer.total
+    for n in range(4):
+        other, _, residual2, _ = inputs(4, 512, 10 + n, BF16)
+        x.copy_(other), residual.copy_(residual2)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = layer.few(x, residual)
+        assert torch.equal(out, eager) and torch.equal(kept, layer.total)
+        torch.cuda.synchronize()
+
+
+def test_a_training_step_in_a_graph():
+    """Forward and backward with the norm, captured while eager results of the same tensors live: the same gradients each time."""
+    layer = L.make_layer(8, 2, 512, 128, seed=2, norm=True)
+    x, gout, residual, gtotal = inputs(130, 512, 1, BF16)
+    step = lambda: (layer.forward(x, residual), *layer.backward(gout, gtotal))
+    want = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        for t in got:
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        again = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(again, want))
+
+
+def test_a_residual_needs_a_norm():
+    layer = L.make_layer(8, 2, 512, 64)
+    x, _, residual, _ = inputs(3, 512, 1, BF16)
+    with pytest.raises(ValueError):
+        layer.forward(x, residual)
+    with pytest.raises(B.HierMoEError):
+        layer.few(torch.zeros((65, 512), dtype=BF16, device="cuda"))
