@@ -4,7 +4,7 @@
 // operands of products of 16 x 16 x 32 in 16 bits, as for the products of few rows.  Values in 8 bits times their block's power of
 // two are exact in bf16, x is bf16; activations go between the two products as sums of two or three bf16 numbers, so that what
 // they lose is far below the output's rounding (2^-17 of each, 2^-25 for fp32 outputs).
-#include "hm_block8.h"
+#include "hm_choice.h"
 
 namespace hm {
 
@@ -16,8 +16,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 struct FewParams {
   const uint16_t *x;
   int64_t ld;
-  const int32_t *ids;      // [T,K]
-  const float *weights;
+  int32_t *ids;            // [T,K]
+  float *weights;
   int32_t T, K, first, experts, H, F;
   uint32_t per_K;          // ceil(2^20 / K)
   const uint8_t *w13, *s13, *w2, *s2;
@@ -33,10 +33,12 @@ __device__ __forceinline__ int expert_here(const FewParams &p, int slot) {   // 
   return (unsigned)e < (unsigned)p.experts ? e : -1;
 }
 // Writes the slots, ascending, to `list`, one of the wave's own: at most one of a token's.  0: nothing to do.  By whole waves.
-__device__ __forceinline__ int slots_of_share(const FewParams &p, int share, int &e, int *list) {
+// `expert_of` says what expert_here does.
+template <typename EXPERT>
+__device__ __forceinline__ int slots_of_share(const FewParams &p, int share, EXPERT expert_of, int &e, int *list) {
   const int lane = lane_id(), slots = p.T * p.K;
   const bool by_slot = slots < p.experts;
-  e = by_slot ? expert_here(p, share) : share;
+  e = by_slot ? expert_of(share) : share;
   int n = 0;
   auto take = [&](int s, int expert) {
     const uint64_t all = __ballot(s < slots && expert == e);
@@ -45,13 +47,13 @@ __device__ __forceinline__ int slots_of_share(const FewParams &p, int share, int
     n += __popcll(all);
   };
   if (slots <= kWave) {
-    take(lane, expert_here(p, min(lane, slots - 1)));
+    take(lane, expert_of(min(lane, slots - 1)));
   } else {
     constexpr int kTogether = 4;   // loads on their way
     for (int s0 = 0; s0 < slots; s0 += kTogether * kWave) {
       int expert[kTogether];
 #pragma unroll
-      for (int i = 0; i < kTogether; ++i) expert[i] = expert_here(p, min(s0 + i * kWave + lane, slots - 1));
+      for (int i = 0; i < kTogether; ++i) expert[i] = expert_of(min(s0 + i * kWave + lane, slots - 1));
 #pragma unroll
       for (int i = 0; i < kTogether; ++i) take(s0 + i * kWave + lane, expert[i]);
     }
@@ -113,16 +115,38 @@ __device__ __forceinline__ Wide zero_wide() {
 // 32 (l / 16) to 32 (l / 16) + 31 of a step.
 constexpr int kUpWaves = 4;
 
-template <int GROUPS, int PLANES>
-__global__ __launch_bounds__(kUpWaves * kWave) void few_up_kernel(FewParams p) {
+//
+// N: with up to four tokens every workgroup makes the choice by itself, lists of N, 16 lanes a token in its first wave, which takes it
+// less time than another launch would; the first one writes it down.  0: it has been made.
+constexpr int kChoosingTokens = kWave / 16;
+template <typename LOGIT, int N, int GROUPS, int PLANES>
+__global__ __launch_bounds__(kUpWaves * kWave) void few_up_kernel(FewParams p, RouteParams route, int lanes_per_group, int run) {
   __shared__ int lists[kUpWaves][kMostFewTokens];
   __shared__ f32x4 sums[kUpWaves][2][kWave];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int width_a = (int)row8_bytes(p.F), slots = p.T * p.K;
   const int *list = lists[wave];
   const int share = (int)blockIdx.y, f0 = (int)blockIdx.x * 16;
-  int e;
-  const int all = slots_of_share(p, share, e, lists[wave]);
+  int e, all;
+  if constexpr (N > 0) {
+    __shared__ int chosen[kWave];
+    if (wave == 0) {
+      const int t = lane >> 4, k = lane & 15;
+      const Choice<16, N> c = choose_by_lists<LOGIT, 16, N>(route, t, lanes_per_group, run);
+      if (t < p.T && k < p.K) {
+        const int slot = t * p.K + k, here = c.id[0] - p.first;
+        chosen[slot] = (unsigned)here < (unsigned)p.experts ? here : -1;
+        if (blockIdx.x == 0 && blockIdx.y == 0) {
+          p.ids[slot] = c.id[0];
+          p.weights[slot] = c.weight[0];
+        }
+      }
+    }
+    __syncthreads();
+    all = slots_of_share(p, share, [&](int slot) { return chosen[slot]; }, e, lists[wave]);
+  } else {
+    all = slots_of_share(p, share, [&](int slot) { return expert_here(p, slot); }, e, lists[wave]);
+  }
   if (all == 0) return;   // the same for the workgroup
   const int row = lane & 15, part = (lane >> 4) * 32, steps = (int)blocks8(p.H);
   const int64_t pitch = row8_bytes(p.H), scale_pitch = scale8_bytes(p.H);
@@ -331,7 +355,7 @@ __global__ __launch_bounds__(kUpWaves * kWave) void few_down_slots_kernel(FewPar
   const int *list = lists[wave];
   const int share = (int)blockIdx.y, h0 = (int)blockIdx.x * 16 * FRAGS;
   int e;
-  const int n = slots_of_share(p, share, e, lists[wave]);
+  const int n = slots_of_share(p, share, [&](int slot) { return expert_here(p, slot); }, e, lists[wave]);
   if (n == 0) return;   // the same for the workgroup
   const int row = lane & 15, part = (lane >> 4) * 32, steps = (int)blocks8(p.F);
   const int64_t pitch = row8_bytes(p.F), scale_pitch = scale8_bytes(p.F);
@@ -418,19 +442,32 @@ __global__ __launch_bounds__(256) void few_sum_kernel(FewParams p) {
 
 static int few_planes(hm_dtype out) { return out == HM_F32 ? 3 : 2; }
 
-template <int GROUPS, int PLANES>
-static void launch_few_up(const FewParams &p, int64_t shares, hipStream_t stream) {
-  hipLaunchKernelGGL((few_up_kernel<GROUPS, PLANES>), dim3((unsigned)(row8_bytes(p.F) / 16), (unsigned)shares),
-                     dim3(kUpWaves * kWave), 0, stream, p);
+template <typename LOGIT, int N, int GROUPS, int PLANES>
+static void launch_few_up(const FewParams &p, const RouteParams &route, int64_t shares, hipStream_t stream) {
+  const int lanes_per_group = 16 / route.r.groups, run = (route.r.E / route.r.groups + lanes_per_group - 1) / lanes_per_group;
+  hipLaunchKernelGGL((few_up_kernel<LOGIT, N, GROUPS, PLANES>), dim3((unsigned)(row8_bytes(p.F) / 16), (unsigned)shares),
+                     dim3(kUpWaves * kWave), 0, stream, p, route, lanes_per_group, run);
+}
+// The choice by the workgroups of the first product, as far as it goes.
+static bool chooses_itself(const RouteParams &route) {
+  return route.T <= kChoosingTokens && list_lanes(route.r, route.bias != nullptr, route.T) == 16;
+}
+template <typename LOGIT, int PLANES>
+static void launch_choosing_up(const FewParams &p, const RouteParams &route, int64_t shares, hipStream_t stream) {
+  if (p.K <= 8) launch_few_up<LOGIT, 8, 1, PLANES>(p, route, shares, stream);
+  else launch_few_up<LOGIT, 16, 1, PLANES>(p, route, shares, stream);
 }
 template <int PLANES, typename OUT>
-static hm_status launch_few(const FewParams &p, int64_t shares, int E, hipStream_t stream) {
-  if (p.T <= 16 || p.T * p.K <= 6 * E) {
-    launch_few_up<1, PLANES>(p, shares, stream);
+static hm_status launch_few(const FewParams &p, const RouteParams &route, hm_dtype logits, int64_t shares, hipStream_t stream) {
+  if (chooses_itself(route)) {
+    if (logits == HM_BF16) launch_choosing_up<uint16_t, PLANES>(p, route, shares, stream);
+    else launch_choosing_up<float, PLANES>(p, route, shares, stream);
+  } else if (p.T <= 16 || p.T * p.K <= 6 * route.r.E) {
+    launch_few_up<float, 0, 1, PLANES>(p, route, shares, stream);
   } else if (p.T <= 32) {
-    launch_few_up<2, PLANES>(p, shares, stream);
+    launch_few_up<float, 0, 2, PLANES>(p, route, shares, stream);
   } else {
-    launch_few_up<4, PLANES>(p, shares, stream);
+    launch_few_up<float, 0, 4, PLANES>(p, route, shares, stream);
   }
   const hm_status up = hm_launch_status();
   if (up != HM_OK) return up;
@@ -476,12 +513,21 @@ extern "C" hm_status hm_layer_few(const void *x, int64_t ld, const void *logits,
   if (T > 0 && (!x || !w13 || !w13_scale || !w2 || !w2_scale || !out)) return HM_ERR_NULL;
   if (T > 0 && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < hm_layer_few_workspace_bytes(T, router->K, H, F)))
     return HM_ERR_WORKSPACE;
-  const hm_status routed = hm_route(logits, logits_dtype, logits_ld, bias, T, router, topk_ids, topk_weights, hip_stream);
-  if (routed != HM_OK || T == 0) return routed;
+  // what hm_route looks at, which makes the choice for more than a few tokens
+  const RouteParams route = {logits, logits_ld, bias, T, *router, topk_ids, topk_weights};
+  const hm_status fits = check_router(router);
+  if (fits != HM_OK) return fits;
+  if (!dtype_known(logits_dtype) || (logits_ld < router->E && T > 1)) return HM_ERR_SHAPE;
+  if (T == 0) return HM_OK;
+  if (!logits || !topk_ids || !topk_weights) return HM_ERR_NULL;
+  if (!chooses_itself(route)) {
+    const hm_status routed = hm_route(logits, logits_dtype, logits_ld, bias, T, router, topk_ids, topk_weights, hip_stream);
+    if (routed != HM_OK) return routed;
+  }
   const FewParams p = {(const uint16_t *)x, ld, topk_ids, topk_weights, T, router->K, first, experts, H, F,
-                       ((1u << 20) + router->K - 1) / router->K, w13, w13_scale, w2, w2_scale,
-                       (uint16_t *)workspace, (float *)((char *)workspace + (int64_t)T * router->K * 6 * row8_bytes(F)), out};
+                       ((1u << 20) + router->K - 1) / router->K, w13, w13_scale, w2, w2_scale, (uint16_t *)workspace,
+                       (float *)((char *)workspace + (int64_t)T * router->K * 6 * row8_bytes(F)), out};
   const hipStream_t stream = (hipStream_t)hip_stream;
-  if (out_dtype == HM_F32) return launch_few<3, float>(p, hit, router->E, stream);
-  return launch_few<2, uint16_t>(p, hit, router->E, stream);
+  if (out_dtype == HM_F32) return launch_few<3, float>(p, route, logits_dtype, hit, stream);
+  return launch_few<2, uint16_t>(p, route, logits_dtype, hit, stream);
 }
