@@ -457,6 +457,19 @@ static void launch_choosing_up(const FewParams &p, const RouteParams &route, int
   if (p.K <= 8) launch_few_up<LOGIT, 8, 1, PLANES>(p, route, shares, stream);
   else launch_few_up<LOGIT, 16, 1, PLANES>(p, route, shares, stream);
 }
+// Dynamic LDS that few_down_kernel may have: asked for once, as it is more than a kernel gets by default.  It takes in the eight
+// slots of one token of 2,048 columns, and leaves room for two workgroups a CU.
+constexpr int kMostStaged = 66 * 1024;
+template <int PLANES, typename OUT>
+static int64_t staged_limit() {
+  static const bool granted = [] {
+    const hipError_t e = hipFuncSetAttribute((const void *)few_down_kernel<PLANES, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             kMostStaged);
+    if (e != hipSuccess) (void)hipGetLastError();   // not sticky: do not let it fail the next launch check
+    return e == hipSuccess;
+  }();
+  return granted ? kMostStaged : 65536 - 4096;   // beside what it has anyway
+}
 template <int PLANES, typename OUT>
 static hm_status launch_few(const FewParams &p, const RouteParams &route, hm_dtype logits, int64_t shares, hipStream_t stream) {
   if (chooses_itself(route)) {
@@ -472,7 +485,7 @@ static hm_status launch_few(const FewParams &p, const RouteParams &route, hm_dty
   const hm_status up = hm_launch_status();
   if (up != HM_OK) return up;
   const int64_t slots = (int64_t)p.T * p.K, staged = PLANES * slots * (row8_bytes(p.F) + 8) * 2, sums = (int64_t)kDownWaves * p.T * 16 * 4;
-  if (slots <= kWave && staged + sums <= 66 * 1024) {
+  if (slots <= kWave && staged + sums <= staged_limit<PLANES, OUT>()) {
     const int columns = p.H < 4096 ? 8 : 16;
     hipLaunchKernelGGL((few_down_kernel<PLANES, OUT>), dim3((unsigned)((p.H + columns - 1) / columns)), dim3(kDownWaves * kWave),
                        (size_t)(sums + staged), stream, p, columns);
