@@ -147,17 +147,14 @@ __device__ __forceinline__ void load_logits(const IN *p, int n, float (&v)[N]) {
 // 8), against 4 bytes read.  us: 65,536 tokens, 256 experts, logistic with bias and groups 30 (2.4 TB/s), softmax 24,
 // bf16 18; one token 5.3. 8 lanes a token from 16,384 tokens on: 65,536 x 64 8.4 and, with 16 lanes, 14.7; 8,192 x 256
 // 8.3 and 6.9.
-template <int L, int N>
-struct Choice {
-  static constexpr int kMine = N > L ? N / L : 1;
-  int id[kMine];   // of slots sub, sub + L, ... ; -1: none
-  float weight[kMine];
-};
-template <typename IN, int L, int N>
-__device__ __forceinline__ Choice<L, N> choose_by_lists(const RouteParams &p, int64_t t, int lanes_per_group, int run) {
+// store(k, expert, weight) is called for each slot of a token that is there, by the lane that holds it.
+template <typename IN, int L, int N, typename STORE>
+__device__ __forceinline__ void choose_by_lists(const RouteParams &p, int64_t t, int lanes_per_group, int run,
+                                                STORE store) {
   const int sub = (int)threadIdx.x & (L - 1);
+  const bool there = t < p.T;
   const int E = p.r.E, K = p.r.K, per = E / p.r.groups, group = sub / lanes_per_group;
-  const IN *x = (const IN *)p.logits + min(t, (int64_t)p.T - 1) * p.ld;
+  const IN *x = (const IN *)p.logits + (there ? t : p.T - 1) * p.ld;
   const bool softmax = p.r.score == HM_SCORE_SOFTMAX;   // then there is no bias
   const int e = group * per + (sub - group * lanes_per_group) * run;
   const int end = min(e + run, (group + 1) * per);
@@ -171,6 +168,7 @@ __device__ __forceinline__ Choice<L, N> choose_by_lists(const RouteParams &p, in
     float next[N], next_b[N];   // on their way while this batch is sorted
     load_logits<N>(x + first + N, end - first - N, next);
     if (p.bias) load_logits<N>(p.bias + first + N, end - first - N, next_b);
+    __builtin_amdgcn_sched_barrier(0);   // else the bias comes behind the wait for the logits: 65,536 x 256 30 -> 34 us
     double batch[N];
     if (p.bias) {
 #pragma unroll
@@ -223,9 +221,9 @@ __device__ __forceinline__ Choice<L, N> choose_by_lists(const RouteParams &p, in
     merge(list, other);
   });
   // Slot k is lane k's; with fewer lanes than slots a lane has several.
-  constexpr int kMine = Choice<L, N>::kMine;
+  constexpr int kMine = N > L ? N / L : 1;
   float score[kMine], total = 0.0f;
-  Choice<L, N> c;
+  int id[kMine];
 #pragma unroll
   for (int m = 0; m < kMine; ++m) {
     const int k = sub + m * L;
@@ -234,8 +232,8 @@ __device__ __forceinline__ Choice<L, N> choose_by_lists(const RouteParams &p, in
     for (int i = m * L; i < min(N, (m + 1) * L); ++i) key = i == k ? list[i] : key;
     const float choice = choice_of(key);
     const bool chosen = k < K && choice != kNone();
-    c.id[m] = chosen ? expert_of(key) : -1;
-    const float logit = p.bias ? (chosen ? usable(logit_at(x, c.id[m])) : kNone()) : choice;
+    id[m] = chosen ? expert_of(key) : -1;
+    const float logit = p.bias ? (chosen ? usable(logit_at(x, id[m])) : kNone()) : choice;
     score[m] = !chosen ? 0.0f : softmax ? expf(logit - choice_of(list[0])) : logistic(logit);
     total += score[m];
   }
@@ -261,8 +259,10 @@ __device__ __forceinline__ Choice<L, N> choose_by_lists(const RouteParams &p, in
     for (int m = 0; m < kMine; ++m) score[m] *= shift;
   }
 #pragma unroll
-  for (int m = 0; m < kMine; ++m) c.weight[m] = by > 0.0f ? score[m] / by * p.r.scale : 0.0f;
-  return c;
+  for (int m = 0; m < kMine; ++m) {
+    const int k = sub + m * L;
+    if (there && k < K) store(k, id[m], by > 0.0f ? score[m] / by * p.r.scale : 0.0f);
+  }
 }
 
 constexpr int kMostExperts = 4096, kMostSlots = 64;

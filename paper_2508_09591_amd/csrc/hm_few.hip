@@ -131,16 +131,15 @@ __global__ __launch_bounds__(kUpWaves * kWave) void few_up_kernel(FewParams p, R
   if constexpr (N > 0) {
     __shared__ int chosen[kWave];
     if (wave == 0) {
-      const int t = lane >> 4, k = lane & 15;
-      const Choice<16, N> c = choose_by_lists<LOGIT, 16, N>(route, t, lanes_per_group, run);
-      if (t < p.T && k < p.K) {
-        const int slot = t * p.K + k, here = c.id[0] - p.first;
+      const int t = lane >> 4;
+      choose_by_lists<LOGIT, 16, N>(route, t, lanes_per_group, run, [&](int k, int expert, float weight) {
+        const int slot = t * p.K + k, here = expert - p.first;
         chosen[slot] = (unsigned)here < (unsigned)p.experts ? here : -1;
         if (blockIdx.x == 0 && blockIdx.y == 0) {
-          p.ids[slot] = c.id[0];
-          p.weights[slot] = c.weight[0];
+          p.ids[slot] = expert;
+          p.weights[slot] = weight;
         }
-      }
+      });
     }
     __syncthreads();
     all = slots_of_share(p, share, [&](int slot) { return chosen[slot]; }, e, lists[wave]);

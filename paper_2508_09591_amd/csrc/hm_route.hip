@@ -110,15 +110,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteParams p) {
 template <typename IN, int L, int N>
 __global__ __launch_bounds__(kRouteThreads) void route_lists_kernel(RouteParams p, int lanes_per_group, int run) {
   const int64_t t = (int64_t)blockIdx.x * (kRouteThreads / L) + threadIdx.x / L;
-  const Choice<L, N> c = choose_by_lists<IN, L, N>(p, t, lanes_per_group, run);   // beyond the last token its choice once more
-#pragma unroll
-  for (int m = 0; m < Choice<L, N>::kMine; ++m) {
-    const int k = ((int)threadIdx.x & (L - 1)) + m * L;
-    if (t < p.T && k < p.r.K) {
-      p.ids[t * p.r.K + k] = c.id[m];
-      p.weights[t * p.r.K + k] = c.weight[m];
-    }
-  }
+  choose_by_lists<IN, L, N>(p, t, lanes_per_group, run, [&](int k, int expert, float weight) {
+    p.ids[t * p.r.K + k] = expert;
+    p.weights[t * p.r.K + k] = weight;
+  });
 }
 
 struct RouteBackParams {
