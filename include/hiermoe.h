@@ -562,8 +562,8 @@ hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_scale, const 
  *     s = x + residual,   y = s / sqrt(mean(s^2) + eps) * weight      per row of C values
  * residual [rows,C] of total_dtype or NULL; with it the sum, rounded to that type, is kept in total (not NULL then), and
  * what is normed is the sum as it is kept.  y [rows,C] of y_dtype, and q, scale: the same values in 8 bits in the layout
- * `rows` above, rounded once from fp32; either may be NULL, not both.  Sums are fp32: a row whose squares add up to more
- * than 3.4e38 gives zeros, one with a NaN gives NaN.  x, residual and total have rows ld, residual_ld, total_ld elements
+ * `rows` above, rounded once from fp32; either may be NULL, not both.  Squares are added in fp32: a row whose squares add up
+ * to more than 3.4e38 gives zeros, one with a NaN gives NaN, and with eps 0 values below 1e-16 may count for too little.  x, residual and total have rows ld, residual_ld, total_ld elements
  * apart; total may be x or residual itself (the same elements in the same place), y may be x.
  * Limits: C <= 32768, rows <= 2^31 - 1, eps >= 0.
  */
@@ -599,10 +599,10 @@ hm_status hm_rms_norm_backward(const void *gy, hm_dtype gy_dtype, int64_t gy_ld,
  * in up to four forms, each NULL or not, one at least not: values gh [rows,2F] of gh_dtype; rows in 8 bits q, scale
  * (C = 2 F), for the rows' gradient; columns in 8 bits q_columns, scale_columns (C = 2 F), and those of a itself, a_columns,
  * a_scale (C = F), for the gradients of the two weights.  Columns need offsets; with offsets only rows of segments are
- * written, and of columns the blocks that segments need.  Outputs lie apart from each other and from the inputs.
+ * written, and of columns the blocks that segments need.  Outputs of both calls lie apart from each other and from the inputs.
  * Limits: F <= 2^20 (2^19 on the way back), segments <= 1024, rows <= 2^31 - 1 (with offsets - 128 * segments),
- * rows * ceil(F / 512) <= 2^25 (F: 2 F on the way back), columns: (rows / 128 + segments) * ceil(F / 128) <= 2^22 - 8;
- * beyond HM_ERR_SHAPE.  Offsets that descend or lie outside [0,rows] are data errors as above.
+ * rows * ceil(F / 512) <= 2^25 (F: 2 F on the way back), columns: (rows / 128 + segments) * ceil(F / 128) <= 2^22 - 8 and
+ * ld, ga_ld <= 2^22; beyond HM_ERR_SHAPE.  Offsets that descend or lie outside [0,rows] are data errors as above.
  */
 hm_status hm_gated(const void *h, hm_dtype dtype, int64_t ld, const int32_t *offsets, int32_t segments, int64_t rows,
                    int32_t F, void *a, hm_dtype a_dtype, uint8_t *q, uint8_t *scale, void *hip_stream);

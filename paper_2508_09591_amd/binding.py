@@ -886,6 +886,14 @@ def _pair8(q, scale, shape, scale_shape, name: str):
     return (None, None) if q is None else (_codes(q, shape, name), _scales(scale, scale_shape, "the scales of " + name))
 
 
+def _scratch_for(stream, alloc):
+    """A workspace that lives for one call on the given stream: of that stream's memory, so that nobody gets it before the call is done."""
+    if stream is None:
+        return alloc()
+    with torch.cuda.stream(stream):
+        return alloc()
+
+
 def alloc_rms_norm_workspace(rows: int, C: int, device="cuda") -> torch.Tensor:
     """Scratch for hm_rms_norm_backward."""
     return torch.empty(int(lib().hm_rms_norm_backward_workspace_bytes(rows, C)), dtype=torch.uint8, device=device)
@@ -941,7 +949,7 @@ def hm_rms_norm_backward(gy: torch.Tensor, s: torch.Tensor, weight: torch.Tensor
         if other is not None and other.dtype != s.dtype:
             raise TypeError("%s must be %s as s is, got %s" % (name, s.dtype, other.dtype))
     if workspace is None:
-        workspace = alloc_rms_norm_workspace(rows, C, device=s.device)
+        workspace = _scratch_for(stream, lambda: alloc_rms_norm_workspace(rows, C, device=s.device))
     rc = lib().hm_rms_norm_backward(g, _floats(gy, "gy"), g_ld, at, _floats(s, "s"), ld,
                                     _dev(_shaped(weight, (C,), "weight"), weight.dtype, "weight"), _floats(weight, "weight"), float(eps), rows, C,
                                     t, t_ld, to, to_ld, _dev(_shaped(gweight, (C,), "gweight"), torch.float32, "gweight"),
@@ -1036,7 +1044,7 @@ def hm_layer_few(x: torch.Tensor, logits: torch.Tensor, router: Router, w13: tor
     if bias is not None:
         _shaped(bias, (router.E,), "bias")
     if workspace is None:
-        workspace = alloc_layer_few_workspace(T, router, H, F, device=x.device)
+        workspace = _scratch_for(stream, lambda: alloc_layer_few_workspace(T, router, H, F, device=x.device))
     rc = lib().hm_layer_few(at, ld, from_logits, _floats(logits, "logits"), logits_ld, _dev(bias, torch.float32, "bias"), T, router.ref(),
                             _codes(w13, (experts, wide, row8_bytes(H)), "w13"),
                             _scales(w13_scale, (experts, (wide + 127) // 128, scale8_bytes(H)), "w13_scale"),

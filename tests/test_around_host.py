@@ -76,7 +76,8 @@ def test_the_activation_checks_its_arguments():
     refused(call, B.HM_ERR_SHAPE, dict(F=(1 << 20) + 1, ld=1 << 23), dict(adtype=4), dict(a=P(0x1001)), dict(off=None, rows=(1 << 25) + 1, F=512, ld=1024))
     refused(back, B.HM_ERR_SHAPE, dict(F=(1 << 19) + 1, ld=1 << 23, gld=1 << 23), dict(gld=31), dict(ga=P(0x1001)), dict(ghdtype=4), dict(gh=P(0x1001)),
             dict(qc=P(0x1004)), dict(sc=P(0x1001)), dict(ac=P(0x1008)), dict(asc=P(0x1002)),
-            dict(off=None, rows=(1 << 25) + 1, F=256, ld=512, gld=256, qc=None, sc=None, ac=None, asc=None))
+            dict(off=None, rows=(1 << 25) + 1, F=256, ld=512, gld=256, qc=None, sc=None, ac=None, asc=None),
+            dict(ld=(1 << 22) + 1), dict(gld=(1 << 22) + 1))   # with columns
 
 
 @fake_pointers

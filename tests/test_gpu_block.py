@@ -142,3 +142,73 @@ def test_a_residual_needs_a_norm():
         layer.forward(x, residual)
     with pytest.raises(B.HierMoEError):
         layer.few(torch.zeros((65, 512), dtype=BF16, device="cuda"))
+
+
+class _Recorder:
+    """The native half with a note of each call: its name and whether it was taken."""
+    def __init__(self, native):
+        self.native, self.calls = native, []
+
+    def __getattr__(self, name):
+        def call(*args):
+            rc = getattr(self.native, name)(*args)
+            self.calls.append((name, rc is not None))
+            return rc
+        return call
+
+
+def every_call(T, E, K, H, F, workspaces=True):
+    """[(name, call(stream), its outputs)] of the calls around the products, on tensors of their own."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    r = lambda *shape, dtype=BF16: torch.randn(shape, generator=g, device="cuda").to(dtype)
+    empty = lambda *shape, dtype=BF16: torch.empty(shape, dtype=dtype, device="cuda")
+    x, past, weight, router = r(T, H), r(T, H), r(H, dtype=torch.float32), B.Router(E, K)
+    total, y, y8, gx, gw = empty(T, H), empty(T, H), B.alloc_rows8(T, H), empty(T, H), empty(H, dtype=torch.float32)
+    h, ga, a, offsets = r(T, 2 * F), r(T, F), empty(T, F), torch.tensor([0, T // 2, T], dtype=torch.int32, device="cuda")
+    back8 = (*B.alloc_rows8(T, 2 * F), *(t.zero_() for t in (*B.alloc_columns8(T, 2, 2 * F), *B.alloc_columns8(T, 2, F))))
+    w13 = B.hm_quantize_weights(r(E, 2 * F, H), *B.alloc_weights8(E, 2 * F, H))
+    w2 = B.hm_quantize_weights(r(E, H, F), *B.alloc_weights8(E, H, F))
+    logits, ids, w, out = r(T, E, dtype=torch.float32), empty(T, K, dtype=torch.int32), empty(T, K, dtype=torch.float32), empty(T, H)
+    ws = (B.alloc_rms_norm_workspace(T, H), B.alloc_layer_few_workspace(T, router, H, F)) if workspaces else (None, None)
+    return [("rms_norm", lambda s: B.hm_rms_norm(x, weight, 1e-6, y, *y8, past, total, stream=s), (total, y, *y8)),
+            ("rms_norm_backward", lambda s: B.hm_rms_norm_backward(past, x, weight, 1e-6, gx, gw, None, ws[0], stream=s), (gx, gw)),
+            ("gated", lambda s: B.hm_gated(h, a, None, None, offsets, stream=s), (a,)),
+            ("gated_backward", lambda s: B.hm_gated_backward(h, ga, offsets, None, *back8, stream=s), back8),
+            ("layer_few", lambda s: B.hm_layer_few(x, logits, router, *w13, *w2, ids, w, out, ws[1], stream=s), (ids, w, out))]
+
+
+def test_ordinary_calls_are_the_native_halfs(monkeypatch):
+    calls = every_call(20, 8, 2, 256, 128)
+    rec = _Recorder(B._native)
+    monkeypatch.setattr(B, "_native", rec)
+    for _, call, _ in calls:
+        call(None)
+    torch.cuda.synchronize()
+    assert rec.calls == [(name, True) for name, _, _ in calls]
+    rec.calls.clear()
+    for _, call, _ in calls:
+        call(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert rec.calls == []   # a given stream is Python's
+
+
+@pytest.mark.parametrize("name", ["rms_norm_backward", "layer_few"])
+def test_scratch_of_a_call_belongs_to_its_stream(name):
+    """A workspace that the call brings along is not given to the current stream while the call's own has yet to come to it."""
+    rows = 40
+    (_, call, outputs), = [c for c in every_call(rows, 8, 2, 256, 128, workspaces=False) if c[0] == name]
+    need = B.alloc_rms_norm_workspace(rows, 256) if name == "rms_norm_backward" else B.alloc_layer_few_workspace(rows, B.Router(8, 2), 256, 128)
+    need = need.numel()
+    call(None)
+    want = [t.clone() for t in outputs]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    call(side)
+    mine = [torch.full((need,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.current_stream().synchronize()
+    torch.cuda.synchronize()
+    assert all(bool((t == 7).all()) for t in mine)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outputs, want))
