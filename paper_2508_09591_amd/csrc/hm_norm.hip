@@ -230,19 +230,24 @@ static int norm_groups(int64_t rows, int32_t C) {
   return (int)(rows < most ? rows : most);
 }
 
-// Calls launch(vectors, threads) with the threads of a row and the vectors that each has of it.
+// Calls launch(vectors, threads) with the threads of a row and the vectors that each has of it.  Few rows leave most CUs without
+// one, and the fewer vectors a thread has the sooner a row is done; many rows hide each other's trips to memory, and a row of fewer
+// waves waits less for its own.  us forward (back), bf16 with a residual, few's shape against many's: one row of 1,024 3.1 (3.3) and 3.7
+// (3.2), of 7,168 4.3 (4.5) and 5.4 (5.0); 512 rows 4.1 (8.1) and 4.4 (8.2), 10.1 (17.3) and 10.3 (17.9); 1,024 rows 5.3 (11.6) and
+// 4.8 (11.2), 17.4 (23.4) and 16.4 (21.4); 8,192 rows 20.2 (27.5) and 14.0 (21.1), 114 (108) and 111 (97).  One wave a row up to 512
+// columns: 8,192 rows 8.7 (16.0), two vectors of it 13.0 (23.8).  Between 8,193 and 16,384 columns 512 threads of four vectors take
+// one row 7.3 (6.7), two of 1,024 6.0 (5.8), and 8,192 of 16,384 231 (212) and 220 (207).
 template <typename LAUNCH>
 static void norm_shape(int64_t rows, int32_t C, LAUNCH launch) {
 #define HM_NORM_SHAPE(v, t) launch(std::integral_constant<int, v>(), std::integral_constant<int, t>())
-  const bool few = rows <= 256;
+  const bool few = rows <= 512;
   if (C <= 512) HM_NORM_SHAPE(1, 64);
-  else if (C <= 1024) HM_NORM_SHAPE(2, 64);
+  else if (C <= 1024 && !few) HM_NORM_SHAPE(2, 64);
   else if (C <= 2048) HM_NORM_SHAPE(1, 256);
-  else if (C <= 4096 && few) HM_NORM_SHAPE(1, 512);
-  else if (C <= 4096) HM_NORM_SHAPE(2, 256);
-  else if (C <= 8192 && few) HM_NORM_SHAPE(1, 1024);
-  else if (C <= 8192) HM_NORM_SHAPE(2, 512);
-  else if (C <= 16384) HM_NORM_SHAPE(4, 512);
+  else if (C <= 4096) HM_NORM_SHAPE(1, 512);
+  else if (C <= 8192 && !few) HM_NORM_SHAPE(2, 512);
+  else if (C <= 8192) HM_NORM_SHAPE(1, 1024);
+  else if (C <= 16384) HM_NORM_SHAPE(2, 1024);
   else HM_NORM_SHAPE(4, 1024);
 #undef HM_NORM_SHAPE
 }

@@ -59,7 +59,7 @@ for rows in (1, 2, 256, 257, 1000, 100000, 1 << 31):
         assert rc == rb == 0 and len(forward) == 1
         vectors, threads = shape(forward[0]["name"])
         assert vectors * threads * 8 >= C and forward[0]["block"][0] == max(threads, 256)
-        assert vectors * threads * 8 < 2 * C or C <= 512   # most have something to do
+        assert vectors * threads * 8 < 2 * C or C <= (1024 if rows <= 512 else 512)   # most have something to do
         assert forward[0]["grid"][0] <= 2048
         vectors, threads = shape(backward[0]["name"])
         groups = min(rows, 1024 if C <= 1024 else 512)

@@ -45,7 +45,7 @@ def numbers8(q, s):
 
 
 SIZES = [(1, 1), (1, 7168), (3, 7), (5, 127), (2, 129), (9, 511), (4, 512), (66, 513), (7, 1030), (3, 2056), (5, 2049), (3, 4100), (4, 8192), (3, 8200), (2, 16390),
-         (2, 32768), (1, 32761)]
+         (2, 32768), (1, 32761), (600, 1000), (520, 4200)]
 TYPES = [(BF16, None, F32), (BF16, BF16, BF16), (BF16, F32, F32), (F32, None, BF16), (F32, F32, F32), (F32, BF16, F32)]
 
 
