@@ -4,6 +4,8 @@
 // operands of products of 16 x 16 x 32 in 16 bits, as for the products of few rows.  Values in 8 bits times their block's power of
 // two are exact in bf16, x is bf16; activations go between the two products as sums of two or three bf16 numbers, so that what
 // they lose is far below the output's rounding (2^-17 of each, 2^-25 for fp32 outputs).
+// us, and weights a second: a token's 8 experts of 7,168 x 2,048 74 (353 MB, 4.8 TB/s), of 2,048 x 768 18 (38 MB: two launches of two
+// trips to memory each); 64 tokens on 32 experts of the former 230 (1.23 GB, 5.3 TB/s).
 #include "hm_choice.h"
 
 namespace hm {
@@ -112,10 +114,11 @@ __device__ __forceinline__ Wide zero_wide() {
 // ---- the first product and the activation --------------------------------------------------------------
 // A workgroup takes an expert and 16 columns of its activation: as many rows of the gate's weights and of the up's.  Its four
 // waves share the steps of 128 columns of x and add up in LDS.  A lane has row l % 16 of the weights and of the slots, bytes
-// 32 (l / 16) to 32 (l / 16) + 31 of a step.
+// 32 (l / 16) to 32 (l / 16) + 31 of a step.  Two strips of columns a workgroup, eight waves, x in LDS and loads past the caches
+// were no faster.
 constexpr int kUpWaves = 4;
 
-//
+// GROUPS: of 16 slots each that one reading of the weights serves.
 // N: with up to four tokens every workgroup makes the choice by itself, lists of N, 16 lanes a token in its first wave, which takes it
 // less time than another launch would; the first one writes it down.  0: it has been made.
 constexpr int kChoosingTokens = kWave / 16;
@@ -239,7 +242,8 @@ __global__ __launch_bounds__(kUpWaves * kWave) void few_up_kernel(FewParams p, R
 // ---- the second product and the sum over a token's experts ---------------------------------------------
 // Few slots: a workgroup takes up to 16 columns of the output, all activations stand in its LDS, and its waves share the weights'
 // rows of all experts hit evenly, in pieces of four steps; behind an expert's pieces a wave adds what its slots get, times their
-// weights, to its own sums of the tokens, which are added up in the end.
+// weights, to its own sums of the tokens, which are added up in the end.  Activations read from memory in between would come behind the
+// weights that are on their way, as loads return in order: 41 us for a token's 8 experts of 7,168 x 2,048, 28 from LDS.
 constexpr int kDownWaves = 8, kPieceSteps = 4;
 template <int PLANES, typename OUT>
 __global__ __launch_bounds__(kDownWaves * kWave, PLANES == 2 ? 4 : 2) void few_down_kernel(FewParams p, int columns) {
@@ -344,7 +348,8 @@ __global__ __launch_bounds__(kDownWaves * kWave, PLANES == 2 ? 4 : 2) void few_d
 }
 
 // The same by experts: a workgroup takes one and FRAGS times 16 columns of the output, and leaves what its slots get; its four waves
-// take every fourth step.
+// take every fourth step.  64 tokens on 32 experts of 7,168 x 2,048 79 to 89 us (5.3 to 6 TB/s) and the sum's 5; all slots' activations do
+// not fit LDS there, and with all of a workgroup's experts in turn it took 453.
 template <int PLANES, int FRAGS>
 __global__ __launch_bounds__(kUpWaves * kWave) void few_down_slots_kernel(FewParams p) {
   __shared__ int lists[kUpWaves][kMostFewTokens];
@@ -471,13 +476,16 @@ static int64_t staged_limit() {
 }
 template <int PLANES, typename OUT>
 static hm_status launch_few(const FewParams &p, const RouteParams &route, hm_dtype logits, int64_t shares, hipStream_t stream) {
+  // The choice inside the first product: one token of 128 experts of 2,048 x 768 18.2 us, with a launch of its own 19.6.
+  // Four groups of slots take registers, hence waves, one reads an expert's weights again where there are more.  us with one and four:
+  // 8 experts of 7,168 x 2,048 and 5, 8, 10, 16 slots each (of 20 to 64 tokens) 81 and 88, 93 and 97, 100 and 98, 165 and 128; 32 experts
+  // and 8, 10, 16 of 8 a token 324 and 332, 335 and 344, 478 and 432; of 2,048 x 768 50 and 54, 54 and 58, 77 and 73.  Two groups
+  // are like four.  Up to 16 tokens no expert has more than one.
   if (chooses_itself(route)) {
     if (logits == HM_BF16) launch_choosing_up<uint16_t, PLANES>(p, route, shares, stream);
     else launch_choosing_up<float, PLANES>(p, route, shares, stream);
-  } else if (p.T <= 16 || p.T * p.K <= 6 * route.r.E) {
+  } else if (p.T <= 16 || p.T * p.K <= 10 * route.r.E) {
     launch_few_up<float, 0, 1, PLANES>(p, route, shares, stream);
-  } else if (p.T <= 32) {
-    launch_few_up<float, 0, 2, PLANES>(p, route, shares, stream);
   } else {
     launch_few_up<float, 0, 4, PLANES>(p, route, shares, stream);
   }
@@ -485,11 +493,15 @@ static hm_status launch_few(const FewParams &p, const RouteParams &route, hm_dty
   if (up != HM_OK) return up;
   const int64_t slots = (int64_t)p.T * p.K, staged = PLANES * slots * (row8_bytes(p.F) + 8) * 2, sums = (int64_t)kDownWaves * p.T * 16 * 4;
   if (slots <= kWave && staged + sums <= staged_limit<PLANES, OUT>()) {
+    // half the columns leave the matrix unit half empty, but a workgroup for each CU: 2,048 columns 7.8 to 8.5 us with 8, 8.7 to 9.4
+    // with 16, 7,168 35 and 28
     const int columns = p.H < 4096 ? 8 : 16;
     hipLaunchKernelGGL((few_down_kernel<PLANES, OUT>), dim3((unsigned)((p.H + columns - 1) / columns)), dim3(kDownWaves * kWave),
                        (size_t)(sums + staged), stream, p, columns);
     return hm_launch_status();
   }
+  // wide strips keep more loads on their way, narrow ones are more workgroups: 32 experts of 7,168 columns (3,584 wide strips) 85 and
+  // 95 us, 60 of 1,030 (1,020) 28.6 and 25.2
   const bool wide = shares * ((p.H + 63) / 64) >= 2048;
   const int64_t strip = wide ? 64 : 32;
   hipLaunchKernelGGL((wide ? few_down_slots_kernel<PLANES, 4> : few_down_slots_kernel<PLANES, 2>),

@@ -1,6 +1,7 @@
 // The activation between an expert's two products: rows h = [gate | up] of 2 F values, a = silu(gate) up, and the way back
 //     g_gate = ga up s (1 + gate (1 - s)),   g_up = ga gate s,   s = 1 / (1 + exp(-gate)),
-// written in the layouts that the products behind it read: rows in 8 bits, and on the way back also columns in 8 bits.
+// written in the layouts that the products behind it read: rows in 8 bits, and on the way back also columns in 8 bits, with a itself
+// computed again instead of kept.
 #include "hm_block8.h"
 
 namespace hm {
@@ -47,7 +48,9 @@ __device__ __forceinline__ void rows_of_segments(const int32_t *__restrict__ off
   }
 }
 
-// A wave takes 512 columns of a row of a; neighbouring waves take neighbouring pieces.
+// A wave takes 512 columns of a row of a; neighbouring waves take neighbouring pieces, so that a row's lines are asked for together:
+// 65,536 rows of 2 x 2,048 bf16 to 8 bits in 124 to 130 us (672 MB, 5.2 to 5.4 TB/s: memory), 173 where a workgroup took several rows
+// in turn.  64 rows 3.7 us: a launch and a trip to memory.
 template <typename IN>
 __global__ __launch_bounds__(kGatedThreads) void gated_kernel(GatedParams p) {
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -90,7 +93,8 @@ __device__ __forceinline__ float gradient_of_gate(const Gate &g, float up, float
 }
 __device__ __forceinline__ float gradient_of_up(const Gate &g, float ga) { return ga * g.times; }
 
-// Rows of [g_gate | g_up]: a wave takes 512 columns of a row, of either half or of both.
+// Rows of [g_gate | g_up]: a wave takes 512 columns of a row, of either half or of both.  Where columns are wanted too, this is for
+// rows in 8 bits of an F that is no multiple of 128 alone, whose blocks lie in both halves: 5,003 rows of F = 1,001 fp32 17 us.
 template <typename IN>
 __global__ __launch_bounds__(kGatedThreads) void gated_backward_rows_kernel(GatedBackParams p) {
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), F = p.F;
@@ -186,6 +190,10 @@ __device__ __forceinline__ float finite_size(float v) { return fabsf(v) < __buil
 // A tile is a block of 128 rows of a segment and 128 columns of each half; a thread has four rows of four columns.  Rows leave from
 // registers and the columns' largest values meet in LDS, and behind a barrier the values are turned in LDS and stored as columns.
 // What a thread loads for the next tile is on its way meanwhile, so a workgroup goes through several; one fills a CU.
+// 32,768 rows of F = 768 bf16 in all 8-bit layouts: 77 to 81 us, 277 MB at 3.5 TB/s, which copied would be 54; the vector unit is busy
+// for 47 of them.  A workgroup a tile, nothing ahead, g_gate, g_up and a through LDS one after the other, took 194.  fp32 has twice
+// the registers on their way and 72 to 104 bytes of a thread in scratch: loads later instead make no difference (5,003 rows of F =
+// 1,001 53 us, two generations of tiles for 256 workgroups, of which the first waits for memory alone).
 constexpr int kTurnThreads = 1024, kTurnPitch = 128 + 4, kTurnRows = 4, kTurnGroups = 256;
 // Everybody's accesses of LDS are done; loads from memory stay on their way.
 __device__ __forceinline__ void lds_barrier() {

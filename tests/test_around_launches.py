@@ -38,7 +38,7 @@ for T, E, K, H, F, groups, bias, here, out in ((1, 128, 8, 2048, 768, 1, 0, 128,
         up = launches[len(chosen)]
         assert up["grid"][:2] == [(F + 127) // 128 * 8, min(here, T * K)] and up["block"][0] == 256
         if not inside:   # how many slots a workgroup takes at a time
-            assert up["name"].split(",")[2].strip() == ("1" if T <= 16 or T * K <= 6 * E else "2" if T <= 32 else "4"), up["name"]
+            assert up["name"].split(",")[2].strip() == ("1" if T <= 16 or T * K <= 10 * E else "4"), up["name"]
 
 
 def test_kernels_of_the_norm_hold_a_row(recorder):
