@@ -23,7 +23,7 @@ class ExpertLayer:
     ways round: call it again after an optimizer step.  forward() keeps what backward() needs.  gone [E], bool: experts
     that no token may choose, say those of a rank that is lost: their logits are -inf and their gradients 0, while the
     gate stays finite.  It may be set between passes.  norm [H]: the weight of a norm in front of the layer, which then
-    takes x + residual, kept in self.total."""
+    takes x + residual; the last call's sum is self.total."""
 
     def __init__(self, gate: torch.Tensor, w13: torch.Tensor, w2: torch.Tensor, router: hm.Router, bias=None,
                  gone=None, norm=None, eps: float = 1e-6):
@@ -91,6 +91,7 @@ class ExpertLayer:
         T, K = x.shape[0], self.router.K
         x, x8 = self._normed(x, residual, True)   # in 8 bits once a token, then half the bytes to spread
         self.x, self.logits = x, self._logits(x)
+        self.normed = None if self.norm is None else self.total   # few() in between has a total of its own
         self.ids = torch.empty((T, K), dtype=torch.int32, device=x.device)
         self.weights = torch.empty((T, K), dtype=torch.float32, device=x.device)
         hm.hm_route(self.logits, self.router, self.ids, self.weights, self.bias)
@@ -127,7 +128,7 @@ class ExpertLayer:
         g_gate = g_logits.t() @ self.x.float()
         if self.norm is None:
             return g_x, g_gate, g_w13, g_w2
-        g_x, g_norm = hm.hm_rms_norm_backward(g_x, self.total, self.norm, self.eps, torch.empty_like(self.total),
+        g_x, g_norm = hm.hm_rms_norm_backward(g_x, self.normed, self.norm, self.eps, torch.empty_like(self.normed),
                                               empty(self.H), gtotal)
         return g_x, g_gate, g_w13, g_w2, g_norm
 

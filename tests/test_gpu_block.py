@@ -135,6 +135,19 @@ def test_a_training_step_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(again, want))
 
 
+def test_few_tokens_between_forward_and_backward():
+    """A served batch changes nothing of what the way back reads."""
+    layer = L.make_layer(8, 2, 512, 128, seed=3, norm=True)
+    x, gout, residual, gtotal = inputs(20, 512, 4, BF16)
+    layer.forward(x, residual)
+    want = layer.backward(gout, gtotal)
+    layer.forward(x, residual)
+    x2, _, residual2, _ = inputs(20, 512, 9, BF16)
+    layer.few(x2, residual2)
+    assert torch.equal(layer.total, (x2.float() + residual2.float()).to(BF16))
+    assert all(torch.equal(a, b) for a, b in zip(layer.backward(gout, gtotal), want))
+
+
 def test_a_residual_needs_a_norm():
     layer = L.make_layer(8, 2, 512, 64)
     x, _, residual, _ = inputs(3, 512, 1, BF16)
