@@ -17,7 +17,7 @@ __device__ __forceinline__ void wave_first(float &v, int &i) {
   }
 }
 
-// What the choice by lists (below) does not take: K > 16, groups that are no power of two up to 16, a softmax with a
+// What the choice by lists (hm_choice.h) does not take: K > 16, groups that are no power of two up to 16, a softmax with a
 // bias, many experts.  A wave takes a token; its choices stand in LDS and the largest is taken K times: 65,536 tokens
 // of 256 experts 178 us where the lists take 30.
 template <typename IN>

@@ -225,3 +225,48 @@ def test_scratch_of_a_call_belongs_to_its_stream(name):
     torch.cuda.synchronize()
     assert all(bool((t == 7).all()) for t in mine)
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outputs, want))
+
+
+def far_apart(t, ld):
+    """The same rows, ld elements apart, in memory of its own that is touched there alone."""
+    wide = torch.empty((t.shape[0], ld), dtype=t.dtype, device="cuda")[:, :t.shape[1]]
+    return wide.copy_(t)
+
+
+def test_rows_whose_offsets_pass_32_bits():
+    """Rows 2^29 elements apart, and for columns in 8 bits 1,100 rows 2^21 apart: the same bits as of rows that lie together."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    r = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(BF16)
+    T, H, F, ld = 5, 520, 260, 1 << 29
+    x, past, gy, weight = r(T, H), r(T, H), r(T, H), r(H)
+    empty = lambda *shape: torch.empty(shape, dtype=BF16, device="cuda")
+
+    def norm(x, past, total):
+        return B.hm_rms_norm(x, weight, 1e-6, empty(T, H), *B.alloc_rows8(T, H), past, total)
+    want, total = norm(x, past, empty(T, H)), empty(T, ld)[:, :H]
+    got = norm(far_apart(x, ld), far_apart(past, ld), total)
+    assert all(torch.equal(a.contiguous().view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want))
+    gx, gw = empty(T, ld)[:, :H], torch.empty(H, device="cuda")
+    B.hm_rms_norm_backward(far_apart(gy, ld), total, weight, 1e-6, gx, gw)
+    gx2, gw2 = B.hm_rms_norm_backward(gy, want[3], weight, 1e-6, empty(T, H), torch.empty(H, device="cuda"))
+    assert torch.equal(gx, gx2) and torch.equal(gw, gw2)
+    del total, got, gx
+    h, ga = r(T, 2 * F), r(T, F)
+    assert torch.equal(B.hm_gated(far_apart(h, ld), empty(T, F))[0], B.hm_gated(h, empty(T, F))[0])
+    assert torch.equal(B.hm_gated_backward(far_apart(h, ld), far_apart(ga, ld), gh=empty(T, 2 * F))[0], B.hm_gated_backward(h, ga, gh=empty(T, 2 * F))[0])
+    E, K = 8, 2
+    w13 = B.hm_quantize_weights(r(E, 2 * F, H), *B.alloc_weights8(E, 2 * F, H))
+    w2 = B.hm_quantize_weights(r(E, H, F), *B.alloc_weights8(E, H, F))
+    few = lambda x: B.hm_layer_few(x, logits, B.Router(E, K), *w13, *w2, torch.empty((T, K), dtype=torch.int32, device="cuda"),
+                                   torch.empty((T, K), device="cuda"), empty(T, H))
+    logits = r(T, E)
+    assert torch.equal(few(far_apart(x, ld)), few(x))
+    T, ld = 1100, 1 << 21
+    h, ga, offsets = r(T, 2 * F), r(T, F), torch.tensor([0, 300, 1100], dtype=torch.int32, device="cuda")
+
+    def columns(h, ga):
+        outputs = [t.zero_() for t in (*B.alloc_columns8(T, 2, 2 * F), *B.alloc_columns8(T, 2, F))]
+        return B.hm_gated_backward(h, ga, offsets, empty(T, 2 * F), None, None, *outputs)
+    for a, b in zip(columns(far_apart(h, ld), far_apart(ga, ld)), columns(h, ga)):
+        assert (a is None) == (b is None) and (a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8)))
