@@ -448,7 +448,11 @@ static int few_planes(hm_dtype out) { return out == HM_F32 ? 3 : 2; }
 
 template <typename LOGIT, int N, int GROUPS, int PLANES>
 static void launch_few_up(const FewParams &p, const RouteParams &route, int64_t shares, hipStream_t stream) {
-  const int lanes_per_group = 16 / route.r.groups, run = (route.r.E / route.r.groups + lanes_per_group - 1) / lanes_per_group;
+  int lanes_per_group = 0, run = 0;
+  if (N > 0) {   // of the choice by lists, which has at most 16 groups; other routers have more groups than lanes
+    lanes_per_group = 16 / route.r.groups;
+    run = (route.r.E / route.r.groups + lanes_per_group - 1) / lanes_per_group;
+  }
   hipLaunchKernelGGL((few_up_kernel<LOGIT, N, GROUPS, PLANES>), dim3((unsigned)(row8_bytes(p.F) / 16), (unsigned)shares),
                      dim3(kUpWaves * kWave), 0, stream, p, route, lanes_per_group, run);
 }

@@ -89,3 +89,22 @@ for dtype in (0, 1):
             assert launches[0]["grid"][0] == min(tiles, 256) and launches[0]["name"].endswith("true>" if gh else "false>")
         if by_rows:
             assert launches[-1]["grid"][0] == -(-rows * -(-2 * F // 512) // 4)
+
+
+def test_few_tokens_of_a_router_of_many_groups(recorder):
+    """More groups than the 16 lanes that choose inside the first product: hm_route's kernel makes the choice, as it does alone."""
+    result = launch_recorder.run(recorder, r"""
+result = []
+for E, groups in ((272, 17), (320, 20), (256, 32), (64, 64), (4096, 4096)):
+    for T in (1, 4, 5, 64):
+        for logits in (0, 1):
+            r = ctypes.byref(B.hm_router(E, 4, 1, groups, 4, 1, 1, 1.0))
+            rc = L.hm_route(at(2), logits, E, at(3), T, r, at(8), at(9), None)
+            alone = launched()
+            few = L.hm_layer_few(at(1), 512, at(2), logits, E, at(3), T, r, at(4), at(5), at(6), at(7), 0, 8, 512, 128, at(8), at(9), at(10), 0, at(11), 1 << 40, None)
+            result.append([E, groups, T, rc, few, alone, launched()])
+""")
+    for E, groups, T, rc, few, alone, launches in result:
+        assert rc == few == 0, (E, groups, T)
+        assert alone[0]["name"].startswith("route_kernel") and launches[0] == alone[0]
+        assert [k["name"].split("<")[0] for k in launches[1:]] == ["few_up_kernel"] + (["few_down_kernel"] if T <= 5 else ["few_down_slots_kernel", "few_sum_kernel"])

@@ -88,6 +88,22 @@ def test_some_of_the_experts_are_here(first, here):
     check(layer, x, ids, weights, out)
 
 
+@pytest.mark.parametrize("E,groups,top_groups", [(96, 32, 5), (68, 17, 3), (40, 20, 6)])
+def test_a_router_of_many_groups(E, groups, top_groups):
+    """More groups than the lanes that choose inside the first product: the choice is hm_route's, for one token and for many."""
+    K, H, F = 5, 264, 136
+    layer = Layer(E, H, F, seed=E)
+    for score, bias in (("softmax", None), ("sigmoid", torch.linspace(-0.1, 0.1, E, device="cuda"))):
+        router = B.Router(E, K, score, groups=groups, top_groups=top_groups, group_best=2, scale=2.5)
+        for T, dtype in ((1, F32), (4, BF16), (5, F32), (40, BF16)):
+            x, logits = inputs(T, E, H, T + groups)
+            ids, weights, out = layer.run(x, logits, router, bias=bias, dtype=dtype)
+            want_ids, want_weights = torch.empty_like(ids), torch.empty_like(weights)
+            B.hm_route(logits, router, want_ids, want_weights, bias)
+            assert torch.equal(ids, want_ids) and torch.equal(weights, want_weights) and bool((ids >= 0).all())
+            check(layer, x, ids, weights, out)
+
+
 def test_tokens_without_experts_and_padded_ones():
     """-inf and NaN logits leave a token without slots: zeros, whatever its row holds; a NaN row stays its own."""
     T, E, K, H, F = 12, 6, 3, 200, 72
