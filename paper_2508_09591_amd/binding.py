@@ -886,6 +886,15 @@ def _pair8(q, scale, shape, scale_shape, name: str):
     return (None, None) if q is None else (_codes(q, shape, name), _scales(scale, scale_shape, "the scales of " + name))
 
 
+def _segments(offsets: Optional[torch.Tensor]) -> int:
+    """Segments of offsets that may be left out.  A tensor of no entries has no address: the library would take it for left out."""
+    if offsets is None:
+        return 0
+    if offsets.numel() == 0:
+        raise ValueError("offsets must have an entry more than there are segments, got none; leave them out to take all rows")
+    return offsets.numel() - 1
+
+
 def _scratch_for(stream, alloc):
     """A workspace that lives for one call on the given stream: of that stream's memory, so that nobody gets it before the call is done."""
     if stream is None:
@@ -979,7 +988,7 @@ def hm_gated(h: torch.Tensor, a: Optional[torch.Tensor] = None, q: Optional[torc
     if a is None and q is None:
         raise ValueError("a, or q and its scales, must be given")
     codes = _pair8(q, scale, (rows, row8_bytes(F)), (rows, scale8_bytes(F)), "q")
-    rc = lib().hm_gated(at, _floats(h, "h"), ld, _dev(offsets, torch.int32, "offsets"), 0 if offsets is None else offsets.numel() - 1, rows, F,
+    rc = lib().hm_gated(at, _floats(h, "h"), ld, _dev(offsets, torch.int32, "offsets"), _segments(offsets), rows, F,
                         None if a is None else _dev(_shaped(a, (rows, F), "a"), a.dtype, "a"), _optional_floats(a, "a"), *codes,
                         _stream(stream))
     _check("hm_gated", rc)
@@ -1009,7 +1018,7 @@ def hm_gated_backward(h: torch.Tensor, ga: torch.Tensor, offsets: Optional[torch
         raise ValueError("one of the outputs must be given")
     if offsets is None and (q_columns is not None or a_columns is not None):
         raise ValueError("columns need offsets")
-    segments = 0 if offsets is None else offsets.numel() - 1
+    segments = _segments(offsets)
     blocks = rows // 128 + segments
     rc = lib().hm_gated_backward(at, g, _floats(h, "h"), ld, g_ld, _dev(offsets, torch.int32, "offsets"), segments, rows, F,
                                  None if gh is None else _dev(_shaped(gh, (rows, 2 * F), "gh"), gh.dtype, "gh"), _optional_floats(gh, "gh"),

@@ -668,7 +668,7 @@ const int32_t *offsets_or_none(PyObject *o, int32_t &segments) {
   segments = 0;
   if (o == Py_None) return nullptr;
   const at::Tensor &t = here(o);
-  if (t.scalar_type() != at::kInt) throw NotOrdinary();
+  if (t.scalar_type() != at::kInt || t.numel() == 0) throw NotOrdinary();   // no entries are no address, which would stand for all rows
   segments = size32(t.numel() - 1);
   return static_cast<const int32_t *>(t.data_ptr());
 }

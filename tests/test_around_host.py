@@ -121,6 +121,15 @@ def test_the_binding_says_what_does_not_fit():
                        z(4, 2, dtype=torch.int32), z(4, 2, dtype=f32), z(4, 64))
 
 
+def test_offsets_of_no_entries_are_not_none():
+    """They have no address, which the library takes for all rows."""
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)
+    assert B._segments(None) == 0 and B._segments(i32(2)) == 1 and B._segments(i32(17)) == 16
+    assert B._segments(i32(1)) == 0   # which the library refuses, as there is an address
+    with pytest.raises(ValueError, match="offsets"):
+        B._segments(i32(0))
+
+
 NAMES = [n[3:] for n in B._NATIVE_AROUND]
 
 

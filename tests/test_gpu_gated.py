@@ -263,3 +263,17 @@ def test_nothing_to_do_and_what_does_not_fit():
     for bad in (dict(ga=e(4, 32, dtype=F32)), dict(gh=e(4, 64, dtype=torch.float16)), dict(ga=e(32, 4).t())):
         with pytest.raises(TypeError):
             back(**bad)
+
+
+def test_offsets_of_no_entries_are_refused():
+    """With and without a given stream, so by both halves of the binding; nothing is written."""
+    h, ga, off = torch.ones((4, 64), device="cuda"), torch.ones((4, 32), device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    for stream in (None, torch.cuda.current_stream()):
+        a, gh, rows8 = torch.full((4, 32), 7.0, device="cuda"), torch.full((4, 64), 7.0, device="cuda"), poisoned(B.alloc_rows8(4, 64))
+        with pytest.raises(ValueError, match="offsets"):
+            B.hm_gated(h, a, offsets=off, stream=stream)
+        with pytest.raises(ValueError, match="offsets"):
+            B.hm_gated_backward(h, ga, off, gh, *rows8, stream=stream)
+        with pytest.raises(B.HierMoEError):
+            B.hm_gated(h, a, offsets=torch.zeros(1, dtype=torch.int32, device="cuda"), stream=stream)
+        assert bool((a == 7).all()) and bool((gh == 7).all()) and all(is_poison(t) for t in rows8)
