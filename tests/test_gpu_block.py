@@ -65,6 +65,40 @@ def test_norm_layer_and_gradients(T, E, K, H, F, kept):
     assert torch.isfinite(grads[1]).all()
 
 
+def size_of_the_router_gradient(layer, x, residual, gout, ids):
+    """What the terms of the gate's gradient amount to.  A logit's gradient is a difference of dot products gout y, each a sum of H terms of
+    either sign, and it is errors of the terms that add up, not of what is left of them."""
+    total = (x if residual is None else x.double() + residual.double()).double().cpu()
+    y = total * torch.rsqrt(total.square().mean(dim=1, keepdim=True) + layer.eps) * layer.norm.double().cpu()
+    gate, w13, w2, gout, ids = (t.detach().cpu() for t in (layer.gate.double(), layer.w13.double(), layer.w2.double(), gout.double(), ids.long()))
+    w = torch.softmax(y @ gate.t(), dim=1).gather(1, ids)
+    w, length = w / w.sum(dim=1, keepdim=True), torch.zeros_like(w)
+    for e in range(layer.E):
+        t, k = (ids == e).nonzero(as_tuple=True)
+        h = y[t] @ w13[e].t()
+        length[t, k] = ((torch.nn.functional.silu(h[:, :layer.F]) * h[:, layer.F:]) @ w2[e].t()).norm(dim=1)
+    size = gout.norm(dim=1, keepdim=True) * length / layer.H ** 0.5
+    each = w * (size ** 2 + (w * size).square().sum(dim=1, keepdim=True)).sqrt()
+    return (each.square().sum(dim=1) * y.square().sum(dim=1)).sum().sqrt()
+
+
+@pytest.mark.parametrize("T,E,K,H,F,kept", [(200, 8, 2, 512, 320, torch.float32), (157, 16, 4, 1024, 200, BF16), (64, 12, 3, 512, 136, None)])
+def test_the_layers_own_part_of_the_gradients(T, E, K, H, F, kept):
+    """The gradient of x without what came past the layer, which is three to four times as large and would hide its errors, and the gate's."""
+    layer = L.make_layer(E, K, H, F, seed=T, norm=True)
+    x, gout, residual, gtotal = inputs(T, H, T + 1, kept)
+    layer.forward(x, residual)
+    grads = layer.backward(gout, gtotal)
+    assert bool((layer.ids >= 0).all())
+    want = reference(layer, x, residual, gout, None, layer.ids)[2]
+    mine = grads[0].double() - (0 if gtotal is None else gtotal.double())
+    # six values in 8 bits on the way, 2^-5.5 of each: 0.054, with room for the activation's share; that a sum four times as large is rounded
+    # to bf16, 2^-9.8 of it on average, adds 0.005 of the part
+    assert far(mine, want[0]) <= 0.12
+    # the router's: y has four of the roundings, 0.044 of its terms, weights and x none; three times 0.05 as the layer's own test has it
+    assert (grads[1].double().cpu() - want[1]).norm() <= 3 * 0.05 * size_of_the_router_gradient(layer, x, residual, gout, layer.ids)
+
+
 @pytest.mark.parametrize("T,E,K,H,F,kept", [(1, 16, 4, 512, 256, BF16), (16, 8, 2, 1024, 320, torch.float32), (50, 32, 4, 512, 200, None)])
 def test_few_tokens(T, E, K, H, F, kept):
     layer = L.make_layer(E, K, H, F, seed=T, norm=True)
