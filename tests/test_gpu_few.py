@@ -69,6 +69,24 @@ def test_every_size(T, E, K, H, F, dtype):
     check(layer, x, ids, weights, out)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,E,K,H,F", [(64, 64, 1, 264, 136), (50, 40, 4, 520, 72), (33, 24, 2, 264, 700), (20, 16, 1, 264, 640), (30, 32, 2, 136, 120),
+                                       (30, 32, 2, 4100, 120)])
+def test_all_tokens_choose_the_same_expert(T, E, K, H, F, dtype):
+    """More than 16 slots of one expert, though on average there are few: its weights are read again, by the first product and by the second,
+    which goes by experts, or by columns with two pieces of an expert (F = 640 to bf16) or several experts a wave (F = 120)."""
+    layer, router = Layer(E, H, F, seed=T), B.Router(E, K, "softmax")
+    assert T > 16 and T * K <= 10 * E   # so that one reading of the weights serves 16 slots
+    x, logits = inputs(T, E, H, T + 2)
+    logits[:, 3] = 9.0
+    logits[::7, 3] = -9.0   # not of every token: slots are apart
+    ids, weights, out = layer.run(x, logits, router, dtype=dtype)
+    assert (ids == 3).sum() == T - (T + 6) // 7 > 16
+    check(layer, x, ids, weights, out)
+    again = layer.run(x, logits, router, dtype=dtype)[2]
+    assert torch.equal(out, again)
+
+
 @pytest.mark.parametrize("first,here", [(0, 8), (8, 24), (31, 1), (0, 32)])
 def test_some_of_the_experts_are_here(first, here):
     """Groups, a bias, logits in bf16, rows that lie apart; slots of experts elsewhere add nothing, and the ranks' parts add up."""
