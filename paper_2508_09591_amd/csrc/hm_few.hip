@@ -12,7 +12,6 @@ namespace hm {
 
 constexpr int kMostFewTokens = 64, kMostFewSlots = 1024;
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 struct FewParams {
@@ -443,8 +442,6 @@ __global__ __launch_bounds__(256) void few_sum_kernel(FewParams p) {
   }
   store_float((OUT *)p.out + (int64_t)t * p.H + h, sum);
 }
-
-static int few_planes(hm_dtype out) { return out == HM_F32 ? 3 : 2; }
 
 template <typename LOGIT, int N, int GROUPS, int PLANES>
 static void launch_few_up(const FewParams &p, const RouteParams &route, int64_t shares, hipStream_t stream) {
