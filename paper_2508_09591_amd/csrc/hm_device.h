@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "hiermoe.h"
@@ -313,4 +314,21 @@ static inline hm_status hm_launch_status() {
   if (now == hipSuccess || now == hm_pending_at_entry) return HM_OK;
   (void)hipGetLastError();   // ours: reported through the return code, not left for the next caller
   return HM_ERR_HIP;
+}
+// Whether the current device gives `kernel` dynamic LDS of so many bytes, more than it gets by default (64 KiB).  It is
+// asked for once on a device, as the grant is that device's alone; `grant` is a static of the caller's for the kernel.
+struct LdsGrant {
+  std::atomic<int> of[64] = {};   // 0: not asked for, 1: granted, -1: refused
+};
+static inline bool lds_granted(LdsGrant &grant, const void *kernel, int bytes) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return false;
+  int v = grant.of[dev].load(std::memory_order_acquire);
+  if (v == 0) {
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) (void)hipGetLastError();   // not sticky: do not let it fail the next launch check
+    v = e == hipSuccess ? 1 : -1;
+    grant.of[dev].store(v, std::memory_order_release);
+  }
+  return v > 0;
 }

@@ -462,18 +462,13 @@ static void launch_choosing_up(const FewParams &p, const RouteParams &route, int
   if (p.K <= 8) launch_few_up<LOGIT, 8, 1, PLANES>(p, route, shares, stream);
   else launch_few_up<LOGIT, 16, 1, PLANES>(p, route, shares, stream);
 }
-// Dynamic LDS that few_down_kernel may have: asked for once, as it is more than a kernel gets by default.  It takes in the eight
-// slots of one token of 2,048 columns, and leaves room for two workgroups a CU.
+// Dynamic LDS that few_down_kernel may have, more than a kernel gets by default.  It takes in the eight slots of one token of
+// 2,048 columns, and leaves room for two workgroups a CU.
 constexpr int kMostStaged = 66 * 1024;
 template <int PLANES, typename OUT>
 static int64_t staged_limit() {
-  static const bool granted = [] {
-    const hipError_t e = hipFuncSetAttribute((const void *)few_down_kernel<PLANES, OUT>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             kMostStaged);
-    if (e != hipSuccess) (void)hipGetLastError();   // not sticky: do not let it fail the next launch check
-    return e == hipSuccess;
-  }();
-  return granted ? kMostStaged : 65536 - 4096;   // beside what it has anyway
+  static LdsGrant grant;
+  return lds_granted(grant, (const void *)few_down_kernel<PLANES, OUT>, kMostStaged) ? kMostStaged : 65536 - 4096;   // beside what it has anyway
 }
 template <int PLANES, typename OUT>
 static hm_status launch_few(const FewParams &p, const RouteParams &route, hm_dtype logits, int64_t shares, hipStream_t stream) {

@@ -1104,16 +1104,11 @@ __global__ void swap_apply_kernel(int32_t *__restrict__ expert_to_rank, int32_t 
   expert_to_rank[c] = g;
 }
 
-// The co-occurrence kernel may use more dynamic LDS than a kernel gets by default (64 KiB); ask
-// once.  False: the tables stay in global memory.
+// The co-occurrence kernel may use more dynamic LDS than a kernel gets by default (64 KiB).  False: the tables stay
+// in global memory.
 static bool swap_factors_lds_ready() {
-  static const bool ok = [] {
-    const hipError_t e = hipFuncSetAttribute((const void *)swap_factors_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             kSwapLds * (int)sizeof(int32_t));
-    if (e != hipSuccess) (void)hipGetLastError();   // not sticky: do not let it fail the next launch check
-    return e == hipSuccess;
-  }();
-  return ok;
+  static LdsGrant grant;
+  return lds_granted(grant, (const void *)swap_factors_kernel, kSwapLds * (int)sizeof(int32_t));
 }
 
 // Whether the workspace has partial tables of chunks (and a byte per slot): E <= 256 and chunks short enough for
@@ -1149,12 +1144,8 @@ struct CoocLaunch {
 };
 template <int COLS, bool OWN_SLOTS, bool ADDED>
 static CoocLaunch cooc_launch(int E, int groups, int64_t tokens) {   // groups of the finest cut, tokens of a chunk
-  static const bool granted = [] {
-    const hipError_t e = hipFuncSetAttribute((const void *)swap_cooc_kernel<COLS, OWN_SLOTS, ADDED>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, kCoocLds);
-    if (e != hipSuccess) (void)hipGetLastError();   // not sticky: do not let it fail the next launch check
-    return e == hipSuccess;
-  }();
+  static LdsGrant grant;
+  const bool granted = lds_granted(grant, (const void *)swap_cooc_kernel<COLS, OWN_SLOTS, ADDED>, kCoocLds);
   constexpr int kBatch = 4 / COLS * kCoocStep;   // a tile is whole batches of products
   const int rows = CoocTiles<COLS>(E, groups).rows();
   int most = 2 * (kCoocLds / rows - kCoocPad) / kBatch * kBatch;

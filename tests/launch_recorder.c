@@ -2,7 +2,7 @@
  * global scope ahead of the library, it takes the library's runtime calls, notes every launch and runs nothing. */
 #include <hip/hip_runtime_api.h>
 
-enum { MOST = 1024, DEFAULT_LDS = 65536 };   /* dynamic LDS of a kernel that has not been granted more */
+enum { MOST = 1024, DEVICES = 4, DEFAULT_LDS = 65536 };   /* dynamic LDS of a kernel that has not been granted more on a device */
 
 typedef struct {
   const char *name;
@@ -10,9 +10,9 @@ typedef struct {
   uint64_t lds, granted;
 } launch_t;
 
-static struct { const void *fn; const char *name; uint64_t granted; } kernels[MOST];
+static struct { const void *fn; const char *name; uint64_t granted[DEVICES]; } kernels[MOST];
 static launch_t launches[MOST];
-static int n_kernels, n_launches;
+static int n_kernels, n_launches, current;
 static struct { dim3 grid, block; size_t lds; hipStream_t stream; } pending;
 
 static int find(const void *fn) {
@@ -25,6 +25,7 @@ static int find(const void *fn) {
 int recorder_count(void) { return n_launches; }
 const launch_t *recorder_launch(int i) { return &launches[i]; }
 void recorder_reset(void) { n_launches = 0; }
+void recorder_device(int device) { current = device; }
 
 /* what the library's launches and registrations call */
 void **__hipRegisterFatBinary(const void *data) { static void *module; return &module; }
@@ -34,7 +35,8 @@ void __hipRegisterFunction(void **module, const void *fn, char *device_fn, const
   if (n_kernels == MOST) return;
   kernels[n_kernels].fn = fn;
   kernels[n_kernels].name = name;
-  kernels[n_kernels++].granted = DEFAULT_LDS;
+  for (int i = 0; i < DEVICES; ++i) kernels[n_kernels].granted[i] = DEFAULT_LDS;
+  ++n_kernels;
 }
 hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t lds, hipStream_t stream) {
   pending.grid = grid, pending.block = block, pending.lds = lds, pending.stream = stream;
@@ -47,20 +49,20 @@ hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *lds, hipSt
 hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, size_t lds, hipStream_t stream) {
   const int k = find(fn);
   if (k == n_kernels || n_launches == MOST) return hipErrorInvalidDeviceFunction;
-  launches[n_launches++] = (launch_t){kernels[k].name, {grid.x, grid.y, grid.z}, {block.x, block.y, block.z}, lds, kernels[k].granted};
+  launches[n_launches++] = (launch_t){kernels[k].name, {grid.x, grid.y, grid.z}, {block.x, block.y, block.z}, lds, kernels[k].granted[current]};
   return hipSuccess;
 }
 hipError_t hipFuncSetAttribute(const void *fn, hipFuncAttribute attribute, int value) {
   const int k = find(fn);
   if (k == n_kernels || attribute != hipFuncAttributeMaxDynamicSharedMemorySize) return hipErrorInvalidValue;
-  kernels[k].granted = value;
+  kernels[k].granted[current] = value;
   return hipSuccess;
 }
 hipError_t hipDeviceGetAttribute(int *value, hipDeviceAttribute_t attribute, int device) {   /* an MI355X */
   *value = attribute == hipDeviceAttributeMaxSharedMemoryPerMultiprocessor ? 163840 : 256;
   return hipSuccess;
 }
-hipError_t hipGetDevice(int *device) { *device = 0; return hipSuccess; }
+hipError_t hipGetDevice(int *device) { *device = current; return hipSuccess; }
 hipError_t hipGetLastError(void) { return hipSuccess; }
 hipError_t hipPeekAtLastError(void) { return hipSuccess; }
 hipError_t hipGetSymbolAddress(void **address, const void *symbol) { *address = (void *)0x10000; return hipSuccess; }

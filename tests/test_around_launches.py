@@ -108,3 +108,19 @@ for E, groups in ((272, 17), (320, 20), (256, 32), (64, 64), (4096, 4096)):
         assert rc == few == 0, (E, groups, T)
         assert alone[0]["name"].startswith("route_kernel") and launches[0] == alone[0]
         assert [k["name"].split("<")[0] for k in launches[1:]] == ["few_up_kernel"] + (["few_down_kernel"] if T <= 5 else ["few_down_slots_kernel", "few_sum_kernel"])
+
+
+def test_lds_is_granted_on_every_device(recorder):
+    """What a kernel may have beyond the default is a device's: a second device of the process is asked too, once."""
+    result = launch_recorder.run(recorder, r"""
+result = []
+r = ctypes.byref(B.hm_router(32, 8, 1, 1, 1, 1, 1, 1.0))
+for device in (0, 1, 0, 3, 1):
+    recorder.recorder_device(device)
+    for out in (0, 1):
+        rc = L.hm_layer_few(at(1), 7168, at(2), 1, 32, at(3), 1, r, at(4), at(5), at(6), at(7), 0, 32, 7168, 2048 >> out, at(8), at(9), at(10), out, at(11), 1 << 40, None)
+        result.append([device, rc, launched()])
+""")
+    for device, rc, launches in result:
+        assert rc == 0 and launches[-1]["name"].startswith("few_down_kernel")
+        assert launches[-1]["lds"] <= launches[-1]["granted"], (device, launches[-1])
