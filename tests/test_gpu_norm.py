@@ -107,6 +107,21 @@ def test_rows_that_are_no_numbers():
     assert (np.abs(f64(y[[0, 4, 5]]) - want) <= A.U * np.abs(want) + off + A.TINY).all()
 
 
+@pytest.mark.parametrize("rows,C", [(512, 1030), (1024, 1000), (448, 40)])
+def test_the_weights_gradient_keeps_small_parts_beside_large_ones(rows, C):
+    """A row a part, whose terms are exact: 1, and many of 2^-25, of which fp32 keeps none beside the 1.  64 sums of fp32 have up to
+    rows / 64 + 3 parts each, half a step of 1 for every addition, and are added up in 64 bits and rounded once; one sum of a 16th of the
+    parts would lose rows / 32 - 1/2 half steps."""
+    assert parts_of(rows, C) == rows
+    gy = torch.full((rows, C), 2.0 ** -25, device="cuda")
+    gy[0] = 1.0
+    s, gw = torch.ones_like(gy), torch.empty(C, device="cuda")
+    B.hm_rms_norm_backward(gy, s, torch.ones(C, device="cuda"), 0.0, torch.empty_like(gy), gw)
+    want = 1.0 + (rows - 1) * 2.0 ** -25
+    assert rows / 64 + 4 < rows / 32 - 0.5
+    assert (np.abs(f64(gw) - want) <= (rows / 64 + 4) * A.U * want).all()
+
+
 def test_no_rows():
     w = torch.ones(64, device="cuda")
     none, gw = torch.empty((0, 64), dtype=BF16, device="cuda"), torch.full((64,), 5.0, device="cuda")
