@@ -4,8 +4,8 @@
 // Both need a row's sums before they can write the row, so a row stays in registers between: THREADS threads have VEC
 // vectors of eight values of it, the k-th of thread i being vector k THREADS + i.  A wave's vectors are 512 neighbouring
 // columns, four blocks of 8 bits.  Memory bounds both: 8,192 rows of 7,168 bf16 with a residual, values and 8 bits written, take
-// 111 us (528 MB, 4.8 TB/s; a copy of it 103), the way back 97 (470 MB, 4.9 TB/s; 92); one row is a launch, a trip to memory and a
-// barrier (4.3 us).
+// 106 us (528 MB, 5.0 TB/s; a copy of it 103), with an fp32 residual 146 (764 MB; 149), all in fp32 166 (881 MB; 172); the way back 97
+// (470 MB, 4.9 TB/s; 92), in fp32 155 (822 MB; 160).  One row is a launch, a trip to memory and a barrier (4.3 us).
 #include "hm_block8.h"
 
 namespace hm {
@@ -46,7 +46,7 @@ __device__ __forceinline__ void row_sums(const float (&v)[N], float (&sums)[2][N
   }
 }
 // m^-1/2 and what it is short of the exact value, from one step of Newton's in 64 bits: every value of a row would share its error.
-// With it a value is rounded once, where the root's, the product's and the weight's roundings would be three (8,192 x 7,168 104 us).
+// With it a value is rounded once, where the root's, the product's and the weight's roundings would be three.
 struct Inverse {
   float root, rest;
 };
@@ -66,8 +66,10 @@ __device__ __forceinline__ void load_weight(const void *weight, bool bf16, int c
 template <int THREADS>
 constexpr int norm_block() { return THREADS < 256 ? 256 : THREADS; }
 
+// 8,192 rows of 7,168 take 84 registers (99 with an fp32 residual), five (four) waves a SIMD; held to 80 for six they spilled 20 (68) bytes a
+// thread: 111 (168) us instead of 106 (146), of 5,000 columns 97 (144) and 90 (117).
 template <typename IN, typename SUM, int VEC, int THREADS>
-__global__ __launch_bounds__(norm_block<THREADS>(), THREADS == 512 && VEC == 2 ? 6 : 1) void rms_norm_kernel(NormParams p) {
+__global__ __launch_bounds__(norm_block<THREADS>()) void rms_norm_kernel(NormParams p) {
   constexpr int kRows = norm_block<THREADS>() / THREADS;   // of a workgroup
   __shared__ float sums[2][1][THREADS / kWave];
   const int tid = threadIdx.x % THREADS, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -247,10 +249,13 @@ static int norm_groups(int64_t rows, int32_t C) {
 // Calls launch(vectors, threads) with the threads of a row and the vectors that each has of it.  Few rows leave most CUs without
 // one, and the fewer vectors a thread has the sooner a row is done; many rows hide each other's trips to memory, and a row of fewer
 // waves waits less for its own.  us forward (back), bf16 with a residual, few's shape against many's: one row of 1,024 3.1 (3.3) and 3.7
-// (3.2), of 7,168 4.3 (4.5) and 5.4 (5.0); 512 rows 4.1 (8.1) and 4.4 (8.2), 10.1 (17.3) and 10.3 (17.9); 1,024 rows 5.3 (11.6) and
-// 4.8 (11.2), 17.4 (23.4) and 16.4 (21.4); 8,192 rows 20.2 (27.5) and 14.0 (21.1), 114 (108) and 111 (97).  One wave a row up to 512
+// (3.2), of 7,168 4.3 (4.5) and 5.1 (5.1); 512 rows 4.2 (8.1) and 4.4 (8.1), 10.0 (17.1) and 10.0 (17.9); 1,024 rows 5.2 (11.4) and
+// 4.8 (11.2), 17.5 (23.5) and 16.0 (21.0); 8,192 rows 19.8 (27.3) and 14.0 (21.2), 114 (108) and 106 (97).  One wave a row up to 512
 // columns: 8,192 rows 8.7 (16.0), two vectors of it 13.0 (23.8).  Between 8,193 and 16,384 columns 512 threads of four vectors take
-// one row 7.3 (6.7), two of 1,024 6.0 (5.8), and 8,192 of 16,384 231 (212) and 220 (207).
+// one row 7.3 (6.7), two of 1,024 6.0 (5.8), and 8,192 of 16,384 231 (212) and 220 (207).  Beyond, 1,024 threads are all there
+// are: 32 values of a thread, which on the way back, with weight, gradient and two or three rows, pass its 128 registers by 180 to 300 bytes.  Of
+// 32,768 columns one row takes 10.5 (18.9), in fp32 12.6 (27.1); 4,096 rows 234 (344), in fp32 411 (708), where copies take 236 (209)
+// and 393 (366).
 template <typename LAUNCH>
 static void norm_shape(int64_t rows, int32_t C, LAUNCH launch) {
 #define HM_NORM_SHAPE(v, t) launch(std::integral_constant<int, v>(), std::integral_constant<int, t>())
