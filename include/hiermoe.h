@@ -8,8 +8,9 @@
  * token rows into per-destination send buffers, and merges expert outputs coming back in that
  * layout with the router weights ("AlltoAll Combine", Section II-B).  Destinations are index
  * partitions of one buffer; the exchange itself is not part of the library.  In front of the plan stands the router
- * (hm_route), between dispatch and combine the experts' products in 8 bits (hm_expert_matmul), both with their
- * gradients.
+ * (hm_route), between dispatch and combine the experts' products in 8 bits (hm_expert_matmul), in front of all the norm
+ * (hm_rms_norm) and between the products the activation (hm_gated), all with their gradients; a few served tokens take
+ * the layer in one call (hm_layer_few).
  *
  * Conventions
  *   - Unless marked "host", every pointer is a DEVICE pointer into memory the caller owns.
@@ -29,7 +30,8 @@
  *     T*K <= 2^31-1.
  *   - Re-entrant per (plan buffers, workspace, stream); the only global state is what is named
  *     where it is declared: hm_plan_one_launch_limit, the scratch of hm_plan_static, and kernel
- *     attributes (dynamic LDS limits) that hm_swap_counts sets the first time it runs.
+ *     attributes (dynamic LDS limits) that hm_swap_counts and hm_layer_few set the first time they
+ *     run on a device.
  */
 #ifndef HIERMOE_H
 #define HIERMOE_H
@@ -562,9 +564,11 @@ hm_status hm_expert_matmul_dw(const uint8_t *gy, const uint8_t *gy_scale, const 
  *     s = x + residual,   y = s / sqrt(mean(s^2) + eps) * weight      per row of C values
  * residual [rows,C] of total_dtype or NULL; with it the sum, rounded to that type, is kept in total (not NULL then), and
  * what is normed is the sum as it is kept.  y [rows,C] of y_dtype, and q, scale: the same values in 8 bits in the layout
- * `rows` above, rounded once from fp32; either may be NULL, not both.  Squares are added in fp32: a row whose squares add up
- * to more than 3.4e38 gives zeros, one with a NaN gives NaN, and with eps 0 values below 1e-16 may count for too little.  x, residual and total have rows ld, residual_ld, total_ld elements
- * apart; total may be x or residual itself (the same elements in the same place), y may be x.
+ * `rows` above, rounded once from fp32; either may be NULL, not both.  Squares are added in fp32 over parts of a row (up
+ * to 2,048 of its values) and the parts in 64 bits: a row with a part that adds up to more than 3.4e38 gives zeros, one
+ * with a NaN gives NaN, and with eps 0 values below 1e-16 may count for too little.  x, residual and total have rows ld,
+ * residual_ld, total_ld elements apart; total may be x or residual itself (the same elements in the same place), y may
+ * be x.
  * Limits: C <= 32768, rows <= 2^31 - 1, eps >= 0.
  */
 hm_status hm_rms_norm(const void *x, hm_dtype dtype, int64_t ld, const void *residual, hm_dtype total_dtype,
@@ -618,9 +622,11 @@ hm_status hm_gated_backward(const void *h, const void *ga, hm_dtype dtype, int64
  *     [gate; up] = w13_e x[t],   e = ids[t,k] - first
  * x [T,H] bf16, row t from element t*ld on.  w13 [experts, 2 F, up(H,128)] (F rows of gate, then F of up) and
  * w2 [experts, H, up(F,128)] with their scales in the layout `weights` above.  logits, bias, router, topk_ids and topk_weights
- * as in hm_route, which is part of the call.  out [T,H] of out_dtype; a token without an expert here gets zeros.  Nothing is
- * rounded to 8 bits on the way: sums are fp32 and activations keep 16 bits (24 for fp32 results).  A token's output depends
- * on its own row, logits and experts alone.  With an exchange in between, the sum over the ranks is the layer's output.
+ * as in hm_route, which is part of the call.  out [T,H] of out_dtype; a token without an expert here gets zeros.  Nothing
+ * is rounded to 8 bits on the way: sums are fp32 and activations keep 16 bits (24 for fp32 results).  A token's output
+ * depends on its own row, logits and experts alone but for the order of its fp32 sums, which follows from the number of
+ * tokens and from all tokens' experts: the same call gives the same bits, the same token in another batch may differ by
+ * roundings.  With an exchange in between, the sum over the ranks is the layer's output.
  * workspace: hm_layer_few_workspace_bytes(T, K, H, F) bytes of device scratch, 16-byte aligned, not shared by calls that may
  * run at once.  Limits: T <= 64, T * K <= 1024, experts <= 1024, H <= 2^20, F <= 2^19,
  * min(experts, T * K) * ceil(F / 128) <= 2^20; beyond HM_ERR_SHAPE.
